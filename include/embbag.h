@@ -338,6 +338,169 @@ int embbag_baseline_touch_rows_split(int32_t batch, int64_t num_indices,
                                      const embbag_split_tables_t* tables, void* workspace,
                                      size_t workspace_bytes, hipStream_t stream);
 
+/* ---- An output head over an embedding table --------------------------------
+ * Operators beyond the paper's step, for a table that is also the matrix of a
+ * model's scores (next item, next token): 4-bit storage of its rows, bags and
+ * scores from that storage, what may be answered, and training against a
+ * teacher.  Conventions (streams, ownership, argument and data errors) are
+ * those of the header comment. */
+
+/* Element types of the buffers that take more than one. */
+#define EMBBAG_F32 0
+#define EMBBAG_BF16 1 /* bit patterns, stored to nearest, ties to even */
+
+/* Microscaled 4-bit storage (OCP Microscaling Formats v1.0: FP4 E2M1 elements,
+ * E8M0 scales, blocks of 32).  A table of M rows of dimension E (4 <= E <=
+ * 16384, E % 4 == 0) is two row-major device arrays:
+ *   codes  [M][ceil(E/32) * 16] uint8, 16-byte aligned: element e in byte e/2, the
+ *          even element in the low half; 0..7 = 0, 0.5, 1, 1.5, 2, 3, 4, 6 and 8..15
+ *          the same negated.  Elements past E are code 0.
+ *   scales [M][EMBBAG_MX4_SCALE_BYTES(E)] uint8, 4-byte aligned: byte b of block
+ *          e/32 stands for 2^(b - 127), 255 for NaN.  Bytes past the blocks are 0.
+ * An element's value is its code's times its block's scale. */
+#define EMBBAG_MX4_CODE_BYTES(E) ((((int64_t)(E) + 31) / 32) * 16)
+#define EMBBAG_MX4_SCALE_BYTES(E) ((((int64_t)(E) + 127) / 128) * 4)
+
+typedef struct {
+  int32_t num_tables;
+  int32_t dim;
+  const int64_t* rows;    /* host array */
+  uint8_t* const* codes;  /* host arrays of device pointers */
+  uint8_t* const* scales;
+} embbag_mx4_tables_t;
+
+/* Quantises rows of `src` ([rows][dim] of src_type, src_stride elements from row
+ * to row, src_stride % 4 == 0, 16-byte (FP32) or 8-byte (BF16) aligned):
+ * a block whose largest magnitude is a gets the scale 2^e,
+ * e = max(floor(log2 a) - 2, -127), and each element x the code nearest to
+ * x * 2^-e, ties to the even code, magnitudes above 6 to 6.  An all-zero block
+ * has the byte 0; a block with an infinity or a NaN has the byte 255 and codes 0,
+ * and reads back as NaN.
+ * With `row_ids` (device int32 [num_ids], nullable) only rows row_ids[i] are
+ * quantised, e.g. those an update touched; a row may repeat.  An id outside
+ * [0, rows) is skipped and reported through the nullable `d_status`
+ * (EMBBAG_ERR_INDEX_RANGE).  With null row_ids num_ids must be 0 and every row
+ * is quantised. */
+int embbag_mx4_quantize(const void* src, int32_t src_type, int64_t src_stride, int64_t rows,
+                        int32_t dim, const int32_t* row_ids, int64_t num_ids, uint8_t* codes,
+                        uint8_t* scales, int32_t* d_status, hipStream_t stream);
+
+/* Reads all rows back as values of dst_type ([rows][dim], dst_stride as above). */
+int embbag_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t dim,
+                          void* dst, int32_t dst_type, int64_t dst_stride, hipStream_t stream);
+
+/* embbag_forward_pooled from microscaled tables (E <= 1024), into FP32 or BF16
+ * pooled_out [T][B][E] (16- or 8-byte aligned).  Bags are summed in FP32. */
+int embbag_mx4_forward(const embbag_mx4_tables_t* tables, int32_t batch, const int32_t* indices,
+                       const int32_t* offsets, int64_t num_indices,
+                       const float* per_sample_weights, int32_t pooling, void* pooled_out,
+                       int32_t out_type, int32_t* d_status, hipStream_t stream);
+
+/* Scores of every row of a microscaled table W (`n` rows of dimension `k`):
+ *   out[i][j] = sum over e of q(x)[i][e] * W[j][e],   0 <= i < m,
+ * where q rounds each row of x ([m][k] of x_type, x_stride elements from row to
+ * row, alignment as embbag_mx4_quantize's src) to the table's storage as
+ * embbag_mx4_quantize does.  Products are exact, sums FP32.  `out`: [m][n] of
+ * out_type, out_stride >= n elements from row to row, no alignment beyond its
+ * elements'.  `workspace`: device scratch, 256-byte aligned. */
+size_t embbag_mx4_matmul_workspace_bytes(int32_t m, int64_t n, int32_t k);
+int embbag_mx4_matmul(const void* x, int32_t x_type, int64_t x_stride, int32_t m,
+                      const uint8_t* codes, const uint8_t* scales, int64_t n, int32_t k, void* out,
+                      int32_t out_type, int64_t out_stride, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream);
+
+/* The product's gradient with respect to x, straight through q:
+ *   dx[i][e] = sum over j of dy[i][j] * W[j][e].
+ * `dy`: [m][n] of dy_type, dy_stride >= n, no alignment beyond its elements';
+ * `dx`: [m][k] of dx_type, dx_stride and alignment as embbag_mx4_quantize's src.
+ * An FP32 dy enters with all its bits (as three BF16 terms); sums are FP32. */
+size_t embbag_mx4_matmul_grad_workspace_bytes(int32_t m, int64_t n, int32_t k);
+int embbag_mx4_matmul_grad(const void* dy, int32_t dy_type, int64_t dy_stride, int32_t m,
+                           const uint8_t* codes, const uint8_t* scales, int64_t n, int32_t k,
+                           void* dx, int32_t dx_type, int64_t dx_stride, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
+/* What may be answered: for every row r and token v of `logits` ([rows][vocab] of
+ * `type`, row strides in elements, no alignment beyond the elements'),
+ *   l = logits[r][v];
+ *   if v is in row r's list of seen tokens:  l = l > 0 ? l / repetition[r]
+ *                                                     : l * repetition[r];
+ *   c = its occurrences there from position prompt_lens[r] on;
+ *   if c > 0:  l -= frequency[r] * c + presence[r];
+ *   l += the bias of v in row r's list of biases, the last one of a repeated id;
+ *   out[r][v] = l, or -infinity (whatever l is) where the row's mask has no bit.
+ * The lists are bags: seen[seen_offsets[r] .. seen_offsets[r+1]) and
+ * bias_ids/biases[bias_offsets[r] .. bias_offsets[r+1]), offsets device int32
+ * [rows + 1] as those of the look-ups (0 first, non-decreasing, the count last).
+ * `masks`: device uint32 [num_masks][mask_stride], mask_stride >= ceil(vocab/32);
+ * bit v%32 of word v/32 set = v allowed.  Row r uses mask mask_ids[r] (negative:
+ * none), or mask r if mask_ids is null (num_masks >= rows then).
+ * Null lists, masks, prompt_lens (0) or factors (repetition 1, others 0) are left
+ * out.  `out` may be `logits` itself with the same stride; otherwise they must
+ * not overlap.  Arithmetic is FP32.  Bad offsets, an id outside [0, vocab) and a
+ * mask id of num_masks or more are data errors; the output is then unspecified. */
+typedef struct {
+  int32_t rows;
+  int32_t vocab;
+  int32_t type;
+  const void* logits;
+  int64_t logits_stride;
+  void* out;
+  int64_t out_stride;
+  const int32_t* seen;
+  const int32_t* seen_offsets;
+  int64_t num_seen;
+  const int32_t* prompt_lens;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_ids;
+  const int32_t* bias_offsets;
+  const float* biases;
+  int64_t num_biases;
+  const uint32_t* masks;
+  int64_t mask_stride;
+  int32_t num_masks;
+  const int32_t* mask_ids;
+} embbag_logits_t;
+
+int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStream_t stream);
+
+/* Distillation from a teacher's top logits.  For every row r, with z =
+ * logits[r]/temperature, q = softmax(z) over the vocabulary and p the softmax of
+ * teacher[r]/temperature over the row's entries (k with ids[r][k] >= 0):
+ *   loss[r] = w * temperature^2 * sum over k of p_k * (log p_k - log q[ids[r][k]]),
+ *   grad[r][v] = w * temperature * (q[v] - sum of p_k over k with ids[r][k] == v),
+ * w = row_weights[r] (null: 1); grad is the gradient of the loss.  p_k = 0 adds
+ * nothing.  A row is left out (loss +0, gradient +0) when its weight is 0, it has
+ * no entry, all its teacher logits are -infinity, or all its logits are.
+ * `logits`, `grad` ([rows][vocab] of `type`; grad nullable: the loss alone) have
+ * row strides in elements and no alignment beyond the elements'; grad may be
+ * `logits` itself with the same stride, and must not overlap it otherwise.
+ * ids: device int32 [rows][top] (negative: no entry), teacher: [rows][top] of
+ * teacher_type, 1 <= top <= 1024, 1e-6 <= temperature <= 1e6.  loss: FP32 [rows].  An id >= vocab is a data
+ * error; the row's outputs are then unspecified.  Sums are FP32. */
+typedef struct {
+  int32_t rows;
+  int32_t vocab;
+  int32_t type;
+  const void* logits;
+  int64_t logits_stride;
+  int32_t top;
+  const int32_t* ids;
+  int32_t teacher_type;
+  const void* teacher;
+  float temperature;
+  const float* row_weights;
+  float* loss;
+  void* grad;
+  int64_t grad_stride;
+} embbag_distill_t;
+
+size_t embbag_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
+int embbag_distill(const embbag_distill_t* args, void* workspace, size_t workspace_bytes,
+                   int32_t* d_status, hipStream_t stream);
+
 /* Waits for `stream` and returns the device status word (*d_status), or
  * EMBBAG_ERR_HIP if the wait or copy fails. */
 int embbag_status_read(const int32_t* d_status, hipStream_t stream);

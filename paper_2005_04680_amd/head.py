@@ -1,0 +1,327 @@
+"""The output head over an embedding table: thin binding, like the package's
+other entry points (device pointers and the current HIP stream to the C ABI of
+``include/embbag.h``, a status code back, buffer sizes checked first).
+
+4-bit microscaled tables (``Mx4Table``, ``Mx4Tables``): ``embbag_mx4_quantize``,
+``embbag_mx4_dequantize``, ``embbag_mx4_forward`` (bags), ``embbag_mx4_matmul``
+(scores of every row) and ``embbag_mx4_matmul_grad``.  Logits:
+``embbag_logits_process`` (penalties, biases, masks) and ``embbag_distill`` (loss
+and gradient against a teacher's top logits).
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import (EMBBAG_POOL_SUM, _check_bags, _check_numel, _dt, _I32, _need, _ptr, _status_ptr,
+               _stream, _U32, lib)
+
+EMBBAG_F32 = 0
+EMBBAG_BF16 = 1
+
+
+class _Mx4Tables(C.Structure):
+    _fields_ = [("num_tables", C.c_int32), ("dim", C.c_int32), ("rows", C.POINTER(C.c_int64)),
+                ("codes", C.POINTER(C.c_void_p)), ("scales", C.POINTER(C.c_void_p))]
+
+
+class _Logits(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("type", C.c_int32),
+                ("logits", C.c_void_p), ("logits_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_stride", C.c_int64),
+                ("seen", C.c_void_p), ("seen_offsets", C.c_void_p), ("num_seen", C.c_int64),
+                ("prompt_lens", C.c_void_p), ("repetition", C.c_void_p),
+                ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("bias_ids", C.c_void_p), ("bias_offsets", C.c_void_p), ("biases", C.c_void_p),
+                ("num_biases", C.c_int64),
+                ("masks", C.c_void_p), ("mask_stride", C.c_int64), ("num_masks", C.c_int32),
+                ("mask_ids", C.c_void_p)]
+
+
+class _Distill(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("type", C.c_int32),
+                ("logits", C.c_void_p), ("logits_stride", C.c_int64), ("top", C.c_int32),
+                ("ids", C.c_void_p), ("teacher_type", C.c_int32), ("teacher", C.c_void_p),
+                ("temperature", C.c_float), ("row_weights", C.c_void_p), ("loss", C.c_void_p),
+                ("grad", C.c_void_p), ("grad_stride", C.c_int64)]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        L = lib()
+        p, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+        L.embbag_mx4_quantize.argtypes = [p, i32, i64, i64, i32, p, i64, p, p, p, p]
+        L.embbag_mx4_dequantize.argtypes = [p, p, i64, i32, p, i32, i64, p]
+        L.embbag_mx4_forward.argtypes = [p, i32, p, p, i64, p, i32, p, i32, p, p]
+        L.embbag_mx4_matmul_workspace_bytes.argtypes = [i32, i64, i32]
+        L.embbag_mx4_matmul.argtypes = [p, i32, i64, i32, p, p, i64, i32, p, i32, i64, p, sz, p]
+        L.embbag_mx4_matmul_grad_workspace_bytes.argtypes = [i32, i64, i32]
+        L.embbag_mx4_matmul_grad.argtypes = [p, i32, i64, i32, p, p, i64, i32, p, i32, i64, p, sz,
+                                             p]
+        L.embbag_logits_process.argtypes = [p, p, p]
+        L.embbag_distill_workspace_bytes.argtypes = [i32, i32, i32]
+        L.embbag_distill.argtypes = [p, p, sz, p, p]
+        for n in ("mx4_quantize", "mx4_dequantize", "mx4_forward", "mx4_matmul",
+                  "mx4_matmul_grad", "logits_process", "distill"):
+            getattr(L, "embbag_" + n).restype = C.c_int
+        for n in ("mx4_matmul", "mx4_matmul_grad", "distill"):
+            getattr(L, f"embbag_{n}_workspace_bytes").restype = sz
+        _ready = L
+    return _ready
+
+
+# ---- marshalling helpers ---------------------------------------------------
+def _types():
+    import torch
+    return {torch.float32: EMBBAG_F32, torch.bfloat16: EMBBAG_BF16}
+
+
+_type_of = None
+
+
+def _matrix(t, cols, name):
+    """(pointer, type, row stride) of a 2-D FP32 or BF16 GPU tensor of `cols`
+    columns whose rows are contiguous."""
+    global _type_of
+    if _type_of is None:
+        _type_of = _types()
+    code = _type_of.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected float32 or bfloat16")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != cols:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected 2-D with {cols} columns")
+    s0, s1 = t.stride()
+    if shape[0] <= 1:
+        s0 = max(cols, (cols + 3) // 4 * 4)  # no second row: any stride
+    if s1 != 1 and cols > 1:
+        raise TypeError(f"{name}: rows must be contiguous")
+    if s0 < cols:
+        raise TypeError(f"{name}: rows overlap (stride {s0} for {cols} columns)")
+    return t.data_ptr(), code, s0
+
+
+def _list(entries, offsets, rows, name):
+    """Pointers and length of a list per row (None, None: none)."""
+    if offsets is None:
+        _need(entries is None, f"{name}: entries without offsets")
+        return None, None, 0
+    _check_numel(offsets, rows + 1, f"{name} offsets")
+    _need(entries is not None, f"{name}: offsets without entries")
+    return (_ptr(entries, _dt(*_I32), name), _ptr(offsets, _dt(*_I32), f"{name} offsets"),
+            entries.numel())
+
+
+def _per_row(t, rows, name, dtype="float32"):
+    _check_numel(t, rows, name)
+    return _ptr(t, _dt(dtype), name)
+
+
+def _ws(workspace):
+    if workspace is None:
+        return None, 0
+    return _ptr(workspace, None, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def mx4_code_bytes(dim: int) -> int:
+    """Bytes of a row of codes (EMBBAG_MX4_CODE_BYTES)."""
+    return (dim + 31) // 32 * 16
+
+
+def mx4_scale_bytes(dim: int) -> int:
+    """Bytes of a row of scales (EMBBAG_MX4_SCALE_BYTES)."""
+    return (dim + 127) // 128 * 4
+
+
+class Mx4Table:
+    """A 4-bit microscaled table: ``codes`` [M, mx4_code_bytes(dim)] and ``scales``
+    [M, mx4_scale_bytes(dim)], contiguous uint8 GPU tensors, which must keep
+    their storage while the object is in use."""
+
+    def __init__(self, codes, scales, dim):
+        dim = int(dim)
+        _need(len(codes.shape) == 2 and codes.shape[1] == mx4_code_bytes(dim),
+              f"codes: shape {tuple(codes.shape)}, expected [rows, {mx4_code_bytes(dim)}]")
+        _need(tuple(scales.shape) == (codes.shape[0], mx4_scale_bytes(dim)),
+              f"scales: shape {tuple(scales.shape)}, expected "
+              f"[{codes.shape[0]}, {mx4_scale_bytes(dim)}]")
+        self.codes_ptr = _ptr(codes, _dt("uint8"), "codes")
+        self.scales_ptr = _ptr(scales, _dt("uint8"), "scales")
+        self.codes, self.scales, self.dim, self.rows = codes, scales, dim, int(codes.shape[0])
+
+    @classmethod
+    def empty(cls, rows, dim, device="cuda"):
+        """A table of zeros."""
+        import torch
+        return cls(torch.zeros(rows, mx4_code_bytes(dim), dtype=torch.uint8, device=device),
+                   torch.zeros(rows, mx4_scale_bytes(dim), dtype=torch.uint8, device=device), dim)
+
+
+class Mx4Tables:
+    """Microscaled tables of one width with their C descriptor built once."""
+
+    def __init__(self, tables):
+        self.tables = list(tables)
+        T = len(self.tables)
+        self.dim = self.tables[0].dim if T else 0
+        for i, t in enumerate(self.tables):
+            _need(t.dim == self.dim, f"table {i}: dim {t.dim}, expected {self.dim} like table 0")
+        n = max(T, 1)
+        rows = (C.c_int64 * n)(*[t.rows for t in self.tables])
+        codes = (C.c_void_p * n)(*[t.codes_ptr for t in self.tables])
+        scales = (C.c_void_p * n)(*[t.scales_ptr for t in self.tables])
+        self._keep = (rows, codes, scales)
+        pp = C.POINTER(C.c_void_p)
+        self.struct = _Mx4Tables(T, self.dim, C.cast(rows, C.POINTER(C.c_int64)),
+                                 C.cast(codes, pp), C.cast(scales, pp))
+
+    def __len__(self):
+        return len(self.tables)
+
+    def __getitem__(self, i):
+        return self.tables[i]
+
+    def __iter__(self):
+        return iter(self.tables)
+
+
+# ---- entry points (same names as the C ABI) --------------------------------
+def embbag_mx4_quantize(src, table, row_ids=None, d_status=None, stream=None) -> int:
+    """Rows of ``src`` ([M, dim] FP32 or BF16) into ``table``: all of them, or those
+    that the int32 tensor ``row_ids`` names."""
+    p, ty, ld = _matrix(src, table.dim, "src")
+    _need(src.shape[0] == table.rows, f"src: {src.shape[0]} rows, expected {table.rows}")
+    ids = _ptr(row_ids, _dt(*_I32), "row_ids")
+    n = 0 if row_ids is None else row_ids.numel()
+    if row_ids is not None and n == 0:
+        return 0
+    return _lib().embbag_mx4_quantize(p, ty, ld, table.rows, table.dim, ids, n, table.codes_ptr,
+                                      table.scales_ptr, _status_ptr(d_status), _stream(stream))
+
+
+def embbag_mx4_dequantize(table, dst, stream=None) -> int:
+    """All rows of ``table`` as values into ``dst`` ([M, dim] FP32 or BF16)."""
+    p, ty, ld = _matrix(dst, table.dim, "dst")
+    _need(dst.shape[0] == table.rows, f"dst: {dst.shape[0]} rows, expected {table.rows}")
+    return _lib().embbag_mx4_dequantize(table.codes_ptr, table.scales_ptr, table.rows, table.dim, p,
+                                        ty, ld, _stream(stream))
+
+
+def embbag_mx4_forward(tables, batch, indices, offsets, pooled_out, per_sample_weights=None,
+                       pooling=EMBBAG_POOL_SUM, d_status=None, stream=None) -> int:
+    """``embbag_forward_pooled`` from ``Mx4Tables`` into FP32 or BF16 ``pooled_out``."""
+    T, dim = len(tables), tables.dim
+    _check_bags(T, batch, offsets)
+    _check_numel(pooled_out, T * batch * dim, "pooled_out (num_tables x batch x dim)")
+    _check_numel(per_sample_weights, indices.numel(), "per_sample_weights")
+    out = _ptr(pooled_out, _dt("float32", "bfloat16"), "pooled_out")
+    return _lib().embbag_mx4_forward(
+        C.byref(tables.struct), int(batch), _ptr(indices, _dt(*_I32), "indices"),
+        _ptr(offsets, _dt(*_I32), "offsets"), indices.numel(),
+        _ptr(per_sample_weights, _dt("float32"), "per_sample_weights"), int(pooling), out,
+        EMBBAG_BF16 if pooled_out.element_size() == 2 else EMBBAG_F32, _status_ptr(d_status),
+        _stream(stream))
+
+
+def embbag_mx4_matmul_workspace_bytes(m, n, k) -> int:
+    return int(_lib().embbag_mx4_matmul_workspace_bytes(int(m), int(n), int(k)))
+
+
+def embbag_mx4_matmul(x, table, out, workspace, stream=None) -> int:
+    """Scores of every row of ``table``: ``out`` [m, M] = q(``x`` [m, dim]) W^T."""
+    p, ty, ld = _matrix(x, table.dim, "x")
+    q, tq, lq = _matrix(out, table.rows, "out")
+    m = x.shape[0]
+    _need(out.shape[0] == m, f"out: {out.shape[0]} rows, expected {m}")
+    w, n = _ws(workspace)
+    return _lib().embbag_mx4_matmul(p, ty, ld, m, table.codes_ptr, table.scales_ptr, table.rows,
+                                    table.dim, q, tq, lq, w, n, _stream(stream))
+
+
+def embbag_mx4_matmul_grad_workspace_bytes(m, n, k) -> int:
+    return int(_lib().embbag_mx4_matmul_grad_workspace_bytes(int(m), int(n), int(k)))
+
+
+def embbag_mx4_matmul_grad(dy, table, dx, workspace, stream=None) -> int:
+    """Gradient of ``embbag_mx4_matmul`` with respect to x: ``dx`` = ``dy`` W."""
+    p, ty, ld = _matrix(dy, table.rows, "dy")
+    q, tq, lq = _matrix(dx, table.dim, "dx")
+    m = dy.shape[0]
+    _need(dx.shape[0] == m, f"dx: {dx.shape[0]} rows, expected {m}")
+    w, n = _ws(workspace)
+    return _lib().embbag_mx4_matmul_grad(p, ty, ld, m, table.codes_ptr, table.scales_ptr,
+                                         table.rows, table.dim, q, tq, lq, w, n, _stream(stream))
+
+
+def embbag_logits_process(logits, out, seen=None, seen_offsets=None, prompt_lens=None,
+                          repetition=None, frequency=None, presence=None, bias_ids=None,
+                          bias_offsets=None, biases=None, masks=None, mask_ids=None, d_status=None,
+                          stream=None) -> int:
+    """Penalties for seen tokens, biases and masks: ``logits`` [rows, vocab] into
+    ``out`` (which may be ``logits``).  Every argument after ``out`` is optional."""
+    vocab = logits.shape[1] if len(logits.shape) == 2 else -1
+    p, ty, ld = _matrix(logits, vocab, "logits")
+    q, tq, lq = _matrix(out, vocab, "out")
+    if tq != ty:
+        raise TypeError(f"out: dtype {out.dtype}, expected {logits.dtype} like logits")
+    rows = logits.shape[0]
+    _need(out.shape[0] == rows, f"out: {out.shape[0]} rows, expected {rows}")
+    a = _Logits(rows, vocab, ty, p, ld, q, lq)
+    a.seen, a.seen_offsets, a.num_seen = _list(seen, seen_offsets, rows, "seen")
+    a.prompt_lens = _per_row(prompt_lens, rows, "prompt_lens", "int32")
+    a.repetition = _per_row(repetition, rows, "repetition")
+    a.frequency = _per_row(frequency, rows, "frequency")
+    a.presence = _per_row(presence, rows, "presence")
+    a.bias_ids, a.bias_offsets, a.num_biases = _list(bias_ids, bias_offsets, rows, "bias_ids")
+    if bias_ids is not None:
+        _need(biases is not None, "bias_ids without biases")
+    _check_numel(biases, a.num_biases, "biases")
+    a.biases = _ptr(biases, _dt("float32"), "biases")
+    if masks is not None:
+        _need(len(masks.shape) == 2 and masks.shape[1] * 32 >= vocab,
+              f"masks: shape {tuple(masks.shape)}, expected 2-D with at least "
+              f"{(vocab + 31) // 32} words a row")
+        a.masks = _ptr(masks, _dt(*_U32), "masks")
+        a.num_masks, a.mask_stride = masks.shape
+        if mask_ids is None:
+            _need(masks.shape[0] >= rows, f"masks: {masks.shape[0]} for {rows} rows and no mask_ids")
+    a.mask_ids = _per_row(mask_ids, rows, "mask_ids", "int32")
+    return _lib().embbag_logits_process(C.byref(a), _status_ptr(d_status), _stream(stream))
+
+
+def embbag_distill_workspace_bytes(rows, vocab, top) -> int:
+    return int(_lib().embbag_distill_workspace_bytes(int(rows), int(vocab), int(top)))
+
+
+def embbag_distill(logits, teacher_ids, teacher_logits, temperature, loss, workspace, grad=None,
+                   row_weights=None, d_status=None, stream=None) -> int:
+    """Loss of every row of ``logits`` [rows, vocab] against a teacher's top logits
+    ([rows, top]; an id below 0 is no entry) and, with ``grad``, its gradient (into
+    ``logits`` itself if that is given)."""
+    vocab = logits.shape[1] if len(logits.shape) == 2 else -1
+    p, ty, ld = _matrix(logits, vocab, "logits")
+    rows = logits.shape[0]
+    _need(len(teacher_ids.shape) == 2 and teacher_ids.shape[0] == rows,
+          f"teacher_ids: shape {tuple(teacher_ids.shape)}, expected [{rows}, top]")
+    top = teacher_ids.shape[1]
+    _check_numel(teacher_logits, rows * top, "teacher_logits")
+    _check_numel(loss, rows, "loss")
+    a = _Distill(rows, vocab, ty, p, ld, top, _ptr(teacher_ids, _dt(*_I32), "teacher_ids"))
+    a.teacher = _ptr(teacher_logits, _dt("float32", "bfloat16"), "teacher_logits")
+    a.teacher_type = EMBBAG_BF16 if teacher_logits.element_size() == 2 else EMBBAG_F32
+    a.temperature = float(temperature)
+    a.row_weights = _per_row(row_weights, rows, "row_weights")
+    a.loss = _ptr(loss, _dt("float32"), "loss")
+    if grad is not None:
+        q, tq, lq = _matrix(grad, vocab, "grad")
+        if tq != ty:
+            raise TypeError(f"grad: dtype {grad.dtype}, expected {logits.dtype} like logits")
+        _need(grad.shape[0] == rows, f"grad: {grad.shape[0]} rows, expected {rows}")
+        a.grad, a.grad_stride = q, lq
+    w, n = _ws(workspace)
+    return _lib().embbag_distill(C.byref(a), w, n, _status_ptr(d_status), _stream(stream))
