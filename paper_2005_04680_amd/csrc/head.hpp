@@ -102,6 +102,12 @@ __device__ __forceinline__ u4 pack16(const float (&v)[8]) {
             pack_bf16(v[6], v[7])};
 }
 
+// 16 bytes to or from a row of any alignment (the hardware takes vector accesses at element
+// boundaries).
+typedef u4 u4_any __attribute__((aligned(2)));
+__device__ __forceinline__ void store16(void* p, const u4& v) { *static_cast<u4_any*>(p) = v; }
+__device__ __forceinline__ u4 load16(const void* p) { return *static_cast<const u4_any*>(p); }
+
 // Elements before the first 16-byte boundary at or after p.
 template <class T>
 __device__ __forceinline__ int head_of(const T* p) {
