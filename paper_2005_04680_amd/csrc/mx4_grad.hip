@@ -1,83 +1,353 @@
 // Gradient of the scores with respect to x: dx = dy W, W a 4-bit microscaled
 // table.
+//
+// The contraction runs over W's rows, across its blocks: W's values go through the
+// BF16 matrix instructions, which hold every code times its scale exactly (an element is
+// 0.5 to 6 times a power of two).  A block of 256 threads makes a BK x BM tile of dx^T over a
+// range of W's rows, in steps of 64 rows.  Per step, double-buffered:
+//   - dy's tile goes to LDS as it is, [BM][64] BF16, the 16-byte place of a row exchanged
+//     with the row's number (row % 8) so that fragments spread over the banks;
+//   - W's tile is converted on its way, [64][BK] BF16, rows 32 bytes apart in the banks, and is
+//     turned around by the transposing LDS read that makes the fragments.
+// Where tiles alone leave compute units idle the rows of W are split over blocks as
+// well; the FP32 parts are then added in order by a second kernel.
+//
+// An FP32 dy is the sum of three BF16 terms of 8 bits each, by truncation; the steps go through
+// the terms one after the other.
 #include "head.hpp"
 
 namespace embbag {
 namespace {
 
-constexpr int kRowsPerBlock = 8;  // rows of dy
-constexpr int kStep = 64;         // rows of W whose dy a block holds at a time
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef u4 u4_el __attribute__((aligned(2)));
+typedef f4 f4_el __attribute__((aligned(4)));
 
-// A thread holds 8 columns of 8 rows of dx.
-template <class TY, class TX>
-__global__ __launch_bounds__(kWave) void scores_grad(const TY* __restrict__ dy, int64_t ldy,
-                                                     int32_t m, Mx4View w, uint32_t ktiles,
-                                                     TX* __restrict__ dx, int64_t ldx) {
-  __shared__ float y[kRowsPerBlock][kStep];
+constexpr int kRows = 64;                   // rows of W per step
+constexpr int kYRow = kRows * 2;            // bytes of a row of dy's tile
+
+template <int BK>
+constexpr int kWRow = BK * 2 + 32;          // bytes of a row of W's tile
+template <int BK, int BM>
+constexpr int kStage = BM * kYRow + kRows * kWRow<BK>;
+
+// Term t of x (t = 0, 1, 2): its 8 highest bits, the next 8, the rest, as a BF16 pattern.
+// An infinity or a NaN is its own first term and leaves nothing.
+__device__ __forceinline__ uint32_t bf16_term(float x, int t) {
+  uint32_t u = __float_as_uint(x);
+  const bool special = (u & 0x7F800000u) == 0x7F800000u;
+  if (special) u |= (u & 0x007FFFFFu) != 0u ? 0x00400000u : 0u;
+  for (int i = 0; i < t; ++i) {
+    const float rest = __uint_as_float(u) - __uint_as_float(u & 0xFFFF0000u);
+    u = special ? 0u : __float_as_uint(rest);
+  }
+  return u >> 16;
+}
+
+// 8 elements of a row of dy as BF16 (`term` of FP32 ones).
+__device__ __forceinline__ u4 load8(const __bf16* p, int) {
+  return *reinterpret_cast<const u4_el*>(p);
+}
+__device__ __forceinline__ u4 load8(const float* p, int term) {
+  const f4 a = *reinterpret_cast<const f4_el*>(p), b = *reinterpret_cast<const f4_el*>(p + 4);
+  return u4{bf16_term(a.x, term) | (bf16_term(a.y, term) << 16),
+            bf16_term(a.z, term) | (bf16_term(a.w, term) << 16),
+            bf16_term(b.x, term) | (bf16_term(b.y, term) << 16),
+            bf16_term(b.z, term) | (bf16_term(b.w, term) << 16)};
+}
+// The first n of them, zeros behind.
+__device__ u4 load8_some(const __bf16* p, int n, int) {
+  const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+  uint32_t v[4] = {};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) v[e / 2] |= uint32_t(q[e]) << (16 * (e % 2));
+  return u4{v[0], v[1], v[2], v[3]};
+}
+__device__ u4 load8_some(const float* p, int n, int term) {
+  uint32_t v[4] = {};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) v[e / 2] |= bf16_term(p[e], term) << (16 * (e % 2));
+  return u4{v[0], v[1], v[2], v[3]};
+}
+
+// A word of codes as 8 BF16 values.
+__device__ __forceinline__ u4 bf16_values8(uint32_t c, float scale) {
+  return u4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3))};
+}
+
+// WK x WM wavefronts, each TK x TM products of 32 x 32.  Block: split z of the rows of W
+// (`per` steps each), k tile, m tile.  `dx` is the output, or part z of the parts.
+template <int TK, int TM, int WK, int WM, class TY, class TX>
+__global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy, int64_t ldy,
+                                                       int32_t m, Mx4View w, uint32_t ktiles,
+                                                       uint32_t mtiles, int32_t per,
+                                                       TX* __restrict__ dx, int64_t ldx,
+                                                       int64_t part_stride) {
+  static_assert(WK * WM == kWavesPerBlock, "four wavefronts");
+  constexpr int BK = 32 * TK * WK, BM = 32 * TM * WM;
+  constexpr int STAGE = kStage<BK, BM>;
+  constexpr int YL = BM / 32;                              // loads of dy per thread
+  constexpr int WL = (kRows * BK / 32 + kBlock - 1) / kBlock;  // blocks of W per thread
+  constexpr bool kTerms = sizeof(TY) == 4;
+  extern __shared__ __align__(16) uint8_t lds[];
+
+  const int lane = lane_id(), wave = wave_id();
+  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t tiles = ktiles * mtiles;
+  const uint32_t z = id / tiles, tile = id - z * tiles;
+  const uint32_t mt = tile / ktiles, kt = tile - mt * ktiles;
+  const int m0 = int(mt) * BM, k0 = int(kt) * BK;
+  const int64_t n0 = int64_t(z) * per * kRows;
+  const int64_t left = w.rows - n0;
+  const int rows = int(min(left, int64_t(per) * kRows));  // of W, in this block (>= 1)
+  const int steps = (rows + kRows - 1) / kRows;
   const int nb = mx4_blocks(w.dim), sb = mx4_scale_bytes(w.dim);
-  const uint32_t kt = blockIdx.x % ktiles, mt = blockIdx.x / ktiles;
-  const int e0 = (int(kt) * kWave + int(threadIdx.x)) * 8;
-  const int m0 = int(mt) * kRowsPerBlock;
-  const bool in = e0 < w.dim;
-  float acc[kRowsPerBlock][8] = {};
-  for (int64_t n0 = 0; n0 < w.rows; n0 += kStep) {
-    __syncthreads();
+
+  // dy: load i of this thread is 8 columns (8 * yc ..) of row i * 32 + threadIdx.x / 8.
+  const int yr = threadIdx.x / 8, yc = threadIdx.x % 8;
+  const TY* ysrc[YL];
 #pragma unroll
-    for (int i = 0; i < kRowsPerBlock; ++i) {
-      const int64_t n = n0 + threadIdx.x;
-      y[i][threadIdx.x] =
-          m0 + i < m && n < w.rows ? to_f32(dy[int64_t(m0 + i) * ldy + n]) : 0.f;
+  for (int i = 0; i < YL; ++i)
+    ysrc[i] = dy + int64_t(min(m0 + i * 32 + yr, m - 1)) * ldy + n0 + yc * 8;
+  // W: block i of this thread is number wb + 4 i (of the tile's BK/32) of row wr.
+  constexpr int PER = BK / 32 < 4 ? BK / 32 : 4;  // threads per row
+  const int wr = threadIdx.x / PER, wb = threadIdx.x % PER;
+  const bool wact = wr < kRows;
+  u4 yv[YL], wv[WL];
+  uint32_t ws[WL];
+
+  auto load = [&](int s) {
+    const int step = kTerms ? s / 3 : s;
+    const int r0 = step * kRows;
+    const int term = kTerms ? s - step * 3 : 0;
+    if (r0 + kRows <= rows) {
+#pragma unroll
+      for (int i = 0; i < YL; ++i) yv[i] = load8(ysrc[i] + r0, term);
+    } else {
+#pragma unroll
+      for (int i = 0; i < YL; ++i) yv[i] = load8_some(ysrc[i] + r0, rows - r0 - yc * 8, term);
     }
-    __syncthreads();
-    if (!in) continue;
-    const int steps = int(min(int64_t(kStep), w.rows - n0));
-    for (int j = 0; j < steps; ++j) {
-      const int64_t row = n0 + j;
-      const uint32_t c = *reinterpret_cast<const uint32_t*>(w.codes + row * nb * 16 + e0 / 2);
-      float v[8];
-      mx4_values8(c, mx4_scale(w.scales[row * sb + e0 / kMxBlock]), v);
+    const bool in = wact && r0 + wr < rows;
+    const int64_t row = n0 + min(r0 + wr, rows - 1);
 #pragma unroll
-      for (int i = 0; i < kRowsPerBlock; ++i) {
+    for (int i = 0; i < WL; ++i) {
+      const int b = min(k0 / kMxBlock + wb + 4 * i, nb - 1);
+      wv[i] = *reinterpret_cast<const u4*>(w.codes + (row * nb + b) * 16);
+      ws[i] = w.scales[row * sb + b];
+      if (!in) wv[i] = u4{0u, 0u, 0u, 0u}, ws[i] = 0u;
+    }
+  };
+  auto store = [&](int buf) {
+    uint8_t* ys = lds + buf * STAGE;
+    uint8_t* wst = ys + BM * kYRow + wr * kWRow<BK>;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[i][e] = fmaf(y[i][j], v[e], acc[i][e]);
+    for (int i = 0; i < YL; ++i)
+      *reinterpret_cast<u4*>(ys + (i * 32 + yr) * kYRow + (yc ^ (yr & 7)) * 16) = yv[i];
+    if (wact) {
+#pragma unroll
+      for (int i = 0; i < WL; ++i) {
+        const float s = mx4_scale(ws[i]);
+        u4* p = reinterpret_cast<u4*>(wst + (wb + 4 * i) * 64);
+        p[0] = bf16_values8(wv[i].x, s);
+        p[1] = bf16_values8(wv[i].y, s);
+        p[2] = bf16_values8(wv[i].z, s);
+        p[3] = bf16_values8(wv[i].w, s);
       }
     }
-  }
-  if (!in) return;
+  };
+
+  const int wk = wave % WK, wm = wave / WK;
+  const int row = lane % 32, half = lane / 32;
+  f16v acc[TK][TM];
 #pragma unroll
-  for (int i = 0; i < kRowsPerBlock; ++i) {
-    if (m0 + i >= m) break;
-    TX* p = dx + int64_t(m0 + i) * ldx + e0;
-    store4(p, f4{acc[i][0], acc[i][1], acc[i][2], acc[i][3]});
-    if (e0 + 4 < w.dim) store4(p + 4, f4{acc[i][4], acc[i][5], acc[i][6], acc[i][7]});
+  for (int i = 0; i < TK; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f16v{};
+
+  // Fragments of part p (rows 16 p .. 16 p + 15): lane l holds column l % 32 and 8 rows from
+  // 8 * (l / 32).  W's come from two transposing reads: 16 lanes bring 4 rows of 16 columns
+  // and each leaves with its column.
+  const int yfrag = (wm * TM * 32 + row) * kYRow;
+  const int wfrag = BM * kYRow + (half * 8 + (lane % 16) / 4) * kWRow<BK> +
+                    (wk * TK * 32 + (lane / 16 % 2) * 16 + (lane % 4) * 4) * 2;
+  u4 a[2][TK], b[2][TM];
+  auto fetch = [&](int buf, int p) {
+    const uint8_t* st = lds + buf * STAGE;
+#pragma unroll
+    for (int i = 0; i < TK; ++i) {
+      const uint8_t* q = st + wfrag + p * 16 * kWRow<BK> + i * 64;
+      typedef __attribute__((address_space(3))) s4v* lds4;
+      const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)q);
+      const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(q + 4 * kWRow<BK>));
+      const u2 l2 = __builtin_bit_cast(u2, lo), h2 = __builtin_bit_cast(u2, hi);
+      a[p & 1][i] = u4{l2.x, l2.y, h2.x, h2.y};
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      b[p & 1][i] = *reinterpret_cast<const u4*>(st + yfrag + i * 32 * kYRow +
+                                                 ((p * 2 + half) ^ (row & 7)) * 16);
+  };
+  auto products = [&](int p) {
+#pragma unroll
+    for (int i = 0; i < TK; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf8, a[p & 1][i]), __builtin_bit_cast(bf8, b[p & 1][j]), acc[i][j], 0,
+            0, 0);
+  };
+
+  const int total = kTerms ? steps * 3 : steps;
+  load(0);
+  store(0);
+  if (total > 1) load(1);
+  for (int s = 0; s < total; ++s) {
+    __syncthreads();
+    fetch(s & 1, 0);
+    fetch(s & 1, 1);
+    products(0);
+    if (s + 1 < total) store(~s & 1);
+    fetch(s & 1, 2);
+    if (s + 2 < total) load(s + 2);
+    products(1);
+    fetch(s & 1, 3);
+    products(2);
+    products(3);
+  }
+
+  TX* out = dx + int64_t(z) * part_stride;
+#pragma unroll
+  for (int j = 0; j < TM; ++j) {
+    const int mm = m0 + (wm * TM + j) * 32 + row;
+    if (mm >= m) continue;
+#pragma unroll
+    for (int i = 0; i < TK; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int k = k0 + (wk * TK + i) * 32 + q * 8 + half * 4;
+        if (k < w.dim)
+          store4(out + int64_t(mm) * ldx + k,
+                 f4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2],
+                    acc[i][j][q * 4 + 3]});
+      }
   }
 }
 
+// dx = the sum of the parts [splits][m][k], in order.
+template <class TX>
+__global__ __launch_bounds__(kBlock) void grad_join(const float* __restrict__ parts, int32_t splits,
+                                                    int32_t m, FastDiv k4, TX* __restrict__ dx,
+                                                    int64_t ldx) {
+  const int64_t n = int64_t(m) * k4.div;
+  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+  if (i >= n) return;
+  f4 s = load4(parts + i * 4);
+  for (int z = 1; z < splits; ++z) s += load4(parts + (z * n + i) * 4);
+  const uint32_t row = quotient(uint32_t(i), k4);
+  store4(dx + int64_t(row) * ldx + (uint32_t(i) - row * k4.div) * 4, s);
+}
+
+// Tile and split of a gradient.
+struct GradPlan {
+  int bk, bm;
+  uint32_t ktiles, mtiles, splits;
+  int32_t per;  // steps per split
+};
+GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
+  GradPlan p = {};
+  if (m == 0) return p;
+  p.bk = k > 128 ? 256 : 128;
+  p.bm = m > 64 ? 256 : (m > 32 ? 64 : 32);
+  p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
+  p.mtiles = uint32_t((m + p.bm - 1) / p.bm);
+  const int64_t steps = (n + kRows - 1) / kRows;
+  const int64_t tiles = int64_t(p.ktiles) * p.mtiles;
+  int64_t splits = kNumCu * (p.bm > 64 ? 1 : 2) / tiles;
+  if (splits > steps / 4) splits = steps / 4;
+  if (splits < 1) splits = 1;
+  // (Ranges of rows fit 31 bits.)
+  while (steps / splits > (int64_t(1) << 24)) ++splits;
+  p.per = int32_t((steps + splits - 1) / splits);
+  p.splits = uint32_t((steps + p.per - 1) / p.per);
+  return p;
+}
+
+template <int TK, int TM, int WK, int WM, class TY, class TX>
+void launch_tile(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, const Mx4View& w,
+                 TX* dx, int64_t ldx, int64_t part_stride, hipStream_t st) {
+  auto kernel = grad_tile<TK, TM, WK, WM, TY, TX>;
+  constexpr int lds = 2 * kStage<32 * TK * WK, 32 * TM * WM>;
+  if (lds > 65536)
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  hipLaunchKernelGGL(kernel, dim3(p.ktiles * p.mtiles * p.splits), dim3(kBlock), lds, st,
+                     static_cast<const TY*>(dy), ldy, m, w, p.ktiles, p.mtiles, p.per, dx, ldx,
+                     part_stride);
+}
+
 template <class TY, class TX>
-void launch_simple(const void* dy, int64_t ldy, int32_t m, const Mx4View& w, void* dx, int64_t ldx,
-                   hipStream_t st) {
-  const uint32_t ktiles = uint32_t((w.dim + kWave * 8 - 1) / (kWave * 8));
-  const dim3 grid(ktiles * unsigned((m + kRowsPerBlock - 1) / kRowsPerBlock));
-  hipLaunchKernelGGL((scores_grad<TY, TX>), grid, dim3(kWave), 0, st, static_cast<const TY*>(dy),
-                     ldy, m, w, ktiles, static_cast<TX*>(dx), ldx);
+void launch_plan(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, const Mx4View& w,
+                 TX* dx, int64_t ldx, int64_t ps, hipStream_t st) {
+  if (p.bk == 256) {
+    if (p.bm == 256)
+      launch_tile<4, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    else if (p.bm == 64)
+      launch_tile<2, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    else
+      launch_tile<2, 1, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+  } else {
+    if (p.bm == 256)
+      launch_tile<2, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    else if (p.bm == 64)
+      launch_tile<1, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    else
+      launch_tile<1, 1, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+  }
+}
+
+template <class TX>
+void launch_grad(const GradPlan& p, const void* dy, bool dy_bf16, int64_t ldy, int32_t m,
+                 const Mx4View& w, TX* dx, int64_t ldx, float* parts, hipStream_t st) {
+  if (p.splits == 1) {
+    if (dy_bf16)
+      launch_plan<__bf16>(p, dy, ldy, m, w, dx, ldx, 0, st);
+    else
+      launch_plan<float>(p, dy, ldy, m, w, dx, ldx, 0, st);
+    return;
+  }
+  const int64_t ps = int64_t(m) * w.dim;
+  if (dy_bf16)
+    launch_plan<__bf16>(p, dy, ldy, m, w, parts, w.dim, ps, st);
+  else
+    launch_plan<float>(p, dy, ldy, m, w, parts, w.dim, ps, st);
+  const int64_t n = ps / 4;
+  hipLaunchKernelGGL(grad_join<TX>, dim3(unsigned((n + kBlock - 1) / kBlock)), dim3(kBlock), 0, st,
+                     parts, int32_t(p.splits), m, fast_div(uint32_t(w.dim / 4)), dx, ldx);
 }
 
 }  // namespace
 
-size_t mx4_matmul_grad_workspace(int32_t m, int64_t n, int32_t k) { return 256; }
+size_t mx4_matmul_grad_workspace(int32_t m, int64_t n, int32_t k) {
+  const GradPlan p = grad_plan(m, n, k);
+  return p.splits > 1 ? (size_t(p.splits) * size_t(m) * size_t(k) * 4 + 255) / 256 * 256 : 0;
+}
 
 hipError_t launch_mx4_matmul_grad(const void* dy, bool dy_bf16, int64_t dy_stride, int32_t m,
                                   const Mx4View& w, void* dx, bool dx_bf16, int64_t dx_stride,
                                   char* ws, hipStream_t st) {
   if (m == 0) return hipSuccess;
-  if (dy_bf16 && dx_bf16)
-    launch_simple<__bf16, __bf16>(dy, dy_stride, m, w, dx, dx_stride, st);
-  else if (dy_bf16)
-    launch_simple<__bf16, float>(dy, dy_stride, m, w, dx, dx_stride, st);
-  else if (dx_bf16)
-    launch_simple<float, __bf16>(dy, dy_stride, m, w, dx, dx_stride, st);
+  const GradPlan p = grad_plan(m, w.rows, w.dim);
+  float* parts = reinterpret_cast<float*>(ws);
+  if (dx_bf16)
+    launch_grad(p, dy, dy_bf16, dy_stride, m, w, static_cast<__bf16*>(dx), dx_stride, parts, st);
   else
-    launch_simple<float, float>(dy, dy_stride, m, w, dx, dx_stride, st);
+    launch_grad(p, dy, dy_bf16, dy_stride, m, w, static_cast<float*>(dx), dx_stride, parts, st);
   return hipGetLastError();
 }
 
