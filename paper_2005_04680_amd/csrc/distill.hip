@@ -1,17 +1,26 @@
 // Distillation from a teacher's top logits: loss and its gradient.
 //
-// Two kernels over slices of rows.  `distill_sums` leaves, per slice, the largest logit, the
-// sum of exp2((x - largest) * c) (c = log2(e) / temperature) and the slice's
-// part of sum_k p_k x[id_k]; `distill_grad` joins a row's parts in order and
-// writes the slice's gradient.  The teacher's softmax is small: every block makes it again.
+// With many rows a block takes a whole one and keeps it in registers (up to 256 KB: 16 vectors
+// of 16 bytes for each of 1024 threads): the row is read once for its largest logit, the
+// sum of the exponentials and the gradient, which is written once.  What does not fit is read
+// again, from the caches if they still hold it.  With few rows a row is split into slices, one block
+// each: a first kernel leaves every slice's largest logit and sum, a second joins a row's parts
+// in order and writes the gradient.
+//
+// exp(x) is taken as 2^((x - largest) * log2(e) / temperature).  The teacher's entries are few: one
+// wavefront makes their softmax while the row is on its way.  The entry that names an id
+// first subtracts all its entries' probabilities, after the row has been written: no atomics.
 #include "head.hpp"
 
 namespace embbag {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kSlice = 8192;  // logits per block
+constexpr int kRowThreads = 1024;
+constexpr int kPer = kMaxTeacher / kBlock;  // entries per thread of the smallest block
+
+__device__ __forceinline__ float low() { return -__builtin_inff(); }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 struct Part {
   float top, sum, cross;
@@ -19,7 +28,8 @@ struct Part {
 
 struct DistillDev {
   embbag_distill_t a;
-  uint32_t slices;
+  int32_t slice;    // elements per slice
+  uint32_t slices;  // per row
   Part* parts;
 };
 
@@ -31,201 +41,406 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (int j = 1; j < kWave; j *= 2) v += __shfl_xor(v, j, kWave);
   return v;
 }
-// Over the block, to every thread; `s` has a float per wavefront.
-__device__ __forceinline__ float block_max(float v, float* s) {
-  v = wave_max(v);
-  __syncthreads();
-  if (lane_id() == 0) s[wave_id()] = v;
-  __syncthreads();
-  v = s[0];
-  for (int w = 1; w < int(blockDim.x) / kWave; ++w) v = fmaxf(v, s[w]);
-  return v;
-}
-__device__ __forceinline__ float block_sum(float v, float* s) {
-  v = wave_sum(v);
-  __syncthreads();
-  if (lane_id() == 0) s[wave_id()] = v;
-  __syncthreads();
-  v = s[0];
-  for (int w = 1; w < int(blockDim.x) / kWave; ++w) v += s[w];
-  return v;
-}
 
-// The teacher's softmax of row r: ids and probabilities to LDS; returns whether the row
-// counts (weight, entries), and sum p log p in *plogp.
-__device__ __forceinline__ bool teacher_row(const embbag_distill_t& a, int r, int* ids, float* p,
-                                            float* red, float* plogp, int* err) {
-  const float w = a.row_weights != nullptr ? a.row_weights[r] : 1.f;
+// A row's teacher, in LDS.
+struct Teacher {
+  int ids[kMaxTeacher];
+  float p[kMaxTeacher];
+  float plogp;
+  int live;
+  float red[3][kRowThreads / kWave];
+};
+
+// The softmax of row r's entries, by one wavefront: ids (-1: none), probabilities, the sum of
+// p log p, and whether the row has any entry that is not -infinity.
+__device__ __forceinline__ void teacher_row(const embbag_distill_t& a, int r, Teacher& t,
+                                            int32_t* status) {
   const float inv_t = 1.f / a.temperature;
   const int64_t row = int64_t(r) * a.top;
-  const float low = -__builtin_inff();
-  float top = low, some = 0.f;
-  for (int k = threadIdx.x; k < a.top; k += blockDim.x) {
+  float top = low();
+  bool some = false, bad = false;
+  for (int k = lane_id(); k < a.top; k += kWave) {
     int id = a.ids[row + k];
-    if (id >= a.vocab) {
-      *err = EMBBAG_ERR_INDEX_RANGE;
-      id = -1;
-    }
-    const float t = a.teacher_type == EMBBAG_BF16
+    bad = bad || id >= a.vocab;
+    if (id >= a.vocab) id = -1;
+    const float x = a.teacher_type == EMBBAG_BF16
                         ? to_f32(static_cast<const __bf16*>(a.teacher)[row + k])
                         : static_cast<const float*>(a.teacher)[row + k];
-    ids[k] = id;
-    p[k] = id >= 0 ? t * inv_t : low;
-    top = id >= 0 ? fmaxf(top, t * inv_t) : top;
-    if (id >= 0 && t != low) some = 1.f;  // (a NaN as well)
+    t.ids[k] = id;
+    t.p[k] = id >= 0 ? x * inv_t : low();
+    if (id >= 0) top = fmaxf(top, x * inv_t);
+    some = some || (id >= 0 && x != low());  // (a NaN as well)
   }
-  top = block_max(top, red);
-  const bool live = w != 0.f && block_max(some, red) != 0.f;
-  const float ref = top == low ? 0.f : top;
+  if (bad && status != nullptr) atomicMin(status, EMBBAG_ERR_INDEX_RANGE);
+  top = wave_max(top);
+  const float ref = top == low() ? 0.f : top;
   float sum = 0.f;
-  for (int k = threadIdx.x; k < a.top; k += blockDim.x)
-    sum += ids[k] >= 0 ? __builtin_exp2f((p[k] - ref) * kLog2e) : 0.f;
-  sum = block_sum(sum, red);
+  for (int k = lane_id(); k < a.top; k += kWave)
+    sum += t.ids[k] >= 0 ? exp2_of((t.p[k] - ref) * kLog2e) : 0.f;
+  sum = wave_sum(sum);
   const float inv = 1.f / sum, log_sum = __builtin_logf(sum);
   float pl = 0.f;
-  for (int k = threadIdx.x; k < a.top; k += blockDim.x) {
-    const float z = p[k] - ref;
-    const float q = ids[k] >= 0 ? __builtin_exp2f(z * kLog2e) * inv : 0.f;
-    p[k] = q;
+  for (int k = lane_id(); k < a.top; k += kWave) {
+    const float z = t.p[k] - ref;
+    const float q = t.ids[k] >= 0 ? exp2_of(z * kLog2e) * inv : 0.f;
+    t.p[k] = q;
     if (q != 0.f) pl += q * (z - log_sum);
   }
-  *plogp = block_sum(pl, red);
-  return live;
-}
-
-template <class T>
-__global__ __launch_bounds__(kBlock) void distill_sums(DistillDev dv, int32_t* __restrict__ status) {
-  __shared__ int ids[kMaxTeacher];
-  __shared__ float p[kMaxTeacher];
-  __shared__ float red[kWavesPerBlock];
-  const embbag_distill_t& a = dv.a;
-  const int r = int(blockIdx.x / dv.slices);
-  const uint32_t sl = blockIdx.x - uint32_t(r) * dv.slices;
-  const int base = int(sl) * kSlice;
-  const int len = min(kSlice, a.vocab - base);
-  const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride + base;
-  int err = 0;
-  float plogp;
-  const bool live = teacher_row(a, r, ids, p, red, &plogp, &err);
-  if (err != 0 && status != nullptr) atomicMin(status, err);
-  if (!live) return;
-  const float c = kLog2e / a.temperature;
-  const float low = -__builtin_inff();
-  float top = low;
-  for (int i = threadIdx.x; i < len; i += kBlock) top = fmaxf(top, to_f32(x[i]));
-  top = block_max(top, red);
-  const float ref = top == low ? 0.f : top;
-  float sum = 0.f;
-  for (int i = threadIdx.x; i < len; i += kBlock)
-    sum += __builtin_exp2f((to_f32(x[i]) - ref) * c);
-  sum = block_sum(sum, red);
-  float cross = 0.f;
-  for (int k = threadIdx.x; k < a.top; k += kBlock) {
-    const int at = ids[k] - base;
-    if (ids[k] >= 0 && uint32_t(at) < uint32_t(len) && p[k] != 0.f) cross += p[k] * to_f32(x[at]);
+  pl = wave_sum(pl);
+  const bool any = __builtin_amdgcn_ballot_w64(some) != 0ull;
+  if (lane_id() == 0) {
+    t.plogp = pl;
+    t.live = any;
   }
-  cross = block_sum(cross, red);
-  if (threadIdx.x == 0) dv.parts[int64_t(r) * dv.slices + sl] = {top, sum, cross};
 }
 
+// Entry k of the row, if its id lies in [base, base + len): whether it is the id's
+// first, and the probabilities of all the id's entries, added in order.
+__device__ __forceinline__ bool first_entry(const Teacher& t, int top, int k, float* p) {
+  const int id = t.ids[k];
+  bool first = true;
+  float s = 0.f;
+  for (int i = 0; i < top; ++i) {
+    if (t.ids[i] != id) continue;
+    first = first && i >= k;
+    s += t.p[i];
+  }
+  *p = s;
+  return first;
+}
+
+// 16 bytes of a row of which n elements exist: the others become -infinity.
 template <class T>
-__global__ __launch_bounds__(kBlock) void distill_grad(DistillDev dv) {
-  __shared__ int ids[kMaxTeacher];
-  __shared__ float p[kMaxTeacher];
-  __shared__ float red[kWavesPerBlock];
+__device__ __forceinline__ u4 load_vec(const T* p, int n) {
+  constexpr int V = kVec<T>;
+  if (n >= V) return load16(p);
+  float v[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = e < n ? to_f32(p[e]) : low();
+  return pack16(v);
+}
+template <class T>
+__device__ __forceinline__ void store_vec(T* p, int n, const float (&v)[kVec<T>]) {
+  constexpr int V = kVec<T>;
+  if (n >= V) {
+    store16(p, pack16(v));
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (e < n) p[e] = T(v[e]);
+}
+
+// Zeros to a row (or slice) of n elements.
+template <class T>
+__device__ __forceinline__ void zero_row(T* g, int n) {
+  constexpr int V = kVec<T>;
+  const float z[V] = {};
+  for (int64_t i = int64_t(threadIdx.x) * V; i < n; i += int64_t(blockDim.x) * V)
+    store_vec(g + i, int(min(int64_t(n) - i, int64_t(V))), z);
+}
+
+// Adds the exponentials of a vector to a running (top, sum).
+template <int V>
+__device__ __forceinline__ void add_online(const float (&v)[V], float c, float* top, float* sum) {
+  float t = *top;
+#pragma unroll
+  for (int e = 0; e < V; ++e) t = fmaxf(t, v[e]);
+  const float ref = t == low() ? 0.f : t;
+  float s = *sum == 0.f ? 0.f : *sum * exp2_of((*top - ref) * c);
+#pragma unroll
+  for (int e = 0; e < V; ++e) s += exp2_of((v[e] - ref) * c);
+  *top = t;
+  *sum = s;
+}
+
+// One block per row; its first NV * THREADS vectors stay in registers.
+template <class T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void distill_row(DistillDev dv, int32_t* __restrict__ status) {
+  constexpr int V = kVec<T>;
+  constexpr int WAVES = THREADS / kWave;
+  constexpr int PER = kMaxTeacher / THREADS;
+  __shared__ Teacher t;
   const embbag_distill_t& a = dv.a;
-  const int r = int(blockIdx.x / dv.slices);
-  const uint32_t sl = blockIdx.x - uint32_t(r) * dv.slices;
-  const int base = int(sl) * kSlice;
-  const int len = min(kSlice, a.vocab - base);
-  const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride + base;
-  T* g = a.grad != nullptr ? static_cast<T*>(a.grad) + int64_t(r) * a.grad_stride + base : nullptr;
-  int err = 0;
-  float plogp;
-  bool live = teacher_row(a, r, ids, p, red, &plogp, &err);
-  float top = -__builtin_inff(), sum = 0.f, cross = 0.f;
+  const int r = int(blockIdx.x);
+  const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride;
+  T* g = a.grad != nullptr ? static_cast<T*>(a.grad) + int64_t(r) * a.grad_stride : nullptr;
+  const float w = a.row_weights != nullptr ? a.row_weights[r] : 1.f;
+  if (w == 0.f) {
+    if (threadIdx.x == 0) a.loss[r] = 0.f;
+    if (g != nullptr) zero_row(g, a.vocab);
+    return;
+  }
   const float c = kLog2e / a.temperature;
-  if (live) {
-    const Part* q = dv.parts + int64_t(r) * dv.slices;
-    for (uint32_t i = 0; i < dv.slices; ++i) top = fmaxf(top, q[i].top);
-    const float ref = top == -__builtin_inff() ? 0.f : top;
-    for (uint32_t i = 0; i < dv.slices; ++i) {
-      const float m = q[i].top == -__builtin_inff() ? 0.f : q[i].top;
-      sum += q[i].sum == 0.f ? 0.f : q[i].sum * __builtin_exp2f((m - ref) * c);
-      cross += q[i].cross;
+  const int tid = threadIdx.x;
+  auto left = [&](int i) { return a.vocab - (i * THREADS + tid) * V; };
+
+  u4 v[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (left(i) > 0) v[i] = load_vec(x + (i * THREADS + tid) * V, left(i));
+  if (wave_id() == 0) teacher_row(a, r, t, status);
+  float top = low();
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (left(i) > 0) {
+      float f[V];
+      unpack16(v[i], f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = fmaxf(top, f[e]);
     }
-    live = !(sum == 0.f);
-    top = ref;
   }
-  const float w = live ? (a.row_weights != nullptr ? a.row_weights[r] : 1.f) : 0.f;
-  const float T1 = a.temperature;
-  if (sl == 0 && threadIdx.x == 0) {
-    const float lse = top / T1 + __builtin_logf(sum);
-    a.loss[r] = live ? w * T1 * T1 * (plogp - cross / T1 + lse) : 0.f;
+  // What the registers do not hold, with its sum at the same time.
+  float rest_top = low(), rest = 0.f;
+  for (int64_t i = (int64_t(NV) * THREADS + tid) * V; i < a.vocab; i += THREADS * V) {
+    float f[V];
+    unpack16(load_vec(x + i, int(min(a.vocab - i, int64_t(V)))), f);
+    add_online<V>(f, c, &rest_top, &rest);
+  }
+  top = wave_max(fmaxf(top, rest_top));
+  if (lane_id() == 0) t.red[0][wave_id()] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) top = fmaxf(top, t.red[0][i]);
+  const float ref = top == low() ? 0.f : top;
+
+  float sum = rest == 0.f ? 0.f : rest * exp2_of(((rest_top == low() ? 0.f : rest_top) - ref) * c);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (left(i) > 0) {
+      float f[V];
+      unpack16(v[i], f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum += exp2_of((f[e] - ref) * c);
+    }
+  }
+  // The entries' logits, before the row is written (g may be x).
+  float cross = 0.f, xk[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int k = j * THREADS + tid;
+    xk[j] = k < a.top && t.ids[k] >= 0 ? to_f32(x[t.ids[k]]) : 0.f;
+    if (k < a.top && t.p[k] != 0.f) cross += t.p[k] * xk[j];
+  }
+  sum = wave_sum(sum);
+  cross = wave_sum(cross);
+  if (lane_id() == 0) t.red[1][wave_id()] = sum, t.red[2][wave_id()] = cross;
+  __syncthreads();
+  sum = cross = 0.f;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) sum += t.red[1][i], cross += t.red[2][i];
+  const bool live = t.live && !(sum == 0.f);
+  if (tid == 0) {
+    const float T1 = a.temperature;
+    a.loss[r] = live ? w * T1 * T1 * (t.plogp - (cross - ref) / T1 + __builtin_logf(sum)) : 0.f;
   }
   if (g == nullptr) return;
   if (!live) {
-    for (int i = threadIdx.x; i < len; i += kBlock) g[i] = T(0.f);
+    zero_row(g, a.vocab);
     return;
   }
-  const float f = w * T1, inv = 1.f / sum;
-  // An entry's logit is read before the slice is written: g may be x.  The first
-  // entry of an id subtracts the probabilities of all its entries, in order.
-  float fix[kMaxTeacher / kBlock];
+  const float f = w * a.temperature, scale = f / sum;
 #pragma unroll
-  for (int j = 0; j < kMaxTeacher / kBlock; ++j) {
-    const int k = j * kBlock + int(threadIdx.x);
-    fix[j] = 0.f;
-    if (k < a.top && ids[k] >= 0 && uint32_t(ids[k] - base) < uint32_t(len)) {
-      bool first = true;
-      float pk = 0.f;
-      for (int i = 0; i < a.top; ++i) {
-        if (ids[i] != ids[k]) continue;
-        first = first && i >= k;
-        pk += p[i];
-      }
-      fix[j] = f * (__builtin_exp2f((to_f32(x[ids[k] - base]) - top) * c) * inv - pk);
-      if (!first) fix[j] = __builtin_nanf("");
+  for (int i = 0; i < NV; ++i) {
+    if (left(i) > 0) {
+      float q[V];
+      unpack16(v[i], q);
+#pragma unroll
+      for (int e = 0; e < V; ++e) q[e] = scale * exp2_of((q[e] - ref) * c);
+      store_vec(g + (i * THREADS + tid) * V, left(i), q);
     }
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < len; i += kBlock)
-    g[i] = T(f * (__builtin_exp2f((to_f32(x[i]) - top) * c) * inv));
+  for (int64_t i = (int64_t(NV) * THREADS + tid) * V; i < a.vocab; i += THREADS * V) {
+    const int n = int(min(a.vocab - i, int64_t(V)));
+    float q[V];
+    unpack16(load_vec(x + i, n), q);
+#pragma unroll
+    for (int e = 0; e < V; ++e) q[e] = scale * exp2_of((q[e] - ref) * c);
+    store_vec(g + i, n, q);
+  }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kMaxTeacher / kBlock; ++j) {
-    const int k = j * kBlock + int(threadIdx.x);
-    if (k < a.top && ids[k] >= 0 && uint32_t(ids[k] - base) < uint32_t(len)) {
-      bool first = true;
-      for (int i = 0; i < k; ++i) first = first && ids[i] != ids[k];
-      if (first) g[ids[k] - base] = T(fix[j]);
-    }
+  for (int j = 0; j < PER; ++j) {
+    const int k = j * THREADS + tid;
+    float p;
+    if (k < a.top && t.ids[k] >= 0 && first_entry(t, a.top, k, &p))
+      g[t.ids[k]] = T(scale * exp2_of((xk[j] - ref) * c) - f * p);
   }
 }
 
-uint32_t slices_of(int32_t vocab) { return uint32_t((int64_t(vocab) + kSlice - 1) / kSlice); }
+// Sums over the block, to every thread.
+__device__ __forceinline__ float block_sum(float v, float* red) {
+  v = wave_sum(v);
+  if (lane_id() == 0) red[wave_id()] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < kWavesPerBlock; ++i) v += red[i];
+  return v;
+}
+
+// Few rows: the parts of a slice.
+template <class T>
+__global__ __launch_bounds__(kBlock) void distill_sums(DistillDev dv, int32_t* __restrict__ status) {
+  constexpr int V = kVec<T>;
+  __shared__ Teacher t;
+  const embbag_distill_t& a = dv.a;
+  const int r = int(blockIdx.x / dv.slices);
+  const uint32_t sl = blockIdx.x - uint32_t(r) * dv.slices;
+  const int64_t base = int64_t(sl) * dv.slice;
+  const int len = int(min(int64_t(dv.slice), a.vocab - base));
+  const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride + base;
+  if (wave_id() == 0) teacher_row(a, r, t, sl == 0 ? status : nullptr);
+  const float c = kLog2e / a.temperature;
+  float top = low(), sum = 0.f;
+  for (int i = threadIdx.x * V; i < len; i += kBlock * V) {
+    float f[V];
+    unpack16(load_vec(x + i, len - i), f);
+    add_online<V>(f, c, &top, &sum);
+  }
+  const float mine = top;
+  top = wave_max(top);
+  if (lane_id() == 0) t.red[0][wave_id()] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWavesPerBlock; ++i) top = fmaxf(top, t.red[0][i]);
+  const float ref = top == low() ? 0.f : top;
+  sum = sum == 0.f ? 0.f : sum * exp2_of(((mine == low() ? 0.f : mine) - ref) * c);
+  float cross = 0.f;
+  for (int k = threadIdx.x; k < a.top; k += kBlock) {
+    const int64_t at = t.ids[k] - base;
+    if (t.ids[k] >= 0 && at >= 0 && at < len && t.p[k] != 0.f) cross += t.p[k] * to_f32(x[at]);
+  }
+  sum = block_sum(sum, t.red[1]);
+  cross = block_sum(cross, t.red[2]);
+  if (threadIdx.x == 0) dv.parts[int64_t(r) * dv.slices + sl] = {top, sum, cross};
+}
+
+// Few rows: joins a row's parts, and the gradient of a slice.
+template <class T>
+__global__ __launch_bounds__(kBlock) void distill_grad(DistillDev dv) {
+  constexpr int V = kVec<T>;
+  __shared__ Teacher t;
+  const embbag_distill_t& a = dv.a;
+  const int r = int(blockIdx.x / dv.slices);
+  const uint32_t sl = blockIdx.x - uint32_t(r) * dv.slices;
+  const int64_t base = int64_t(sl) * dv.slice;
+  const int len = int(min(int64_t(dv.slice), a.vocab - base));
+  const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride + base;
+  T* g = a.grad != nullptr ? static_cast<T*>(a.grad) + int64_t(r) * a.grad_stride + base : nullptr;
+  if (wave_id() == 0) teacher_row(a, r, t, nullptr);
+  const float w = a.row_weights != nullptr ? a.row_weights[r] : 1.f;
+  const float c = kLog2e / a.temperature;
+  const Part* q = dv.parts + int64_t(r) * dv.slices;
+  float top = low(), sum = 0.f, cross = 0.f;
+  for (uint32_t i = 0; i < dv.slices; ++i) top = fmaxf(top, q[i].top);
+  const float ref = top == low() ? 0.f : top;
+  for (uint32_t i = 0; i < dv.slices; ++i) {
+    const float m = q[i].top == low() ? 0.f : q[i].top;
+    sum += q[i].sum == 0.f ? 0.f : q[i].sum * exp2_of((m - ref) * c);
+    cross += q[i].cross;
+  }
+  __syncthreads();
+  const bool live = w != 0.f && t.live && !(sum == 0.f);
+  if (sl == 0 && threadIdx.x == 0) {
+    const float T1 = a.temperature;
+    a.loss[r] = live ? w * T1 * T1 * (t.plogp - (cross - ref) / T1 + __builtin_logf(sum)) : 0.f;
+  }
+  if (g == nullptr) return;
+  if (!live) {
+    zero_row(g, len);
+    return;
+  }
+  const float f = w * a.temperature, scale = f / sum;
+  float xk[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int k = j * kBlock + int(threadIdx.x);
+    const int64_t at = k < a.top ? t.ids[k] - base : -1;
+    xk[j] = k < a.top && t.ids[k] >= 0 && at >= 0 && at < len ? to_f32(x[at]) : 0.f;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x * V; i < len; i += kBlock * V) {
+    float v[V];
+    unpack16(load_vec(x + i, len - i), v);
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = scale * exp2_of((v[e] - ref) * c);
+    store_vec(g + i, len - i, v);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int k = j * kBlock + int(threadIdx.x);
+    if (k >= a.top) break;
+    const int64_t at = t.ids[k] - base;
+    float p;
+    if (t.ids[k] >= 0 && at >= 0 && at < len && first_entry(t, a.top, k, &p))
+      g[at] = T(scale * exp2_of((xk[j] - ref) * c) - f * p);
+  }
+}
+
+// Rows from this number on get a block each.
+constexpr int kWholeRows = 64;
+constexpr int kLeastSlice = 4096;
+
+// Slices of the rows of a call with few of them: about four blocks per compute unit.
+int32_t slice_of(int32_t rows, int32_t vocab) {
+  const int64_t want = (int64_t(kNumCu) * 4 + rows - 1) / (rows > 0 ? rows : 1);
+  int64_t s = (int64_t(vocab) + want - 1) / want;
+  s = (s + 7) / 8 * 8;
+  return int32_t(s < kLeastSlice ? kLeastSlice : s);
+}
+
+template <class T, int NV>
+void launch_row(const DistillDev& dv, int32_t* status, hipStream_t st) {
+  hipLaunchKernelGGL((distill_row<T, kRowThreads, NV>), dim3(uint32_t(dv.a.rows)),
+                     dim3(kRowThreads), 0, st, dv, status);
+}
+
+template <class T>
+void launch_type(const DistillDev& dv, int32_t* status, hipStream_t st) {
+  const embbag_distill_t& a = dv.a;
+  if (a.rows >= kWholeRows) {
+    const int64_t vecs = (int64_t(a.vocab) + kVec<T> - 1) / kVec<T>;
+    if (vecs <= kBlock * 4)
+      hipLaunchKernelGGL((distill_row<T, kBlock, 4>), dim3(uint32_t(a.rows)), dim3(kBlock), 0, st,
+                         dv, status);
+    else if (vecs <= kRowThreads * 4)
+      launch_row<T, 4>(dv, status, st);
+    else if (vecs <= kRowThreads * 8)
+      launch_row<T, 8>(dv, status, st);
+    else
+      launch_row<T, 16>(dv, status, st);
+    return;
+  }
+  const dim3 grid(dv.slices * uint32_t(a.rows));
+  hipLaunchKernelGGL(distill_sums<T>, grid, dim3(kBlock), 0, st, dv, status);
+  hipLaunchKernelGGL(distill_grad<T>, grid, dim3(kBlock), 0, st, dv);
+}
+
+uint32_t slices_of(int32_t vocab, int32_t slice) {
+  return uint32_t((int64_t(vocab) + slice - 1) / slice);
+}
 
 }  // namespace
 
 size_t distill_workspace(int32_t rows, int32_t vocab, int32_t top) {
-  const size_t n = size_t(rows) * slices_of(vocab) * sizeof(Part);
-  return (n + 255) / 256 * 256 + 256;
+  if (rows >= kWholeRows) return 0;
+  const size_t n = size_t(rows) * slices_of(vocab, slice_of(rows, vocab)) * sizeof(Part);
+  return (n + 255) / 256 * 256;
 }
 
 hipError_t launch_distill(const embbag_distill_t& a, char* ws, int32_t* status, hipStream_t st) {
   if (a.rows == 0) return hipSuccess;
   DistillDev dv;
   dv.a = a;
-  dv.slices = slices_of(a.vocab);
+  dv.slice = slice_of(a.rows, a.vocab);
+  dv.slices = slices_of(a.vocab, dv.slice);
   dv.parts = reinterpret_cast<Part*>(ws);
-  const dim3 grid(dv.slices * uint32_t(a.rows));
-  if (a.type == EMBBAG_BF16) {
-    hipLaunchKernelGGL(distill_sums<__bf16>, grid, dim3(kBlock), 0, st, dv, status);
-    hipLaunchKernelGGL(distill_grad<__bf16>, grid, dim3(kBlock), 0, st, dv);
-  } else {
-    hipLaunchKernelGGL(distill_sums<float>, grid, dim3(kBlock), 0, st, dv, status);
-    hipLaunchKernelGGL(distill_grad<float>, grid, dim3(kBlock), 0, st, dv);
-  }
+  if (a.type == EMBBAG_BF16)
+    launch_type<__bf16>(dv, status, st);
+  else
+    launch_type<float>(dv, status, st);
   return hipGetLastError();
 }
 
