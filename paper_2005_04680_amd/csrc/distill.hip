@@ -19,7 +19,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowThreads = 1024;
 constexpr int kPer = kMaxTeacher / kBlock;  // entries per thread of the smallest block
 
-__device__ __forceinline__ float low() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 struct Part {
@@ -107,28 +106,6 @@ __device__ __forceinline__ bool first_entry(const Teacher& t, int top, int k, fl
   }
   *p = s;
   return first;
-}
-
-// 16 bytes of a row of which n elements exist: the others become -infinity.
-template <class T>
-__device__ __forceinline__ u4 load_vec(const T* p, int n) {
-  constexpr int V = kVec<T>;
-  if (n >= V) return load16(p);
-  float v[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = e < n ? to_f32(p[e]) : low();
-  return pack16(v);
-}
-template <class T>
-__device__ __forceinline__ void store_vec(T* p, int n, const float (&v)[kVec<T>]) {
-  constexpr int V = kVec<T>;
-  if (n >= V) {
-    store16(p, pack16(v));
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    if (e < n) p[e] = T(v[e]);
 }
 
 // Zeros to a row (or slice) of n elements.

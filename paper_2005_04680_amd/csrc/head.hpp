@@ -108,10 +108,28 @@ typedef u4 u4_any __attribute__((aligned(2)));
 __device__ __forceinline__ void store16(void* p, const u4& v) { *static_cast<u4_any*>(p) = v; }
 __device__ __forceinline__ u4 load16(const void* p) { return *static_cast<const u4_any*>(p); }
 
-// Elements before the first 16-byte boundary at or after p.
+__device__ __forceinline__ float low() { return -__builtin_inff(); }
+
+// 16 bytes of a row of which n elements exist: the others become -infinity.
 template <class T>
-__device__ __forceinline__ int head_of(const T* p) {
-  return int((16u - (uint32_t(reinterpret_cast<uintptr_t>(p)) & 15u)) & 15u) / int(sizeof(T));
+__device__ __forceinline__ u4 load_vec(const T* p, int n) {
+  constexpr int V = kVec<T>;
+  if (n >= V) return load16(p);
+  float v[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = e < n ? to_f32(p[e]) : low();
+  return pack16(v);
+}
+template <class T>
+__device__ __forceinline__ void store_vec(T* p, int n, const float (&v)[kVec<T>]) {
+  constexpr int V = kVec<T>;
+  if (n >= V) {
+    store16(p, pack16(v));
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (e < n) p[e] = T(v[e]);
 }
 
 // u / d for u < 2^31 as a product and a shift; d >= 1.
