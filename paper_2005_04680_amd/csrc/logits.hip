@@ -2,12 +2,13 @@
 // logits.
 //
 // A block takes one slice of one row.  It walks the row's lists and keeps in LDS,
-// for every token of its slice, a word of occurrences (bit 31: in the prompt; the
+// for every token of its slice, its occurrences (the top bit: in the prompt; the
 // rest: how often after it) and the place of its last bias: integer additions and
 // maxima, whose order does not matter.  The slice itself is on its way meanwhile, 16 bytes per
 // load, and is read and written once.  A block is a chain of a few memory latencies
 // (offsets, lists, stores), so the lists come in batches of 16 entries per thread and
-// several blocks share a compute unit.  Every element is read and written by one thread, so
+// many blocks share a compute unit: a token's two numbers share one word of LDS, 16 bits each.  Rows
+// whose lists are too long for that take their slice in two halves, a word for each.  Every element is read and written by one thread, so
 // that `out` may be `logits`.
 #include "head.hpp"
 
@@ -15,6 +16,7 @@ namespace embbag {
 namespace {
 
 constexpr uint32_t kPrompt = 0x80000000u;
+constexpr uint32_t kPrompt16 = 0x8000u;
 constexpr int kSliceTokens = 4096;
 
 struct LogitsDev {
@@ -32,37 +34,49 @@ __device__ __forceinline__ void list_of(const int32_t* o, int r, int rows, int64
   *to = bad ? 0 : b;
 }
 
-// Calls fn(place in the list, entry) for entries [from, to) of `list`, four loads of four
-// entries in flight per thread.
+// Calls fn(place in the list, entry) for entries [from, to) of `list`, up to four loads of four
+// entries in flight per thread.  Returns the largest entry, unsigned.
 template <class Fn>
-__device__ __forceinline__ void walk(const int32_t* list, int from, int to, Fn fn) {
-  constexpr int U = 4;
+__device__ __forceinline__ uint32_t walk(const int32_t* list, int from, int to, Fn fn) {
+  constexpr uint32_t U = 4, kStep = 4 * kBlock;
   const uint32_t n = uint32_t(to) - uint32_t(from);
+  uint32_t largest = 0u;
   list += from;
-  uint32_t j0 = 0;
-  for (; j0 < n; j0 += U * 4 * kBlock) {
+  for (uint32_t j0 = 0; j0 < n; j0 += U * kStep) {
     u4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t j = j0 + (u * kBlock + threadIdx.x) * 4;
-      v[u] = u4{0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
-      if (j + 4 <= n) {
-        v[u] = load16(list + j);
-      } else if (j < n) {
-        v[u].x = uint32_t(list[j]);
-        if (j + 1 < n) v[u].y = uint32_t(list[j + 1]);
-        if (j + 2 < n) v[u].z = uint32_t(list[j + 2]);
-      }
+    for (uint32_t u = 0; u < U; ++u) {
+      const uint32_t j = j0 + u * kStep + threadIdx.x * 4;
+      if (j0 + u * kStep < n && j + 4 <= n) v[u] = load16(list + j);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t j = j0 + (u * kBlock + threadIdx.x) * 4;
-      if (j < n) fn(j, v[u].x);
-      if (j + 1 < n) fn(j + 1, v[u].y);
-      if (j + 2 < n) fn(j + 2, v[u].z);
-      if (j + 3 < n) fn(j + 3, v[u].w);
+    for (uint32_t u = 0; u < U; ++u) {
+      if (j0 + u * kStep >= n) break;
+      const uint32_t j = j0 + u * kStep + threadIdx.x * 4;
+      if (j + 4 <= n) {
+        largest = max(max(largest, max(v[u].x, v[u].y)), max(v[u].z, v[u].w));
+        fn(j, v[u].x);
+        fn(j + 1, v[u].y);
+        fn(j + 2, v[u].z);
+        fn(j + 3, v[u].w);
+      } else {
+        for (uint32_t i = j; i < n; ++i) {
+          const uint32_t e = uint32_t(list[i]);
+          largest = max(largest, e);
+          fn(i, e);
+        }
+      }
     }
   }
+  return largest;
+}
+
+// l / rho from the reciprocal: the product's remainder, which is exact, corrects it to the
+// division's rounding.  (Overflow and infinities stay what the product gave.)
+__device__ __forceinline__ float divide(float l, float rho, float inv) {
+  const float q = l * inv;
+  const float c = fmaf(fmaf(-q, rho, l), inv, q);
+  return fabsf(q) < __builtin_inff() ? c : q;
 }
 
 template <class T, bool SEEN, bool BIAS>
@@ -70,8 +84,8 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
                                                         int32_t* __restrict__ status) {
   constexpr int V = kVec<T>;
   constexpr int NV = kSliceTokens / (kBlock * V);  // vectors per thread
-  constexpr int LISTS = int(SEEN) + int(BIAS);
-  __shared__ __align__(16) uint32_t lds[LISTS * kSliceTokens + 4];
+  constexpr bool BOTH = SEEN && BIAS, ANY = SEEN || BIAS;
+  __shared__ __align__(16) uint32_t lds[ANY ? kSliceTokens : 4];
   const embbag_logits_t& a = dv.a;
   const int r = int(blockIdx.x / dv.slices);
   const int base = int(blockIdx.x - uint32_t(r) * dv.slices) * kSliceTokens;
@@ -79,8 +93,6 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
   const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride + base;
   T* y = static_cast<T*>(a.out) + int64_t(r) * a.out_stride + base;
   int err = 0;
-  uint32_t* occ = lds;
-  uint32_t* bia = lds + (SEEN ? kSliceTokens : 0);
 
   u4 raw[NV];
 #pragma unroll
@@ -91,38 +103,6 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
   int s0 = 0, s1 = 0, b0 = 0, b1 = 0;
   if constexpr (SEEN) list_of(a.seen_offsets, r, a.rows, a.num_seen, &s0, &s1, &err);
   if constexpr (BIAS) list_of(a.bias_offsets, r, a.rows, a.num_biases, &b0, &b1, &err);
-  if constexpr (LISTS > 0) {
-#pragma unroll
-    for (int i = 0; i < LISTS * kSliceTokens / (kBlock * 4); ++i)
-      *reinterpret_cast<u4*>(lds + (i * kBlock + threadIdx.x) * 4) = u4{0u, 0u, 0u, 0u};
-    __syncthreads();
-  }
-  if constexpr (SEEN) {
-    const int plen = a.prompt_lens != nullptr ? a.prompt_lens[r] : 0;
-    walk(a.seen, s0, s1, [&](uint32_t j, uint32_t v) {
-      if (v >= uint32_t(a.vocab)) {
-        err = min(err, EMBBAG_ERR_INDEX_RANGE);
-        return;
-      }
-      const uint32_t at = v - uint32_t(base);
-      if (at < uint32_t(len)) {
-        if (int64_t(j) < plen)
-          atomicOr(&occ[at], kPrompt);
-        else
-          atomicAdd(&occ[at], 1u);
-      }
-    });
-  }
-  if constexpr (BIAS) {
-    walk(a.bias_ids, b0, b1, [&](uint32_t j, uint32_t v) {
-      if (v >= uint32_t(a.vocab)) {
-        err = min(err, EMBBAG_ERR_INDEX_RANGE);
-        return;
-      }
-      const uint32_t at = v - uint32_t(base);
-      if (at < uint32_t(len)) atomicMax(&bia[at], j + 1u);
-    });
-  }
   const uint32_t* mask = nullptr;
   if (a.masks != nullptr) {
     const int id = a.mask_ids != nullptr ? a.mask_ids[r] : r;
@@ -131,57 +111,102 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
     else if (id >= 0)
       mask = a.masks + int64_t(id) * a.mask_stride;
   }
-  const float rho = SEEN && a.repetition != nullptr ? a.repetition[r] : 1.f;
-  const float freq = SEEN && a.frequency != nullptr ? a.frequency[r] : 0.f;
-  const float pres = SEEN && a.presence != nullptr ? a.presence[r] : 0.f;
-  if constexpr (LISTS > 0) __syncthreads();
-
+  // V tokens from a multiple of V: their bits lie in one word.
+  uint32_t bits[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int v = (i * kBlock + int(threadIdx.x)) * V;
-    if (v >= len) continue;
-    float l[V];
-    unpack16(raw[i], l);
+    bits[i] = 0xFFFFFFFFu;
+    if (mask != nullptr && v < len) bits[i] = mask[(base + v) >> 5] >> ((base + v) & 31);
+  }
+  const int plen = SEEN && a.prompt_lens != nullptr ? a.prompt_lens[r] : 0;
+  const float rho = SEEN && a.repetition != nullptr ? a.repetition[r] : 1.f;
+  const float inv = 1.f / rho;
+  const bool plain = rho > 0x1p-60f && rho < 0x1p60f;
+  const float freq = SEEN && a.frequency != nullptr ? a.frequency[r] : 0.f;
+  const float pres = SEEN && a.presence != nullptr ? a.presence[r] : 0.f;
+
+  // With both lists: one word of two 16-bit numbers, or halves of the slice with two words.
+  const bool narrow = BOTH && uint32_t(s1 - s0) < kPrompt16 && uint32_t(b1 - b0) < 0xFFFFu;
+  const int parts = BOTH && !narrow ? 2 : 1;
+  for (int part = 0; part < parts; ++part) {
+    const int tokens = kSliceTokens / parts, from = base + part * tokens;
+    const uint32_t here = uint32_t(max(0, min(tokens, a.vocab - from)));
+    uint32_t* bia = lds + (BOTH && !narrow ? tokens : 0);
+    if constexpr (ANY) {
+      if (part > 0) __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kSliceTokens / (kBlock * 4); ++i)
+        *reinterpret_cast<u4*>(lds + (i * kBlock + threadIdx.x) * 4) = u4{0u, 0u, 0u, 0u};
+      __syncthreads();
+    }
+    // (A shared word takes its maxima while its low half is 0.)
+    if constexpr (BIAS) {
+      const uint32_t worst = walk(a.bias_ids, b0, b1, [&](uint32_t j, uint32_t v) {
+        const uint32_t at = v - uint32_t(from);
+        if (at < here) atomicMax(&bia[at], narrow ? (j + 1u) << 16 : j + 1u);
+      });
+      if (worst >= uint32_t(a.vocab)) err = min(err, EMBBAG_ERR_INDEX_RANGE);
+      if constexpr (SEEN) __syncthreads();
+    }
     if constexpr (SEEN) {
-      uint32_t o[V], any = 0u;
+      const uint32_t prompt = narrow ? kPrompt16 : kPrompt;
+      const uint32_t worst = walk(a.seen, s0, s1, [&](uint32_t j, uint32_t v) {
+        const uint32_t at = v - uint32_t(from);
+        if (at < here) {
+          if (int64_t(j) < plen)
+            atomicOr(&lds[at], prompt);
+          else
+            atomicAdd(&lds[at], 1u);
+        }
+      });
+      if (worst >= uint32_t(a.vocab)) err = min(err, EMBBAG_ERR_INDEX_RANGE);
+    }
+    if constexpr (ANY) __syncthreads();
+
 #pragma unroll
-      for (int e = 0; e < V; e += 4) {
-        const u4 w = *reinterpret_cast<const u4*>(occ + v + e);
-        o[e] = w.x, o[e + 1] = w.y, o[e + 2] = w.z, o[e + 3] = w.w;
-        any |= w.x | w.y | w.z | w.w;
-      }
-      if (any != 0u) {
+    for (int i = 0; i < NV; ++i) {
+      if (parts == 2 && i / (NV / 2) != part) continue;
+      const int v = (i * kBlock + int(threadIdx.x)) * V;
+      if (v >= len) continue;
+      float l[V];
+      unpack16(raw[i], l);
+      if constexpr (ANY) {
+        uint32_t o[V], b[V], any = 0u;
+        const uint32_t* at = lds + (v - part * tokens);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          if (o[e] == 0u) continue;
-          l[e] = l[e] > 0.f ? l[e] / rho : l[e] * rho;
-          const uint32_t c = o[e] & ~kPrompt;
-          if (c != 0u) l[e] -= freq * float(c) + pres;
+        for (int e = 0; e < V; e += 4) {
+          const u4 w = *reinterpret_cast<const u4*>(at + e);
+          o[e] = w.x, o[e + 1] = w.y, o[e + 2] = w.z, o[e + 3] = w.w;
+          any |= w.x | w.y | w.z | w.w;
+        }
+        if (BOTH && !narrow) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) b[e] = at[tokens + e], any |= b[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            b[e] = BOTH ? o[e] >> 16 : o[e];
+            if (BOTH) o[e] = (o[e] & kPrompt16) << 16 | (o[e] & (kPrompt16 - 1u));
+          }
+        }
+        if (any != 0u) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            if (SEEN && o[e] != 0u) {
+              l[e] = l[e] > 0.f ? (plain ? divide(l[e], rho, inv) : l[e] / rho) : l[e] * rho;
+              const uint32_t c = o[e] & ~kPrompt;
+              l[e] -= c != 0u ? freq * float(c) + pres : 0.f;
+            }
+            if (BIAS && b[e] != 0u) l[e] += a.biases[int64_t(b0) + b[e] - 1];
+          }
         }
       }
-    }
-    if constexpr (BIAS) {
-      uint32_t o[V], any = 0u;
-#pragma unroll
-      for (int e = 0; e < V; e += 4) {
-        const u4 w = *reinterpret_cast<const u4*>(bia + v + e);
-        o[e] = w.x, o[e + 1] = w.y, o[e + 2] = w.z, o[e + 3] = w.w;
-        any |= w.x | w.y | w.z | w.w;
-      }
-      if (any != 0u) {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (o[e] != 0u) l[e] += a.biases[int64_t(b0) + o[e] - 1];
-      }
-    }
-    if (mask != nullptr) {
-      // V tokens from a multiple of V: their bits lie in one word.
-      const uint32_t bits = mask[(base + v) >> 5] >> ((base + v) & 31);
 #pragma unroll
       for (int e = 0; e < V; ++e)
-        if (((bits >> e) & 1u) == 0u) l[e] = low();
+        if (((bits[i] >> e) & 1u) == 0u) l[e] = low();
+      store_vec(y + v, len - v, l);
     }
-    store_vec(y + v, len - v, l);
   }
   if (err != 0 && status != nullptr) atomicMin(status, err);
 }

@@ -253,6 +253,31 @@ __global__ __launch_bounds__(kBlock) void grad_join(const float* __restrict__ pa
   store4(dx + int64_t(row) * ldx + (uint32_t(i) - row * k4.div) * 4, s);
 }
 
+// The same where there are many parts of few elements: a wavefront adds every WAVES-th part,
+// then the first adds the wavefronts' sums in order.
+template <class TX>
+__global__ __launch_bounds__(1024) void grad_join_many(const float* __restrict__ parts,
+                                                       int32_t splits, int32_t m, FastDiv k4,
+                                                       TX* __restrict__ dx, int64_t ldx) {
+  constexpr int WAVES = 16;
+  __shared__ f4 sums[WAVES][kWave];
+  const int64_t n = int64_t(m) * k4.div;
+  const int64_t i = int64_t(blockIdx.x) * kWave + lane_id();
+  const int wave = wave_id();
+  f4 s = {0.f, 0.f, 0.f, 0.f};
+  if (i < n) {
+#pragma unroll 4
+    for (int z = wave; z < splits; z += WAVES) s += load4(parts + (z * n + i) * 4);
+  }
+  sums[wave][lane_id()] = s;
+  __syncthreads();
+  if (wave != 0 || i >= n) return;
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) s += sums[w][lane_id()];
+  const uint32_t row = quotient(uint32_t(i), k4);
+  store4(dx + int64_t(row) * ldx + (uint32_t(i) - row * k4.div) * 4, s);
+}
+
 // Tile and split of a gradient.
 struct GradPlan {
   int bk, bm;
@@ -263,7 +288,7 @@ GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
   GradPlan p = {};
   if (m == 0) return p;
   p.bk = k > 128 ? 256 : 128;
-  p.bm = m > 64 ? 256 : (m > 32 ? 64 : 32);
+  p.bm = m > 32 ? (m > 64 && double(m) * double(n) * k > 5e10 ? 256 : 64) : 32;
   p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
   p.mtiles = uint32_t((m + p.bm - 1) / p.bm);
   const int64_t steps = (n + kRows - 1) / kRows;
@@ -327,6 +352,11 @@ void launch_grad(const GradPlan& p, const void* dy, bool dy_bf16, int64_t ldy, i
   else
     launch_plan<float>(p, dy, ldy, m, w, parts, w.dim, ps, st);
   const int64_t n = ps / 4;
+  if (p.splits > 8) {
+    hipLaunchKernelGGL(grad_join_many<TX>, dim3(unsigned((n + kWave - 1) / kWave)), dim3(1024), 0, st,
+                       parts, int32_t(p.splits), m, fast_div(uint32_t(w.dim / 4)), dx, ldx);
+    return;
+  }
   hipLaunchKernelGGL(grad_join<TX>, dim3(unsigned((n + kBlock - 1) / kBlock)), dim3(kBlock), 0, st,
                      parts, int32_t(p.splits), m, fast_div(uint32_t(w.dim / 4)), dx, ldx);
 }

@@ -6,6 +6,7 @@ namespace {
 
 typedef int i8v __attribute__((ext_vector_type(8)));
 typedef float f16v __attribute__((ext_vector_type(16)));
+typedef u4 u4_word __attribute__((aligned(4)));
 
 // A fragment of 32 codes as the products take it.
 __device__ __forceinline__ i8v frag8(const u4& v) {
@@ -23,9 +24,23 @@ __global__ __launch_bounds__(kBlock) void pack_x(const T* __restrict__ x, int64_
                                                  const uint32_t* __restrict__ ws, int64_t n,
                                                  uint32_t* __restrict__ ws_out) {
   if (blockIdx.x >= xblocks) {
-    const int64_t row = int64_t(blockIdx.x - xblocks) * kBlock + threadIdx.x;
+    // 64 rows, a quarter of the groups for each wavefront, 4 groups at a time.
+    const int64_t row = int64_t(blockIdx.x - xblocks) * kWave + lane_id();
     if (row >= n) return;
-    for (int g = 0; g < groups; ++g) ws_out[g * n + row] = ws[row * groups + g];
+    const uint32_t* src = ws + row * groups;
+    for (int g = wave_id() * 4; g < groups; g += kWavesPerBlock * 4) {
+      uint32_t v[4];
+      if (groups % 4 == 0) {
+        const u4 q = *reinterpret_cast<const u4_word*>(src + g);
+        v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = g + i < groups ? src[g + i] : 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (g + i < groups) ws_out[(g + i) * n + row] = v[i];
+    }
     return;
   }
   const int64_t u = int64_t(blockIdx.x) * (kBlock / 4) + threadIdx.x / 4;
@@ -364,7 +379,7 @@ hipError_t launch_mx4_matmul(const void* x, bool x_bf16, int64_t x_stride, int32
   const uint32_t* wsc = reinterpret_cast<const uint32_t*>(w.scales);
   const int64_t units = int64_t(m) * groups2 * 4;
   const uint32_t xblocks = uint32_t((units + kBlock / 4 - 1) / (kBlock / 4));
-  const uint32_t wblocks = m > 16 ? uint32_t((w.rows + kBlock - 1) / kBlock) : 0u;
+  const uint32_t wblocks = m > 16 ? uint32_t((w.rows + kWave - 1) / kWave) : 0u;
   const dim3 pgrid(xblocks + wblocks);
   const FastDiv f = fast_div(uint32_t(groups2));
   if (x_bf16)

@@ -121,6 +121,25 @@ def test_parts_left_out():
     check(x, dict(masks=dev(m.view(np.int32))), dict(masks=m), "f32")
 
 
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("seen,biases", [(32767, 40), (32768, 40), (40, 65534), (40, 65535), (70000, 70000)])
+def test_long_lists(seen, biases, type_):
+    """Lists around the lengths that 16-bit numbers hold, one token most of the time."""
+    x, kw, want = case(2, 9000, 0, 0, 2, type_, 13)
+    rng = np.random.default_rng(seen + biases)
+    s = np.where(rng.random(seen) < 0.9, 4100, rng.integers(0, 9000, size=seen)).astype(np.int32)
+    ids = rng.choice([7, 4100, 8999, 2050], size=biases).astype(np.int32)
+    b = rng.normal(size=biases).astype(np.float32)
+    s[-1] = ids[-1] = 2049
+    f = np.array([1e-4, 1e-3], np.float32)
+    kw.update(seen=dev(s), seen_offsets=dev(np.array([0, 0, seen], np.int32)),
+              prompt_lens=dev(np.array([0, 5], np.int32)), frequency=dev(f), bias_ids=dev(ids),
+              bias_offsets=dev(np.array([0, 0, biases], np.int32)), biases=dev(b))
+    want.update(seen=[[], s.tolist()], prompt_lens=[0, 5], frequency=f,
+                bias=[[], list(zip(ids.tolist(), b.tolist()))])
+    check(x, kw, want, type_)
+
+
 def test_a_mask_wins_over_everything():
     x = torch.tensor([[float("nan"), float("inf"), 1.0, -1.0]], device=DEV)
     y = torch.empty_like(x)
