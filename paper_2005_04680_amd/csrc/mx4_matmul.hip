@@ -16,6 +16,7 @@ __device__ __forceinline__ i8v frag8(const u4& v) {
 constexpr int kGroup = 128;      // elements of a step: 4 blocks, whose scales are one word
 constexpr int kGroupBytes = 64;  // their codes
 constexpr int kPad = 256;        // rows of scales are padded to the largest tile
+constexpr size_t kLdsPerCu = 160 * 1024;
 
 // x rounded to the storage of the table: codes [m][groups * 64] (zeros past k), scales as words of
 // 4 blocks [groups][xpitch].  Four lanes per block, as mx4_quantize.  Blocks from `xblocks` on
@@ -91,8 +92,14 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
-// Tiles in the order of the grid: strips of 8 m tiles, in a strip n tile after n tile.  An XCD's
-// 32 blocks then hold 8 tiles of x and 4 of W at a time.
+// Tiles of 32 rows of W that a wavefront turns around at once: 128 bytes of a row of the output.
+template <class T>
+constexpr int turn_tiles(int tn) {
+  return tn < 4 / int(sizeof(T)) ? tn : 4 / int(sizeof(T));
+}
+
+// Tile number id: strips of 8 m tiles, in a strip n tile after n tile.  An XCD's 32 blocks then
+// hold 8 tiles of x and 4 of W at a time.
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t mtiles, uint32_t ntiles, uint32_t* mt,
                                         uint32_t* nt) {
   constexpr uint32_t kStrip = 8;
@@ -112,6 +119,9 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t mtiles, uint32_t n
 // reads (16 rows, one block) cover all banks.  Lane l's row is l % 32; product j of a step
 // takes block 2 (l / 32) + j, whose scale is byte j of the row's word, shifted by l / 32
 // halves.
+//
+// A block takes tile after tile (every XCD its own range of them), and the loads run through the
+// steps of all of them: those of the next tile are on their way while a tile is stored.
 template <int TN, int TM, int WN, int WM, int STAGES, class T>
 __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     const uint8_t* __restrict__ xc, const uint32_t* __restrict__ xs, int64_t xpitch, int32_t m,
@@ -124,44 +134,71 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   constexpr int WLOADS = BN / 16 / W, WSLOADS = BN / 64 / W;  // of W's rows, which come first
   constexpr int CODES = (BN + BM) * kGroupBytes;
   constexpr int STAGE = CODES + (BN + BM) * 4;
+  constexpr int V = kVec<T>;
+  constexpr int TILES = turn_tiles<T>(TN), PITCH = 32 * TILES + V;
+  constexpr int PER_ROW = 32 * TILES / V, ROWS = kWave / PER_ROW, STORES = 32 / ROWS;
   extern __shared__ __align__(16) uint8_t lds[];
 
   const int lane = lane_id(), wave = wave_id();
-  uint32_t mt, nt;
-  tile_of(xcd_remap(blockIdx.x, gridDim.x), mtiles, ntiles, &mt, &nt);
-  const int64_t n0 = int64_t(nt) * BN;
-  const int m0 = int(mt) * BM;
+  T* turn = reinterpret_cast<T*>(lds + STAGES * STAGE) + wave * 32 * PITCH;
   const int nb = mx4_blocks(w.dim);
   const int64_t xrow = int64_t(steps) * kGroupBytes, wrow = int64_t(nb) * 16;
+  // This block's tiles: from `tile` on every `stride`-th below `end`.
+  const uint32_t tiles = mtiles * ntiles, range = (tiles + kNumXcd - 1) / kNumXcd;
+  const uint32_t stride = gridDim.x / kNumXcd;
+  const uint32_t end = min((blockIdx.x % kNumXcd + 1) * range, tiles);
+  uint32_t tile = blockIdx.x % kNumXcd * range + blockIdx.x / kNumXcd;
+  if (tile >= end) return;
 
-  // Loads: number i of this wavefront brings rows 16 * (i * W + wave) .. + 15 of the stage (W's
-  // rows, then x's); rows past the end repeat the last one.
+  // The loads' own place in the stream of steps: number i of this wavefront brings rows
+  // 16 * (i * W + wave) .. + 15 of the stage (W's rows, then x's); rows past the end repeat
+  // the last one.
   const int c = (lane % 4) ^ (lane / 16);
-  const uint8_t* wbase = w.codes + n0 * wrow;
-  const uint8_t* xbase = xc + int64_t(m0) * xrow;
+  uint32_t ltile = tile;
+  int lstep = 0;
+  const uint8_t *wbase, *xbase;
+  const uint32_t *wsbase, *xsbase;
   uint32_t off[LOADS];
+  auto load_tile = [&]() {
+    uint32_t mt, nt;
+    tile_of(ltile, mtiles, ntiles, &mt, &nt);
+    const int64_t n0 = int64_t(nt) * BN;
+    const int m0 = int(mt) * BM;
+    wbase = w.codes + n0 * wrow;
+    xbase = xc + int64_t(m0) * xrow;
+    wsbase = ws + n0 + lane;
+    xsbase = xs + m0 + lane;
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int r = 16 * (i * W + wave) + lane / 4;
-    off[i] = i < WLOADS ? uint32_t(min(int64_t(r), w.rows - 1 - n0) * wrow)
-                    : uint32_t(min(r - BN, m - 1 - m0) * xrow + c * 16);
-  }
-  const uint32_t* wsbase = ws + n0 + lane;
-  const uint32_t* xsbase = xs + m0 + lane;
-  // Load number i of a step (the codes', then the scales').  Steps past the last one bring it again, so
-  // that the number of loads on their way is always the same.
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = 16 * (i * W + wave) + lane / 4;
+      off[i] = i < WLOADS ? uint32_t(min(int64_t(r), w.rows - 1 - n0) * wrow)
+                          : uint32_t(min(r - BN, m - 1 - m0) * xrow + c * 16);
+    }
+  };
+  // Before a step's loads.  After the last tile its steps are loaded again, so that the number
+  // of loads on their way is always the same.
+  auto next_load = [&]() {
+    if (lstep == steps) {
+      lstep = 0;
+      if (ltile + stride < end) {
+        ltile += stride;
+        load_tile();
+      }
+    }
+  };
+  load_tile();
+  // Load number i of a step (the codes', then the scales').
   constexpr int PER = LOADS + SLOADS;
-  auto load = [&](int step, uint8_t* dst, int i) {
-    step = min(step, steps - 1);
+  auto load = [&](uint8_t* dst, int i) {
     if (i < LOADS) {
       const int r0 = 16 * (i * W + wave);
       // (A block past W's row is its last one: x's codes are 0 there, and W's scale.)
-      const uint32_t wk = uint32_t(min(step * 4 + c, nb - 1)) * 16;
-      const uint32_t xk = uint32_t(step) * kGroupBytes;
+      const uint32_t wk = uint32_t(min(lstep * 4 + c, nb - 1)) * 16;
+      const uint32_t xk = uint32_t(lstep) * kGroupBytes;
       to_lds16(i < WLOADS ? wbase + (off[i] + wk) : xbase + (off[i] + xk), dst + r0 * kGroupBytes);
     } else {
       const int r0 = 64 * ((i - LOADS) * W + wave);
-      to_lds4(i - LOADS < WSLOADS ? wsbase + step * wpitch + r0 : xsbase + step * xpitch + (r0 - BN),
+      to_lds4(i - LOADS < WSLOADS ? wsbase + lstep * wpitch + r0 : xsbase + lstep * xpitch + (r0 - BN),
               dst + CODES + r0 * 4);
     }
   };
@@ -169,11 +206,6 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   const int wn = wave % WN, wm = wave / WN;
   const int half = lane / 32, row = lane % 32;
   f16v acc[TN][TM];
-#pragma unroll
-  for (int i = 0; i < TN; ++i)
-#pragma unroll
-    for (int j = 0; j < TM; ++j) acc[i][j] = f16v{};
-
   const int frag_w = (wn * TN * 32 + row) * kGroupBytes;
   const int frag_x = (BN + wm * TM * 32 + row) * kGroupBytes;
   const int scale_w = CODES + (wn * TN * 32 + row) * 4;
@@ -204,7 +236,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
       __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag8(a[J][I]), frag8(b[J][j]), acc[I][j], \
                                                       4, 4, J, int(cw[I]), J, int(cx[j]));   \
   __builtin_amdgcn_sched_barrier(0);
-  auto step_of = [&](const uint8_t* __restrict__ cur, uint8_t* __restrict__ nxt, int step) {
+  auto step_of = [&](const uint8_t* __restrict__ cur, uint8_t* __restrict__ nxt) {
     constexpr int N = TN + TM;  // fragments of a part, read before its last row's products
     constexpr int READS = TN > 1 ? TN - 1 : 1;
 #pragma unroll
@@ -215,7 +247,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
         if (r * READS / N == i) fetch(cur, 0, r), fetch_scale(cur, r);
 #pragma unroll
       for (int l = 0; l < PER; ++l)
-        if (l * 2 * TN / PER == i) load(step + STAGES - 1, nxt, l);
+        if (l * 2 * TN / PER == i) load(nxt, l);
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -230,22 +262,32 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
         if (r * READS / N == i) fetch(cur, 1, r);
 #pragma unroll
       for (int l = 0; l < PER; ++l)
-        if (l * 2 * TN / PER == TN + i) load(step + STAGES - 1, nxt, l);
+        if (l * 2 * TN / PER == TN + i) load(nxt, l);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 #pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i)
+  for (int i = 0; i < STAGES - 1; ++i) {
+    next_load();
 #pragma unroll
-    for (int l = 0; l < PER; ++l) load(i, lds + i * STAGE, l);
+    for (int l = 0; l < PER; ++l) load(lds + i * STAGE, l);
+    ++lstep;
+  }
   int cur = 0;
+  for (;; tile += stride) {
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f16v{};
   for (int step = 0; step < steps; ++step) {
+    next_load();
     // This step's codes are in LDS (those of the next STAGES - 2 may be on their way), and every
     // wavefront holds the last fragments of the stage before, which the next load overwrites.
     wait_loads<(STAGES - 2) * PER>();
     __builtin_amdgcn_s_barrier();
     const int free = cur == 0 ? STAGES - 1 : cur - 1;
-    step_of(lds + cur * STAGE, lds + free * STAGE, step);
+    step_of(lds + cur * STAGE, lds + free * STAGE);
+    ++lstep;
     cur = cur == STAGES - 1 ? 0 : cur + 1;
   }
 #pragma unroll
@@ -254,46 +296,54 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   }
 #undef EMB_ROW
 
-  // Each wavefront turns 32 rows of x at a time around in its own part of LDS (lane: row of x lane
-  // % 32, four consecutive rows of W per quarter of its registers), then stores whole rows.
-  constexpr int COLS = 32 * TN;
-  constexpr int V = kVec<T>;
-  constexpr int PITCH = COLS + V;
-  constexpr int PER_ROW = COLS / V, ROWS = kWave / PER_ROW, STORES = 32 / ROWS;
-  wait_loads<0>();
-  __builtin_amdgcn_s_barrier();
-  T* turn = reinterpret_cast<T*>(lds) + wave * 32 * PITCH;
-  const int64_t n1 = n0 + wn * COLS;
+  // (The next tile's first products take no fragments.)
+#pragma unroll
+  for (int i = 0; i < TN; ++i) a[1][i] = u4{0u, 0u, 0u, 0u};
+
+  // Each wavefront turns 32 rows of x and COLS of W at a time around in its own part of LDS (lane: row
+  // of x lane % 32, four consecutive rows of W per quarter of its registers), then stores rows of
+  // 128 bytes.
+  uint32_t mt, nt;
+  tile_of(tile, mtiles, ntiles, &mt, &nt);
+  const int64_t n1 = int64_t(nt) * BN + wn * TN * 32;
+  const int m1 = int(mt) * BM + wm * TM * 32;
   const int col = lane % PER_ROW * V;
-  const bool whole = n0 + BN <= w.rows && m0 + BM <= m;
+  const bool whole = int64_t(nt) * BN + BN <= w.rows && int(mt) * BM + BM <= m;
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
-    const int mw = m0 + (wm * TM + j) * 32;
 #pragma unroll
-    for (int i = 0; i < TN; ++i)
+    for (int h = 0; h < TN; h += TILES) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        store4(turn + row * PITCH + i * 32 + q * 8 + half * 4,
-               f4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2],
-                  acc[i][j][q * 4 + 3]});
-    T* p = out + int64_t(mw + lane / PER_ROW) * ldo + n1 + col;
-    const T* q = turn + lane / PER_ROW * PITCH + col;
-    if (whole) {
-      u4 v[STORES];
+      for (int i = 0; i < TILES; ++i)
 #pragma unroll
-      for (int r = 0; r < STORES; ++r) v[r] = *reinterpret_cast<const u4*>(q + r * ROWS * PITCH);
+        for (int q = 0; q < 4; ++q)
+          store4(turn + row * PITCH + i * 32 + q * 8 + half * 4,
+                 f4{acc[h + i][j][q * 4], acc[h + i][j][q * 4 + 1], acc[h + i][j][q * 4 + 2],
+                    acc[h + i][j][q * 4 + 3]});
+      const int64_t n2 = n1 + h * 32 + col;
+      const int m2 = m1 + j * 32 + lane / PER_ROW;
+      T* p = out + int64_t(m2) * ldo + n2;
+      const T* q = turn + lane / PER_ROW * PITCH + col;
+      if (whole) {
+        u4 v[STORES];
 #pragma unroll
-      for (int r = 0; r < STORES; ++r) store16(p + int64_t(r * ROWS) * ldo, v[r]);
-    } else {
+        for (int r = 0; r < STORES; ++r) v[r] = *reinterpret_cast<const u4*>(q + r * ROWS * PITCH);
+#pragma unroll
+        for (int r = 0; r < STORES; ++r) store16(p + int64_t(r * ROWS) * ldo, v[r]);
+      } else {
 #pragma unroll 1
-      for (int r = 0; r < STORES; ++r) {
-        if (mw + r * ROWS + lane / PER_ROW >= m) break;
+        for (int r = 0; r < STORES && m2 + r * ROWS < m; ++r) {
 #pragma unroll 1
-        for (int e = 0; e < V; ++e)
-          if (n1 + col + e < w.rows) p[int64_t(r * ROWS) * ldo + e] = q[r * ROWS * PITCH + e];
+          for (int e = 0; e < V && n2 + e < w.rows; ++e)
+            p[int64_t(r * ROWS) * ldo + e] = q[r * ROWS * PITCH + e];
+        }
       }
     }
   }
+  if (tile + stride >= end) break;
+  }
+  // No load to LDS outlives the block.
+  wait_loads<0>();
 }
 
 // One wavefront per 16 rows of W and 16 of x, straight from memory: lane l holds
@@ -373,29 +423,34 @@ ScoreLayout score_layout(int32_t m, int64_t n, int32_t k) {
   return L;
 }
 
-template <int TN, int TM, int WN, int WM, int STAGES, class T>
+template <int TN, int TM, int WN, int WM, int STAGES, int RESIDENT, class T>
 void launch_tile(const uint8_t* xc, const uint32_t* xs, int32_t m, int32_t groups,
                  const Mx4View& w, const uint32_t* ws, T* out, int64_t ldo, hipStream_t st) {
   constexpr int BN = 32 * TN * WN, BM = 32 * TM * WM;
   static_assert(kPad % BN == 0 && kPad % BM == 0, "padded scales");
   constexpr size_t stage = size_t(BN + BM) * (kGroupBytes + 4);
-  constexpr size_t turn = size_t(WN) * WM * 32 * (32 * TN + kVec<T>)*sizeof(T);
-  constexpr size_t lds = STAGES * stage > turn ? STAGES * stage : turn;
+  constexpr size_t turn = size_t(WN) * WM * 32 * (32 * turn_tiles<T>(TN) + kVec<T>)*sizeof(T);
+  constexpr size_t lds = STAGES * stage + turn;
+  static_assert(lds <= kLdsPerCu / RESIDENT, "blocks that share a compute unit");
   const uint32_t mtiles = uint32_t((m + BM - 1) / BM);
   const uint32_t ntiles = uint32_t((w.rows + BN - 1) / BN);
   auto kernel = scores_tile<TN, TM, WN, WM, STAGES, T>;
   if (lds > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                               hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
-  hipLaunchKernelGGL(kernel, dim3(mtiles * ntiles), dim3(WN * WM * kWave), lds, st, xc, xs,
-                     padded(m), m, groups, w, ws, padded(w.rows), mtiles, ntiles, out, ldo);
+  // As many blocks as fit the chip at once, or as there are tiles.
+  const uint32_t range = (mtiles * ntiles + kNumXcd - 1) / kNumXcd;
+  const uint32_t per_xcd = kNumCu / kNumXcd * RESIDENT;
+  const dim3 grid(kNumXcd * (range < per_xcd ? range : per_xcd));
+  hipLaunchKernelGGL(kernel, grid, dim3(WN * WM * kWave), lds, st, xc, xs, padded(m), m, groups, w,
+                     ws, padded(w.rows), mtiles, ntiles, out, ldo);
 }
 
 template <class T>
 void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, int32_t m,
                    int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
   if (m > 16) {
-    launch_tile<4, 4, 2, 2, 4>(xc, xs, m, groups, w, ws, out, ldo, st);
+    launch_tile<4, 4, 2, 2, 4, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
     return;
   }
   const uint32_t ntiles = uint32_t((w.rows + 63) / 64);
