@@ -129,9 +129,10 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     uint32_t ntiles, T* __restrict__ out, int64_t ldo) {
   constexpr int BN = 32 * TN * WN, BM = 32 * TM * WM, W = WN * WM;
   constexpr int LOADS = (BN + BM) / 16 / W;   // codes, per wavefront and step
-  constexpr int SLOADS = (BN + BM) / 64 / W;  // scales
-  static_assert(BN % (64 * W) == 0 && BM % (64 * W) == 0, "whole loads of either side");
-  constexpr int WLOADS = BN / 16 / W, WSLOADS = BN / 64 / W;  // of W's rows, which come first
+  constexpr int SALL = (BN + BM) / 64;        // of scales, in the block
+  constexpr int SLOADS = (SALL + W - 1) / W;  // per wavefront (the last ones may come twice)
+  static_assert(BN % (16 * W) == 0 && BM % (16 * W) == 0 && BN % 64 == 0, "whole loads");
+  constexpr int WLOADS = BN / 16 / W;         // codes of W's rows, which come first
   constexpr int CODES = (BN + BM) * kGroupBytes;
   constexpr int STAGE = CODES + (BN + BM) * 4;
   constexpr int V = kVec<T>;
@@ -157,8 +158,14 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   uint32_t ltile = tile;
   int lstep = 0;
   const uint8_t *wbase, *xbase;
-  const uint32_t *wsbase, *xsbase;
+  const uint32_t* sbase[SLOADS];  // scales' loads, each at its place in the tile's rows
   uint32_t off[LOADS];
+  // Whether a load of scales is of W's rows: known from its number where sides are whole rounds of the
+  // wavefronts.
+  auto of_w = [&](int i) {
+    if constexpr (BN % (64 * W) == 0 && BM % (64 * W) == 0) return i < BN / 64 / W;
+    return (i * W + wave) % SALL < BN / 64;
+  };
   auto load_tile = [&]() {
     uint32_t mt, nt;
     tile_of(ltile, mtiles, ntiles, &mt, &nt);
@@ -166,8 +173,11 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     const int m0 = int(mt) * BM;
     wbase = w.codes + n0 * wrow;
     xbase = xc + int64_t(m0) * xrow;
-    wsbase = ws + n0 + lane;
-    xsbase = xs + m0 + lane;
+#pragma unroll
+    for (int i = 0; i < SLOADS; ++i) {
+      const int r0 = 64 * ((i * W + wave) % SALL);
+      sbase[i] = of_w(i) ? ws + n0 + r0 + lane : xs + m0 + (r0 - BN) + lane;
+    }
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int r = 16 * (i * W + wave) + lane / 4;
@@ -197,9 +207,8 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
       const uint32_t xk = uint32_t(lstep) * kGroupBytes;
       to_lds16(i < WLOADS ? wbase + (off[i] + wk) : xbase + (off[i] + xk), dst + r0 * kGroupBytes);
     } else {
-      const int r0 = 64 * ((i - LOADS) * W + wave);
-      to_lds4(i - LOADS < WSLOADS ? wsbase + lstep * wpitch + r0 : xsbase + lstep * xpitch + (r0 - BN),
-              dst + CODES + r0 * 4);
+      const int r0 = 64 * (((i - LOADS) * W + wave) % SALL);
+      to_lds4(sbase[i - LOADS] + lstep * (of_w(i - LOADS) ? wpitch : xpitch), dst + CODES + r0 * 4);
     }
   };
 
@@ -308,7 +317,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   const int64_t n1 = int64_t(nt) * BN + wn * TN * 32;
   const int m1 = int(mt) * BM + wm * TM * 32;
   const int col = lane % PER_ROW * V;
-  const bool whole = int64_t(nt) * BN + BN <= w.rows && int(mt) * BM + BM <= m;
+  const bool whole = int64_t(nt) * BN + BN <= w.rows;  // whole rows of the tile
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
 #pragma unroll
@@ -329,7 +338,8 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
 #pragma unroll
         for (int r = 0; r < STORES; ++r) v[r] = *reinterpret_cast<const u4*>(q + r * ROWS * PITCH);
 #pragma unroll
-        for (int r = 0; r < STORES; ++r) store16(p + int64_t(r * ROWS) * ldo, v[r]);
+        for (int r = 0; r < STORES; ++r)
+          if (m2 + r * ROWS < m) store16(p + int64_t(r * ROWS) * ldo, v[r]);
       } else {
 #pragma unroll 1
         for (int r = 0; r < STORES && m2 + r * ROWS < m; ++r) {
@@ -450,7 +460,28 @@ template <class T>
 void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, int32_t m,
                    int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
   if (m > 16) {
-    launch_tile<4, 4, 2, 2, 4, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
+    auto tiles = [&](int64_t bn, int64_t bm) {
+      return (w.rows + bn - 1) / bn * ((m + bm - 1) / bm);
+    };
+    auto rounds = [](int64_t t, int64_t resident) { return (t + resident - 1) / resident; };
+    // The largest tiles where the chip takes four rounds of them or more and those cost less than the
+    // rounds of the next size (a round of 256 of 256 x 256 about 10/7 of one of 512 of
+    // 128 x 128); smaller ones while they leave compute units idle.  Measured, us, 256 x 256 /
+    // 128 x 128 / 128 x 64 / 64 x 64: 4096 x 65536 x 4096 652 / 847 / 1653 / 1760; 1000 x 131072 x
+    // 4096 339 / 449 / 886 / 858; 4096 x 65536 x 256 153 / 180 / 282 / 319; 2000 x 20000 x 1024 57 /
+    // 49 / 70 / 73; 1024 x 8192 x 1024 19 / 16 / 18 / 20; 200 x 200003 x 256 42 / 31 / 38 / 41;
+    // 64 x 200003 x 1024 55 / 34 / 31 / 36; 512 x 4096 x 4096 31 / 17 / 23 / 20; 300 x 1000 x 4096
+    // 55 / 26 / 23 / 19.
+    const int64_t big = tiles(256, 256), mid = tiles(128, 128);
+    const int64_t big_rounds = rounds(big, kNumCu);
+    if (m > 512 && big_rounds >= 4 && big_rounds * 10 < rounds(mid, 2 * kNumCu) * 7)
+      launch_tile<4, 4, 2, 2, 4, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
+    else if (m > 64 && mid >= kNumCu / 2)
+      launch_tile<2, 2, 2, 2, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
+    else if (tiles(128, 64) >= kNumCu)
+      launch_tile<1, 2, 4, 1, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
+    else
+      launch_tile<1, 1, 2, 2, 4, 3>(xc, xs, m, groups, w, ws, out, ldo, st);
     return;
   }
   const uint32_t ntiles = uint32_t((w.rows + 63) / 64);
