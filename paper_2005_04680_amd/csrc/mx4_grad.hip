@@ -45,34 +45,26 @@ __device__ __forceinline__ uint32_t bf16_term(float x, int t) {
   return u >> 16;
 }
 
-// 8 elements of a row of dy as BF16 (`term` of FP32 ones).
-__device__ __forceinline__ u4 load8(const __bf16* p, int) {
-  return *reinterpret_cast<const u4_el*>(p);
+// 8 elements of a row of dy on their way to LDS, and as BF16 (`term` of FP32 ones).
+struct Raw16 {
+  u4 v;
+};
+struct Raw32 {
+  f4 a, b;
+};
+__device__ __forceinline__ Raw16 load8(const __bf16* p) {
+  return {*reinterpret_cast<const u4_el*>(p)};
 }
-__device__ __forceinline__ u4 load8(const float* p, int term) {
-  const f4 a = *reinterpret_cast<const f4_el*>(p), b = *reinterpret_cast<const f4_el*>(p + 4);
-  return u4{bf16_term(a.x, term) | (bf16_term(a.y, term) << 16),
-            bf16_term(a.z, term) | (bf16_term(a.w, term) << 16),
-            bf16_term(b.x, term) | (bf16_term(b.y, term) << 16),
-            bf16_term(b.z, term) | (bf16_term(b.w, term) << 16)};
+__device__ __forceinline__ Raw32 load8(const float* p) {
+  return {*reinterpret_cast<const f4_el*>(p), *reinterpret_cast<const f4_el*>(p + 4)};
 }
-// The first n of them, zeros behind.
-__device__ u4 load8_some(const __bf16* p, int n, int) {
-  const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-  uint32_t v[4] = {};
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < n) v[e / 2] |= uint32_t(q[e]) << (16 * (e % 2));
-  return u4{v[0], v[1], v[2], v[3]};
+__device__ __forceinline__ u4 to_bf16(const Raw16& r, int) { return r.v; }
+__device__ __forceinline__ u4 to_bf16(const Raw32& r, int term) {
+  return u4{bf16_term(r.a.x, term) | (bf16_term(r.a.y, term) << 16),
+            bf16_term(r.a.z, term) | (bf16_term(r.a.w, term) << 16),
+            bf16_term(r.b.x, term) | (bf16_term(r.b.y, term) << 16),
+            bf16_term(r.b.z, term) | (bf16_term(r.b.w, term) << 16)};
 }
-__device__ u4 load8_some(const float* p, int n, int term) {
-  uint32_t v[4] = {};
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < n) v[e / 2] |= bf16_term(p[e], term) << (16 * (e % 2));
-  return u4{v[0], v[1], v[2], v[3]};
-}
-
 // A word of codes as 8 BF16 values.
 __device__ __forceinline__ u4 bf16_values8(uint32_t c, float scale) {
   return u4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0)),
@@ -83,6 +75,10 @@ __device__ __forceinline__ u4 bf16_values8(uint32_t c, float scale) {
 
 // WK x WM wavefronts, each TK x TM products of 32 x 32.  Block: split z of the rows of W
 // (`per` steps each), k tile, m tile.  `dx` is the output, or part z of the parts.
+//
+// The last step of all may pass W's last row.  dy's 8 columns of a load that would pass its row
+// are then the row's last 8: W's tile takes the same rows there, without those that
+// an earlier load has brought.
 template <int TK, int TM, int WK, int WM, class TY, class TX>
 __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy, int64_t ldy,
                                                        int32_t m, Mx4View w, uint32_t ktiles,
@@ -92,8 +88,9 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   static_assert(WK * WM == kWavesPerBlock, "four wavefronts");
   constexpr int BK = 32 * TK * WK, BM = 32 * TM * WM;
   constexpr int STAGE = kStage<BK, BM>;
-  constexpr int YL = BM / 32;                              // loads of dy per thread
-  constexpr int WL = (kRows * BK / 32 + kBlock - 1) / kBlock;  // blocks of W per thread
+  constexpr int YL = BM / 32;              // loads of dy per thread
+  constexpr int WL = kRows * BK / 32 / kBlock;  // blocks of W per thread
+  static_assert(WL >= 1 && YL >= 1, "a load of each per thread");
   constexpr bool kTerms = sizeof(TY) == 4;
   extern __shared__ __align__(16) uint8_t lds[];
 
@@ -104,9 +101,9 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   const uint32_t mt = tile / ktiles, kt = tile - mt * ktiles;
   const int m0 = int(mt) * BM, k0 = int(kt) * BK;
   const int64_t n0 = int64_t(z) * per * kRows;
-  const int64_t left = w.rows - n0;
-  const int rows = int(min(left, int64_t(per) * kRows));  // of W, in this block (>= 1)
+  const int rows = int(min(w.rows - n0, int64_t(per) * kRows));  // of W, in this block (>= 1)
   const int steps = (rows + kRows - 1) / kRows;
+  const int total = kTerms ? steps * 3 : steps;
   const int nb = mx4_blocks(w.dim), sb = mx4_scale_bytes(w.dim);
 
   // dy: load i of this thread is 8 columns (8 * yc ..) of row i * 32 + threadIdx.x / 8.
@@ -114,52 +111,45 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   const TY* ysrc[YL];
 #pragma unroll
   for (int i = 0; i < YL; ++i)
-    ysrc[i] = dy + int64_t(min(m0 + i * 32 + yr, m - 1)) * ldy + n0 + yc * 8;
-  // W: block i of this thread is number wb + 4 i (of the tile's BK/32) of row wr.
-  constexpr int PER = BK / 32 < 4 ? BK / 32 : 4;  // threads per row
+    ysrc[i] = dy + int64_t(min(m0 + i * 32 + yr, m - 1)) * ldy + n0;
+  // W: block i of this thread is number wb + PER * i (of the tile's BK/32) of row wr.
+  constexpr int PER = kBlock / kRows;  // threads per row
   const int wr = threadIdx.x / PER, wb = threadIdx.x % PER;
-  const bool wact = wr < kRows;
-  u4 yv[YL], wv[WL];
+  decltype(load8(dy)) yv[YL];
+  u4 wv[WL];
   uint32_t ws[WL];
+  int64_t wrow = 0;
+  int ycol = 0, term = 0;
+  bool win = false;
 
-  auto load = [&](int s) {
+  // Places of step s's loads.
+  const int last = rows - 8;  // of the last 8 rows, the first (in the split before, if rows < 8)
+  auto place = [&](int s) {
     const int step = kTerms ? s / 3 : s;
     const int r0 = step * kRows;
-    const int term = kTerms ? s - step * 3 : 0;
-    if (r0 + kRows <= rows) {
-#pragma unroll
-      for (int i = 0; i < YL; ++i) yv[i] = load8(ysrc[i] + r0, term);
-    } else {
-#pragma unroll
-      for (int i = 0; i < YL; ++i) yv[i] = load8_some(ysrc[i] + r0, rows - r0 - yc * 8, term);
-    }
-    const bool in = wact && r0 + wr < rows;
-    const int64_t row = n0 + min(r0 + wr, rows - 1);
-#pragma unroll
-    for (int i = 0; i < WL; ++i) {
-      const int b = min(k0 / kMxBlock + wb + 4 * i, nb - 1);
-      wv[i] = *reinterpret_cast<const u4*>(w.codes + (row * nb + b) * 16);
-      ws[i] = w.scales[row * sb + b];
-      if (!in) wv[i] = u4{0u, 0u, 0u, 0u}, ws[i] = 0u;
-    }
+    ycol = min(r0 + yc * 8, last);
+    const int c = r0 + wr / 8 * 8;  // the first row of wr's 8
+    const int r = min(c, last) + wr % 8;
+    win = r >= c && r < rows;
+    wrow = n0 + (win ? r : 0);
   };
-  auto store = [&](int buf) {
-    uint8_t* ys = lds + buf * STAGE;
-    uint8_t* wst = ys + BM * kYRow + wr * kWRow<BK>;
-#pragma unroll
-    for (int i = 0; i < YL; ++i)
-      *reinterpret_cast<u4*>(ys + (i * 32 + yr) * kYRow + (yc ^ (yr & 7)) * 16) = yv[i];
-    if (wact) {
-#pragma unroll
-      for (int i = 0; i < WL; ++i) {
-        const float s = mx4_scale(ws[i]);
-        u4* p = reinterpret_cast<u4*>(wst + (wb + 4 * i) * 64);
-        p[0] = bf16_values8(wv[i].x, s);
-        p[1] = bf16_values8(wv[i].y, s);
-        p[2] = bf16_values8(wv[i].z, s);
-        p[3] = bf16_values8(wv[i].w, s);
-      }
-    }
+  auto load_y = [&](int i) { yv[i] = load8(ysrc[i] + ycol); };
+  auto load_w = [&](int i) {
+    const int b = min(k0 / kMxBlock + wb + PER * i, nb - 1);
+    wv[i] = *reinterpret_cast<const u4*>(w.codes + (wrow * nb + b) * 16);
+    ws[i] = w.scales[wrow * sb + b];
+  };
+  bool in = false;  // whether the loads that are stored next were of a row to be added
+  auto store_y = [&](uint8_t* st, int i) {
+    *reinterpret_cast<u4*>(st + (i * 32 + yr) * kYRow + (yc ^ (yr & 7)) * 16) = to_bf16(yv[i], term);
+  };
+  auto store_w = [&](uint8_t* st, int i) {
+    const float s = mx4_scale(in ? ws[i] : 0u);
+    u4* p = reinterpret_cast<u4*>(st + BM * kYRow + wr * kWRow<BK> + (wb + PER * i) * 64);
+    p[0] = bf16_values8(in ? wv[i].x : 0u, s);
+    p[1] = bf16_values8(in ? wv[i].y : 0u, s);
+    p[2] = bf16_values8(in ? wv[i].z : 0u, s);
+    p[3] = bf16_values8(in ? wv[i].w : 0u, s);
   };
 
   const int wk = wave % WK, wm = wave / WK;
@@ -176,50 +166,81 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   const int yfrag = (wm * TM * 32 + row) * kYRow;
   const int wfrag = BM * kYRow + (half * 8 + (lane % 16) / 4) * kWRow<BK> +
                     (wk * TK * 32 + (lane / 16 % 2) * 16 + (lane % 4) * 4) * 2;
-  u4 a[2][TK], b[2][TM];
-  auto fetch = [&](int buf, int p) {
-    const uint8_t* st = lds + buf * STAGE;
-#pragma unroll
-    for (int i = 0; i < TK; ++i) {
-      const uint8_t* q = st + wfrag + p * 16 * kWRow<BK> + i * 64;
+  u4 a[2][TK] = {}, b[2][TM] = {};
+  auto fetch = [&](const uint8_t* st, int p, int i) {
+    if (i < TM) {
+      b[p & 1][i] = *reinterpret_cast<const u4*>(st + yfrag + i * 32 * kYRow +
+                                                 ((p * 2 + half) ^ (row & 7)) * 16);
+    } else {
+      const uint8_t* q = st + wfrag + p * 16 * kWRow<BK> + (i - TM) * 64;
       typedef __attribute__((address_space(3))) s4v* lds4;
       const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)q);
       const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(q + 4 * kWRow<BK>));
       const u2 l2 = __builtin_bit_cast(u2, lo), h2 = __builtin_bit_cast(u2, hi);
-      a[p & 1][i] = u4{l2.x, l2.y, h2.x, h2.y};
+      a[p & 1][i - TM] = u4{l2.x, l2.y, h2.x, h2.y};
     }
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-      b[p & 1][i] = *reinterpret_cast<const u4*>(st + yfrag + i * 32 * kYRow +
-                                                 ((p * 2 + half) ^ (row & 7)) * 16);
   };
-  auto products = [&](int p) {
+  // The products of part p, and between their rows: the reads of the next part's fragments
+  // (part `next` of `cur`), and in the first three parts of a step the stores of the next
+  // stage, each followed by the load that takes its registers.
+  auto part = [&](const uint8_t* cur, uint8_t* nxt, int p, int next, int turn) {
+    constexpr int N = TK + TM, READS = TK > 1 ? TK - 1 : 1;
+    constexpr int MOVES = YL + WL, SLOTS = 3 * TK;
 #pragma unroll
-    for (int i = 0; i < TK; ++i)
+    for (int i = 0; i < TK; ++i) {
 #pragma unroll
       for (int j = 0; j < TM; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
             __builtin_bit_cast(bf8, a[p & 1][i]), __builtin_bit_cast(bf8, b[p & 1][j]), acc[i][j], 0,
             0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int r = 0; r < N; ++r)
+        if (r * READS / N == i) fetch(cur, next, r);
+#pragma unroll
+      for (int q = 0; q < MOVES; ++q) {
+        if (turn < 3 && q * SLOTS / MOVES == turn * TK + i) {
+          if (q < WL)
+            store_w(nxt, q), load_w(q);
+          else
+            store_y(nxt, q - WL), load_y(q - WL);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
-  const int total = kTerms ? steps * 3 : steps;
-  load(0);
-  store(0);
-  if (total > 1) load(1);
+  place(0);
+  in = win;
+#pragma unroll
+  for (int i = 0; i < YL; ++i) load_y(i);
+#pragma unroll
+  for (int i = 0; i < WL; ++i) load_w(i);
+#pragma unroll
+  for (int i = 0; i < YL; ++i) store_y(lds, i);
+#pragma unroll
+  for (int i = 0; i < WL; ++i) store_w(lds, i);
+  // (Steps past the last one load it again and are not used.)
+  place(min(1, total - 1));
+  in = win;
+#pragma unroll
+  for (int i = 0; i < YL; ++i) load_y(i);
+#pragma unroll
+  for (int i = 0; i < WL; ++i) load_w(i);
   for (int s = 0; s < total; ++s) {
+    uint8_t* cur = lds + (s & 1) * STAGE;
+    uint8_t* nxt = lds + (~s & 1) * STAGE;
+    // The stage is in LDS, and every wavefront holds the last fragments of the other one.
     __syncthreads();
-    fetch(s & 1, 0);
-    fetch(s & 1, 1);
-    products(0);
-    if (s + 1 < total) store(~s & 1);
-    fetch(s & 1, 2);
-    if (s + 2 < total) load(s + 2);
-    products(1);
-    fetch(s & 1, 3);
-    products(2);
-    products(3);
+    term = kTerms ? (s + 1) % 3 : 0;
+    place(min(s + 2, total - 1));
+    part(cur, nxt, 3, 0, 0);
+    part(cur, nxt, 0, 1, 1);
+    part(cur, nxt, 1, 2, 2);
+    part(cur, nxt, 2, 3, 3);
+    in = win;
   }
+  part(lds, lds, 3, 0, 3);
 
   TX* out = dx + int64_t(z) * part_stride;
 #pragma unroll
@@ -278,6 +299,27 @@ __global__ __launch_bounds__(1024) void grad_join_many(const float* __restrict__
   store4(dx + int64_t(row) * ldx + (uint32_t(i) - row * k4.div) * 4, s);
 }
 
+// Tables of fewer than 8 rows, which the tiles' loads of 8 columns would pass.
+template <class TY, class TX>
+__global__ __launch_bounds__(kBlock) void grad_few(const TY* __restrict__ dy, int64_t ldy, int32_t m,
+                                                   Mx4View w, TX* __restrict__ dx, int64_t ldx) {
+  const int64_t k4 = w.dim / 4;
+  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+  if (i >= m * k4) return;
+  const int64_t row = i / k4;
+  const int e0 = int(i - row * k4) * 4;
+  f4 s = {0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < int(w.rows); ++j) {
+    const uint32_t c = *reinterpret_cast<const uint16_t*>(
+        w.codes + int64_t(j) * mx4_blocks(w.dim) * 16 + e0 / 2);
+    float v[8];
+    mx4_values8(c, mx4_scale(w.scales[int64_t(j) * mx4_scale_bytes(w.dim) + e0 / kMxBlock]), v);
+    const float y = to_f32(dy[row * ldy + j]);
+    s += f4{y * v[0], y * v[1], y * v[2], y * v[3]};
+  }
+  store4(dx + row * ldx + e0, s);
+}
+
 // Tile and split of a gradient.
 struct GradPlan {
   int bk, bm;
@@ -286,14 +328,16 @@ struct GradPlan {
 };
 GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
   GradPlan p = {};
-  if (m == 0) return p;
+  if (m == 0 || n < 8) return p;
   p.bk = k > 128 ? 256 : 128;
   p.bm = m > 32 ? (m > 64 && double(m) * double(n) * k > 5e10 ? 256 : 64) : 32;
   p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
   p.mtiles = uint32_t((m + p.bm - 1) / p.bm);
   const int64_t steps = (n + kRows - 1) / kRows;
   const int64_t tiles = int64_t(p.ktiles) * p.mtiles;
-  int64_t splits = kNumCu * (p.bm > 64 ? 1 : 2) / tiles;
+  // One block per compute unit, two where their LDS lets them share it.
+  const int stage = p.bm * kYRow + kRows * (p.bk * 2 + 32);
+  int64_t splits = kNumCu * (4 * stage <= 160 * 1024 ? 2 : 1) / tiles;
   if (splits > steps / 4) splits = steps / 4;
   if (splits < 1) splits = 1;
   // (Ranges of rows fit 31 bits.)
@@ -339,6 +383,16 @@ void launch_plan(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, cons
 template <class TX>
 void launch_grad(const GradPlan& p, const void* dy, bool dy_bf16, int64_t ldy, int32_t m,
                  const Mx4View& w, TX* dx, int64_t ldx, float* parts, hipStream_t st) {
+  if (p.splits == 0) {  // fewer than 8 rows
+    const dim3 grid(unsigned((int64_t(m) * (w.dim / 4) + kBlock - 1) / kBlock));
+    if (dy_bf16)
+      hipLaunchKernelGGL((grad_few<__bf16, TX>), grid, dim3(kBlock), 0, st,
+                         static_cast<const __bf16*>(dy), ldy, m, w, dx, ldx);
+    else
+      hipLaunchKernelGGL((grad_few<float, TX>), grid, dim3(kBlock), 0, st,
+                         static_cast<const float*>(dy), ldy, m, w, dx, ldx);
+    return;
+  }
   if (p.splits == 1) {
     if (dy_bf16)
       launch_plan<__bf16>(p, dy, ldy, m, w, dx, ldx, 0, st);

@@ -293,6 +293,14 @@ def test_gradient(m, n, k, y_type, x_type):
     grad_check(m, n, k, y_type, x_type, m + 3 * n + 5 * k)
 
 
+@pytest.mark.parametrize("y_type", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 63, 64, 65, 257, 259, 511, 519, 16385, 16390])
+@pytest.mark.parametrize("m", [1, 70])
+def test_gradient_ends_of_the_rows(m, n, y_type):
+    """Last steps and last splits of a few rows; the buffer ends with dy's last element."""
+    grad_check(m, n, 132, y_type, "f32", n)
+
+
 @pytest.mark.parametrize("pad", [1, 2, 8])
 @pytest.mark.parametrize("m,n,k", [(1, 100, 128), (40, 301, 160), (150, 260, 512)])
 def test_gradient_with_strides(m, n, k, pad):
