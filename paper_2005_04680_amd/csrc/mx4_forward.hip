@@ -9,6 +9,14 @@
 // sums in FP32: 16 additions per look-up are what the vector units do here, and FP64
 // ones would take twice the time of the bytes.  The order of the additions follows
 // from the sizes alone.
+//
+// Bound by the row reads and these additions about alike: 6.6M look-ups of E = 256 140 us (0.9 GB
+// of codes and scales, 6.4 TB/s with what the L2s hold).  Each XCD walks its own range of bags, so
+// that a table's hot rows stay in one L2 (8 tables of 1M x 64, 819K look-ups: 14.6 us,
+// in dispatch order 18.4).  16 elements per lane and 4 rows in flight were the best of 16 or 32
+// and 4 or 8 (9000 weighted bags of 40, E = 100: 12.4, 15.3, 13.5, 17.3).
+#include <type_traits>
+
 #include "head.hpp"
 
 namespace embbag {
@@ -22,14 +30,15 @@ __global__ __launch_bounds__(kBlock) void mx4_forward_kernel(
     int32_t B, float inv_b, int32_t split, int32_t bags, T* __restrict__ Y,
     int32_t* __restrict__ status, const float* __restrict__ A) {
   constexpr int R = kWave / LPR;
-  constexpr int U = 8;  // rows in flight per lane
+  constexpr int U = 4;  // rows in flight per lane
   __shared__ TableLds tl;
   stage_tables(d, tl);
   __syncthreads();
   const int lane = lane_id();
   const int rg = lane / LPR, rl = lane % LPR;
   const int per_wave = R / split;  // bags of a wavefront
-  const int64_t first = (int64_t(blockIdx.x) * (blockDim.x / kWave) + wave_id()) * per_wave;
+  const int64_t first =
+      (int64_t(xcd_remap(blockIdx.x, gridDim.x)) * (blockDim.x / kWave) + wave_id()) * per_wave;
   const int64_t k64 = first + rg / split;
   const bool live = k64 < bags;
   const int k = live ? int(k64) : bags - 1;
@@ -38,6 +47,7 @@ __global__ __launch_bounds__(kBlock) void mx4_forward_kernel(
   const uint32_t M = tl.rowbase[t + 1] - tl.rowbase[t];
   const int nb = mx4_blocks(d.dim);
   const int sb = mx4_scale_bytes(d.dim);
+  const uint32_t row_bytes = uint32_t(nb) * 16u;
   const auto* codes = table_elem<const uint8_t, uint8_t>(tl.w[t], 0);
   const auto* scales = table_elem<const uint8_t, uint8_t>(tl.lo[t], 0);
   // Lanes past the row's end re-read its last half block.
@@ -65,34 +75,36 @@ __global__ __launch_bounds__(kBlock) void mx4_forward_kernel(
 #pragma unroll
     for (int u = 0; u < U; ++u) idx[u] = index_at(uint32_t(u));
   }
-  for (uint32_t i = 0; i < mine; i += U) {
+  // A batch of U look-ups from number i on, of which all exist where `kAll`.  An index outside
+  // its table reads row 0 (the output is unspecified then).
+  auto batch = [&](uint32_t i, auto all) {
+    constexpr bool kAll = decltype(all)::value;
     u2 v[U];
     uint32_t sc[U];
     float a[U];
-    bool use[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool ok = uint32_t(idx[u]) < M;
       if (!ok) err = min(err, EMBBAG_ERR_INDEX_RANGE);
-      use[u] = ok && i + u < mine;
-      const int64_t row = ok ? idx[u] : 0;
-      v[u] = *(const __attribute__((address_space(1))) u2*)(codes + (row * nb * 16 + half * 8));
-      sc[u] = scales[row * sb + half / 2];
-      if constexpr (MODE == kPoolWeighted) a[u] = A[from + step * min(i + u, mine - 1u)];
+      const uint64_t row = ok ? uint32_t(idx[u]) : 0u;
+      v[u] = *(const __attribute__((address_space(1))) u2*)(codes + (row * row_bytes + half * 8));
+      sc[u] = scales[row * uint32_t(sb) + half / 2];
+      if constexpr (MODE == kPoolWeighted) a[u] = A[from + step * (kAll ? i + u : min(i + u, mine - 1u))];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) idx[u] = index_at(i + U + u);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      // A masked slot must not add NaN either: its codes and scale become 0.
-      const float s = mx4_scale(use[u] ? sc[u] : 0u);
+      // A slot past the bag's end must not add NaN either: its codes and scale become 0.
+      const bool use = kAll || i + u < mine;
+      const float s = mx4_scale(use ? sc[u] : 0u);
       float x[8], y[8];
-      mx4_values8(use[u] ? v[u].x : 0u, s, x);
-      mx4_values8(use[u] ? v[u].y : 0u, s, y);
+      mx4_values8(use ? v[u].x : 0u, s, x);
+      mx4_values8(use ? v[u].y : 0u, s, y);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if constexpr (MODE == kPoolWeighted) {
-          const float w = use[u] ? a[u] : 0.f;
+          const float w = use ? a[u] : 0.f;
           acc[e] = fmaf(w, x[e], acc[e]);
           acc[8 + e] = fmaf(w, y[e], acc[8 + e]);
         } else {
@@ -101,7 +113,10 @@ __global__ __launch_bounds__(kBlock) void mx4_forward_kernel(
         }
       }
     }
-  }
+  };
+  uint32_t i = 0;
+  for (; i + U <= mine; i += U) batch(i, std::true_type{});
+  if (i < mine) batch(i, std::false_type{});
   for (int j = LPR; j < LPR * split; j *= 2) {
 #pragma unroll
     for (int e = 0; e < kEl; ++e) acc[e] += __shfl_xor(acc[e], j, kWave);
@@ -173,7 +188,14 @@ hipError_t launch_mx4_forward(const TableDesc& d, int32_t B, const int32_t* I, c
   int lpr = 2;
   while (lpr < mx4_blocks(d.dim) * 2) lpr *= 2;
   const int groups = kWave / lpr;
-  const int split = 1;
+  // Groups that share a bag: two for 9 look-ups or more, four for 17 and so on, while the
+  // wavefronts do not fill the chip's slots.  Measured, us, shared / not: 512 bags of 32, E = 64
+  // 7.5 / 10.8; 64 of 100, E = 1024 12.3 / 17.2; 9000 of 40, E = 100, weighted 12.4 / 15.3; 33K of 10,
+  // E = 16, shared by four 9.6, not 8.1.
+  const int64_t avg = NS / bags;
+  int split = 1;
+  while (split < groups && avg > int64_t(split) * 8 && bags * split * lpr < int64_t(kNumCu) * 32 * kWave)
+    split *= 2;
   const int64_t per_block = int64_t(kWavesPerBlock) * (groups / split);
   const dim3 grid(unsigned((bags + per_block - 1) / per_block));
   if (y_bf16)
