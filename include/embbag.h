@@ -431,7 +431,8 @@ int embbag_mx4_matmul_grad(const void* dy, int32_t dy_type, int64_t dy_stride, i
  *   out[r][v] = l, or -infinity (whatever l is) where the row's mask has no bit.
  * The lists are bags: seen[seen_offsets[r] .. seen_offsets[r+1]) and
  * bias_ids/biases[bias_offsets[r] .. bias_offsets[r+1]), offsets device int32
- * [rows + 1] as those of the look-ups (0 first, non-decreasing, the count last).
+ * [rows + 1] as those of the look-ups (0 first, non-decreasing, the count, below
+ * 2^30, last).
  * `masks`: device uint32 [num_masks][mask_stride], mask_stride >= ceil(vocab/32);
  * bit v%32 of word v/32 set = v allowed.  Row r uses mask mask_ids[r] (negative:
  * none), or mask r if mask_ids is null (num_masks >= rows then).

@@ -39,9 +39,10 @@ bool product_ok(int32_t m, int64_t n, int32_t k) {
   return m >= 0 && m <= kMaxRowsX && n >= 1 && n <= kInt32Max && dim_ok(k) && m * n <= kMaxMatrix;
 }
 
-// A list per row (offsets, entries) of n entries.
+// A list per row (offsets, entries) of n entries, fewer than 2^30: occurrences are counted in
+// 30 bits.
 int check_list(int32_t rows, const int32_t* offsets, const void* entries, int64_t n) {
-  if (n < 0 || n > kInt32Max) return EMBBAG_ERR_INVALID_ARG;
+  if (n < 0 || n >= (int64_t(1) << 30)) return EMBBAG_ERR_INVALID_ARG;
   if (offsets == nullptr) return n == 0 && entries == nullptr ? EMBBAG_OK : EMBBAG_ERR_INVALID_ARG;
   if (n > 0 && entries == nullptr) return EMBBAG_ERR_INVALID_ARG;
   if (rows == 0 && n > 0) return EMBBAG_ERR_OFFSETS;

@@ -1,23 +1,27 @@
 // What may be answered: penalties for seen tokens, biases and masks on rows of
 // logits.
 //
-// A block takes one slice of one row.  It walks the row's lists and keeps in LDS,
-// for every token of its slice, its occurrences (the top bit: in the prompt; the
-// rest: how often after it) and the place of its last bias: integer additions and
-// maxima, whose order does not matter.  The slice itself is on its way meanwhile, 16 bytes per
-// load, and is read and written once.  A block is a chain of a few memory latencies
-// (offsets, lists, stores), so the lists come in batches of 16 entries per thread and
-// many blocks share a compute unit: a token's two numbers share one word of LDS, 16 bits each.  Rows
-// whose lists are too long for that take their slice in two halves, a word for each.  Every element is read and written by one thread, so
-// that `out` may be `logits`.
+// A block takes one slice of one row.  It walks the row's lists and keeps in LDS a word
+// for every token of its slice: bit 31, seen in the prompt; bit 30, has a bias; the rest, how
+// often seen after the prompt (integer additions, whose order does not matter).  The biases of
+// the slice are few: they go to a list, and a token's last one is found among them.  Its
+// thread gets the token's value through the word and writes it again after the stream.  The
+// slice itself is on its way meanwhile, 16 bytes per load, and is read and written once.  A
+// block is a chain of a few memory latencies (offsets, lists, stores), so the lists
+// come in batches of 16 entries per thread and many blocks share a compute unit.  Every
+// element is read by one thread, so that `out` may be `logits`.
+//
+// Rows with more than kListed biases take them in a pass of their own first, with the words as the
+// places of the tokens' last biases.
 #include "head.hpp"
 
 namespace embbag {
 namespace {
 
 constexpr uint32_t kPrompt = 0x80000000u;
-constexpr uint32_t kPrompt16 = 0x8000u;
+constexpr uint32_t kBiased = 0x40000000u;
 constexpr int kSliceTokens = 4096;
+constexpr int kListed = 1024;  // biases of a row that go to the list (16 bits hold their places)
 
 struct LogitsDev {
   embbag_logits_t a;
@@ -84,8 +88,11 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
                                                         int32_t* __restrict__ status) {
   constexpr int V = kVec<T>;
   constexpr int NV = kSliceTokens / (kBlock * V);  // vectors per thread
-  constexpr bool BOTH = SEEN && BIAS, ANY = SEEN || BIAS;
-  __shared__ __align__(16) uint32_t lds[ANY ? kSliceTokens : 4];
+  constexpr int PER = kListed / kBlock;            // listed biases per thread
+  constexpr bool ANY = SEEN || BIAS;
+  __shared__ __align__(16) uint32_t words[ANY ? kSliceTokens : 4];
+  __shared__ uint32_t listed[BIAS ? kListed : 1];  // token of the slice << 16 | place in the row's list
+  __shared__ uint32_t num_listed;
   const embbag_logits_t& a = dv.a;
   const int r = int(blockIdx.x / dv.slices);
   const int base = int(blockIdx.x - uint32_t(r) * dv.slices) * kSliceTokens;
@@ -125,87 +132,128 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
   const bool plain = rho > 0x1p-60f && rho < 0x1p60f;
   const float freq = SEEN && a.frequency != nullptr ? a.frequency[r] : 0.f;
   const float pres = SEEN && a.presence != nullptr ? a.presence[r] : 0.f;
-
-  // With both lists: one word of two 16-bit numbers, or halves of the slice with two words.
-  const bool narrow = BOTH && uint32_t(s1 - s0) < kPrompt16 && uint32_t(b1 - b0) < 0xFFFFu;
-  const int parts = BOTH && !narrow ? 2 : 1;
-  for (int part = 0; part < parts; ++part) {
-    const int tokens = kSliceTokens / parts, from = base + part * tokens;
-    const uint32_t here = uint32_t(max(0, min(tokens, a.vocab - from)));
-    uint32_t* bia = lds + (BOTH && !narrow ? tokens : 0);
-    if constexpr (ANY) {
-      if (part > 0) __syncthreads();
+  auto clear = [&]() {
 #pragma unroll
-      for (int i = 0; i < kSliceTokens / (kBlock * 4); ++i)
-        *reinterpret_cast<u4*>(lds + (i * kBlock + threadIdx.x) * 4) = u4{0u, 0u, 0u, 0u};
-      __syncthreads();
+    for (int i = 0; i < kSliceTokens / (kBlock * 4); ++i)
+      *reinterpret_cast<u4*>(words + (i * kBlock + threadIdx.x) * 4) = u4{0u, 0u, 0u, 0u};
+  };
+
+  // A long list of biases: their sum with 0 for this thread's tokens (-0.0 where there is none, which
+  // adds nothing).
+  const bool longer = BIAS && b1 - b0 > kListed;
+  float add[NV * V];
+  if (longer) {
+    clear();
+    __syncthreads();
+    const uint32_t worst = walk(a.bias_ids, b0, b1, [&](uint32_t j, uint32_t v) {
+      const uint32_t at = v - uint32_t(base);
+      if (at < uint32_t(len)) atomicMax(&words[at], j + 1u);
+    });
+    if (worst >= uint32_t(a.vocab)) err = min(err, EMBBAG_ERR_INDEX_RANGE);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV * V; ++i) {
+      const int v = (i / V * kBlock + int(threadIdx.x)) * V + i % V;
+      const uint32_t b = v < len ? words[v] : 0u;
+      add[i] = b != 0u ? a.biases[int64_t(b0) + b - 1] : -0.f;
     }
-    // (A shared word takes its maxima while its low half is 0.)
-    if constexpr (BIAS) {
+    __syncthreads();
+  }
+
+  if constexpr (ANY) {
+    clear();
+    if (threadIdx.x == 0) num_listed = 0u;
+    __syncthreads();
+  }
+  if constexpr (BIAS) {
+    if (!longer) {
       const uint32_t worst = walk(a.bias_ids, b0, b1, [&](uint32_t j, uint32_t v) {
-        const uint32_t at = v - uint32_t(from);
-        if (at < here) atomicMax(&bia[at], narrow ? (j + 1u) << 16 : j + 1u);
-      });
-      if (worst >= uint32_t(a.vocab)) err = min(err, EMBBAG_ERR_INDEX_RANGE);
-      if constexpr (SEEN) __syncthreads();
-    }
-    if constexpr (SEEN) {
-      const uint32_t prompt = narrow ? kPrompt16 : kPrompt;
-      const uint32_t worst = walk(a.seen, s0, s1, [&](uint32_t j, uint32_t v) {
-        const uint32_t at = v - uint32_t(from);
-        if (at < here) {
-          if (int64_t(j) < plen)
-            atomicOr(&lds[at], prompt);
-          else
-            atomicAdd(&lds[at], 1u);
+        const uint32_t at = v - uint32_t(base);
+        if (at < uint32_t(len)) {
+          listed[atomicAdd(&num_listed, 1u)] = at << 16 | j;
+          atomicOr(&words[at], kBiased);
         }
       });
       if (worst >= uint32_t(a.vocab)) err = min(err, EMBBAG_ERR_INDEX_RANGE);
     }
-    if constexpr (ANY) __syncthreads();
+  }
+  if constexpr (SEEN) {
+    const uint32_t worst = walk(a.seen, s0, s1, [&](uint32_t j, uint32_t v) {
+      const uint32_t at = v - uint32_t(base);
+      if (at < uint32_t(len)) {
+        if (int64_t(j) < plen)
+          atomicOr(&words[at], kPrompt);
+        else
+          atomicAdd(&words[at], 1u);
+      }
+    });
+    if (worst >= uint32_t(a.vocab)) err = min(err, EMBBAG_ERR_INDEX_RANGE);
+  }
+  if constexpr (ANY) __syncthreads();
+
+  // The last listed bias of a token finds itself: no entry of the token has a later place.
+  const int n = BIAS ? int(num_listed) : 0;
+  float bias[PER];
+  int token[PER];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int e = q * kBlock + int(threadIdx.x);
+    token[q] = -1;
+    if (!BIAS || q * kBlock >= n || e >= n) continue;
+    const uint32_t mine = listed[e];
+    bool lastly = true;
+    for (int i = 0; i < n; ++i) lastly = lastly && (listed[i] <= mine || (listed[i] >> 16) != (mine >> 16));
+    if (lastly) {
+      token[q] = int(mine >> 16);
+      bias[q] = a.biases[int64_t(b0) + (mine & 0xFFFFu)];
+    }
+  }
 
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if (parts == 2 && i / (NV / 2) != part) continue;
-      const int v = (i * kBlock + int(threadIdx.x)) * V;
-      if (v >= len) continue;
-      float l[V];
-      unpack16(raw[i], l);
-      if constexpr (ANY) {
-        uint32_t o[V], b[V], any = 0u;
-        const uint32_t* at = lds + (v - part * tokens);
+  for (int i = 0; i < NV; ++i) {
+    const int v = (i * kBlock + int(threadIdx.x)) * V;
+    if (v >= len) continue;
+    float l[V];
+    unpack16(raw[i], l);
+    if constexpr (ANY) {
+      uint32_t o[V], any = 0u;
 #pragma unroll
-        for (int e = 0; e < V; e += 4) {
-          const u4 w = *reinterpret_cast<const u4*>(at + e);
-          o[e] = w.x, o[e + 1] = w.y, o[e + 2] = w.z, o[e + 3] = w.w;
-          any |= w.x | w.y | w.z | w.w;
-        }
-        if (BOTH && !narrow) {
+      for (int e = 0; e < V; e += 4) {
+        const u4 w = *reinterpret_cast<const u4*>(words + v + e);
+        o[e] = w.x, o[e + 1] = w.y, o[e + 2] = w.z, o[e + 3] = w.w;
+        any |= w.x | w.y | w.z | w.w;
+      }
+      if (any != 0u) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) b[e] = at[tokens + e], any |= b[e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            b[e] = BOTH ? o[e] >> 16 : o[e];
-            if (BOTH) o[e] = (o[e] & kPrompt16) << 16 | (o[e] & (kPrompt16 - 1u));
+        for (int e = 0; e < V; ++e) {
+          if (SEEN && (o[e] & ~kBiased) != 0u) {
+            l[e] = l[e] > 0.f ? (plain ? divide(l[e], rho, inv) : l[e] / rho) : l[e] * rho;
+            const uint32_t c = o[e] & (kBiased - 1u);
+            l[e] -= c != 0u ? freq * float(c) + pres : 0.f;
           }
-        }
-        if (any != 0u) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            if (SEEN && o[e] != 0u) {
-              l[e] = l[e] > 0.f ? (plain ? divide(l[e], rho, inv) : l[e] / rho) : l[e] * rho;
-              const uint32_t c = o[e] & ~kPrompt;
-              l[e] -= c != 0u ? freq * float(c) + pres : 0.f;
-            }
-            if (BIAS && b[e] != 0u) l[e] += a.biases[int64_t(b0) + b[e] - 1];
-          }
+          if (BIAS && (o[e] & kBiased) != 0u) words[v + e] = __float_as_uint(l[e]);
         }
       }
+      if (longer) {
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (((bits[i] >> e) & 1u) == 0u) l[e] = low();
-      store_vec(y + v, len - v, l);
+        for (int e = 0; e < V; ++e) l[e] += add[i * V + e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (((bits[i] >> e) & 1u) == 0u) l[e] = low();
+    store_vec(y + v, len - v, l);
+  }
+  if constexpr (BIAS) {
+    if (n > 0) {
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        const int v = token[q];
+        if (v < 0) continue;
+        const bool out = mask != nullptr && ((mask[(base + v) >> 5] >> ((base + v) & 31)) & 1u) == 0u;
+        y[v] = T(out ? low() : __uint_as_float(words[v]) + bias[q]);
+      }
     }
   }
   if (err != 0 && status != nullptr) atomicMin(status, err);

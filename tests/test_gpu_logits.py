@@ -122,9 +122,10 @@ def test_parts_left_out():
 
 
 @pytest.mark.parametrize("type_", ["f32", "bf16"])
-@pytest.mark.parametrize("seen,biases", [(32767, 40), (32768, 40), (40, 65534), (40, 65535), (70000, 70000)])
+@pytest.mark.parametrize("seen,biases", [(32767, 40), (32768, 40), (40, 65534), (40, 65535), (70000, 70000),
+                                         (9, 1023), (9, 1024), (9, 1025)])
 def test_long_lists(seen, biases, type_):
-    """Lists around the lengths that 16-bit numbers hold, one token most of the time."""
+    """Lists around the lengths that are treated apart, one token most of the time."""
     x, kw, want = case(2, 9000, 0, 0, 2, type_, 13)
     rng = np.random.default_rng(seen + biases)
     s = np.where(rng.random(seen) < 0.9, 4100, rng.integers(0, 9000, size=seen)).astype(np.int32)
