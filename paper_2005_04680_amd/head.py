@@ -79,15 +79,21 @@ def _types():
     return {torch.float32: EMBBAG_F32, torch.bfloat16: EMBBAG_BF16}
 
 
-_type_of = None
+_type_of = _I32_T = _F32_T = None
+
+
+def _load_types():
+    global _type_of, _I32_T, _F32_T
+    import torch
+    _I32_T, _F32_T = torch.int32, torch.float32
+    _type_of = _types()
 
 
 def _matrix(t, cols, name):
     """(pointer, type, row stride) of a 2-D FP32 or BF16 GPU tensor of `cols`
     columns whose rows are contiguous."""
-    global _type_of
     if _type_of is None:
-        _type_of = _types()
+        _load_types()
     code = _type_of.get(t.dtype)
     if code is None:
         raise TypeError(f"{name}: dtype {t.dtype}, expected float32 or bfloat16")
@@ -98,7 +104,7 @@ def _matrix(t, cols, name):
         raise ValueError(f"{name}: shape {tuple(shape)}, expected 2-D with {cols} columns")
     s0, s1 = t.stride()
     if shape[0] <= 1:
-        s0 = max(cols, (cols + 3) // 4 * 4)  # no second row: any stride
+        s0 = (cols + 3) // 4 * 4  # no second row: any stride
     if s1 != 1 and cols > 1:
         raise TypeError(f"{name}: rows must be contiguous")
     if s0 < cols:
@@ -106,20 +112,26 @@ def _matrix(t, cols, name):
     return t.data_ptr(), code, s0
 
 
+def _vector(t, n, name, dtype):
+    """Pointer of a contiguous GPU tensor of n elements of `dtype` (None: null; n
+    None: any number)."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (n is None or t.numel() == n):
+        return t.data_ptr()
+    if n is not None:
+        _check_numel(t, n, name)
+    return _ptr(t, (dtype,), name)
+
+
 def _list(entries, offsets, rows, name):
     """Pointers and length of a list per row (None, None: none)."""
     if offsets is None:
         _need(entries is None, f"{name}: entries without offsets")
         return None, None, 0
-    _check_numel(offsets, rows + 1, f"{name} offsets")
     _need(entries is not None, f"{name}: offsets without entries")
-    return (_ptr(entries, _dt(*_I32), name), _ptr(offsets, _dt(*_I32), f"{name} offsets"),
-            entries.numel())
-
-
-def _per_row(t, rows, name, dtype="float32"):
-    _check_numel(t, rows, name)
-    return _ptr(t, _dt(dtype), name)
+    return (_vector(entries, None, name, _I32_T),
+            _vector(offsets, rows + 1, f"{name} offsets", _I32_T), entries.numel())
 
 
 def _ws(workspace):
@@ -271,26 +283,26 @@ def embbag_logits_process(logits, out, seen=None, seen_offsets=None, prompt_lens
         raise TypeError(f"out: dtype {out.dtype}, expected {logits.dtype} like logits")
     rows = logits.shape[0]
     _need(out.shape[0] == rows, f"out: {out.shape[0]} rows, expected {rows}")
-    a = _Logits(rows, vocab, ty, p, ld, q, lq)
-    a.seen, a.seen_offsets, a.num_seen = _list(seen, seen_offsets, rows, "seen")
-    a.prompt_lens = _per_row(prompt_lens, rows, "prompt_lens", "int32")
-    a.repetition = _per_row(repetition, rows, "repetition")
-    a.frequency = _per_row(frequency, rows, "frequency")
-    a.presence = _per_row(presence, rows, "presence")
-    a.bias_ids, a.bias_offsets, a.num_biases = _list(bias_ids, bias_offsets, rows, "bias_ids")
-    if bias_ids is not None:
-        _need(biases is not None, "bias_ids without biases")
-    _check_numel(biases, a.num_biases, "biases")
-    a.biases = _ptr(biases, _dt("float32"), "biases")
+    seen_p, seen_o, num_seen = _list(seen, seen_offsets, rows, "seen")
+    bias_p, bias_o, num_biases = _list(bias_ids, bias_offsets, rows, "bias_ids")
+    if bias_ids is not None and biases is None:
+        raise ValueError("bias_ids without biases")
+    masks_p, num_masks, mask_stride = None, 0, 0
     if masks is not None:
-        _need(len(masks.shape) == 2 and masks.shape[1] * 32 >= vocab,
-              f"masks: shape {tuple(masks.shape)}, expected 2-D with at least "
-              f"{(vocab + 31) // 32} words a row")
-        a.masks = _ptr(masks, _dt(*_U32), "masks")
-        a.num_masks, a.mask_stride = masks.shape
-        if mask_ids is None:
-            _need(masks.shape[0] >= rows, f"masks: {masks.shape[0]} for {rows} rows and no mask_ids")
-    a.mask_ids = _per_row(mask_ids, rows, "mask_ids", "int32")
+        if len(masks.shape) != 2 or masks.shape[1] * 32 < vocab:
+            raise ValueError(f"masks: shape {tuple(masks.shape)}, expected 2-D with at least "
+                             f"{(vocab + 31) // 32} words a row")
+        masks_p = _ptr(masks, _dt(*_U32), "masks")
+        num_masks, mask_stride = masks.shape
+        if mask_ids is None and num_masks < rows:
+            raise ValueError(f"masks: {num_masks} for {rows} rows and no mask_ids")
+    a = _Logits(rows, vocab, ty, p, ld, q, lq, seen_p, seen_o, num_seen,
+                _vector(prompt_lens, rows, "prompt_lens", _I32_T),
+                _vector(repetition, rows, "repetition", _F32_T),
+                _vector(frequency, rows, "frequency", _F32_T),
+                _vector(presence, rows, "presence", _F32_T), bias_p, bias_o,
+                _vector(biases, num_biases, "biases", _F32_T), num_biases, masks_p, mask_stride,
+                num_masks, _vector(mask_ids, rows, "mask_ids", _I32_T))
     return _lib().embbag_logits_process(C.byref(a), _status_ptr(d_status), _stream(stream))
 
 
@@ -309,19 +321,19 @@ def embbag_distill(logits, teacher_ids, teacher_logits, temperature, loss, works
     _need(len(teacher_ids.shape) == 2 and teacher_ids.shape[0] == rows,
           f"teacher_ids: shape {tuple(teacher_ids.shape)}, expected [{rows}, top]")
     top = teacher_ids.shape[1]
-    _check_numel(teacher_logits, rows * top, "teacher_logits")
-    _check_numel(loss, rows, "loss")
-    a = _Distill(rows, vocab, ty, p, ld, top, _ptr(teacher_ids, _dt(*_I32), "teacher_ids"))
-    a.teacher = _ptr(teacher_logits, _dt("float32", "bfloat16"), "teacher_logits")
-    a.teacher_type = EMBBAG_BF16 if teacher_logits.element_size() == 2 else EMBBAG_F32
-    a.temperature = float(temperature)
-    a.row_weights = _per_row(row_weights, rows, "row_weights")
-    a.loss = _ptr(loss, _dt("float32"), "loss")
+    if teacher_logits.numel() != rows * top:
+        _check_numel(teacher_logits, rows * top, "teacher_logits")
+    q, lq = None, 0
     if grad is not None:
         q, tq, lq = _matrix(grad, vocab, "grad")
         if tq != ty:
             raise TypeError(f"grad: dtype {grad.dtype}, expected {logits.dtype} like logits")
         _need(grad.shape[0] == rows, f"grad: {grad.shape[0]} rows, expected {rows}")
-        a.grad, a.grad_stride = q, lq
+    a = _Distill(rows, vocab, ty, p, ld, top,
+                 _vector(teacher_ids, None, "teacher_ids", _I32_T),
+                 EMBBAG_BF16 if teacher_logits.element_size() == 2 else EMBBAG_F32,
+                 _ptr(teacher_logits, _dt("float32", "bfloat16"), "teacher_logits"),
+                 float(temperature), _vector(row_weights, rows, "row_weights", _F32_T),
+                 _vector(loss, rows, "loss", _F32_T), q, lq)
     w, n = _ws(workspace)
     return _lib().embbag_distill(C.byref(a), w, n, _status_ptr(d_status), _stream(stream))
