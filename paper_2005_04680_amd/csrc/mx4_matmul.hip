@@ -18,6 +18,26 @@ constexpr int kGroupBytes = 64;  // their codes
 constexpr int kPad = 256;        // rows of scales are padded to the largest tile
 constexpr size_t kLdsPerCu = 160 * 1024;
 
+// The codes of 8 elements of a row from e0 on (zeros past k) and their block's scale byte; four
+// neighbouring lanes hold a block, as in mx4_quantize.
+template <class T>
+__device__ __forceinline__ uint32_t quantize8(const T* row, int e0, int k, uint32_t* byte) {
+  const f4 zero = {0.f, 0.f, 0.f, 0.f};
+  const f4 x0 = e0 < k ? load4(row + e0) : zero;
+  const f4 x1 = e0 + 4 < k ? load4(row + e0 + 4) : zero;
+  float y[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+  uint32_t amax = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+  amax = max(amax, uint32_t(__shfl_xor(int(amax), 1, 4)));
+  amax = max(amax, uint32_t(__shfl_xor(int(amax), 2, 4)));
+  float factor;
+  *byte = mx4_scale_of(amax, &factor);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] *= factor;
+  return *byte == 255u ? 0u : mx4_codes8(y);
+}
+
 // x rounded to the storage of the table: codes [m][groups * 64] (zeros past k), scales as words of
 // 4 blocks [groups][xpitch].  Four lanes per block, as mx4_quantize.  Blocks from `xblocks` on
 // copy W's scales to words [groups][wpitch].
@@ -56,22 +76,8 @@ __global__ __launch_bounds__(kBlock) void pack_x(const T* __restrict__ x, int64_
   if (g4 >= int64_t(m) * G) return;
   const uint32_t row = quotient(uint32_t(g4), groups);
   const int g = int(uint32_t(g4) - row * groups.div), j = int(u % 4);
-  const int e0 = g * kGroup + j * kMxBlock + part * 8;
-  const T* p = x + int64_t(row) * stride + e0;
-  const f4 zero = {0.f, 0.f, 0.f, 0.f};
-  const f4 x0 = e0 < k ? load4(p) : zero;
-  const f4 x1 = e0 + 4 < k ? load4(p + 4) : zero;
-  float y[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-  amax = max(amax, uint32_t(__shfl_xor(int(amax), 1, 4)));
-  amax = max(amax, uint32_t(__shfl_xor(int(amax), 2, 4)));
-  float factor;
-  const uint32_t byte = mx4_scale_of(amax, &factor);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] *= factor;
-  const uint32_t c = byte == 255u ? 0u : mx4_codes8(y);
+  uint32_t byte;
+  const uint32_t c = quantize8(x + int64_t(row) * stride, g * kGroup + j * kMxBlock + part * 8, k, &byte);
   *reinterpret_cast<uint32_t*>(codes + (int64_t(row) * G + g) * kGroupBytes + j * 16 + part * 4) = c;
   if (part == 0) scales[(int64_t(g) * xpitch + row) * 4 + j] = uint8_t(byte);
 }
@@ -356,58 +362,84 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   wait_loads<0>();
 }
 
-// One wavefront per 16 rows of W and 16 of x, straight from memory: lane l holds
+// One wavefront per 16 rows of W and up to 16 of x, W straight from memory: lane l holds
 // row l % 16, and of every 4 groups of 128 elements the group l / 16; the four blocks
-// of its group go through four products whose scales are the bytes of one word.
-template <class T>
-__global__ __launch_bounds__(kBlock) void scores_direct(const uint8_t* __restrict__ xc,
+// of its group go through four products whose scales are the bytes of one word.  Few elements of x
+// (kFused) are rounded by every block for itself, others by pack_x before.  One row of x, 200003 x
+// 1024: 21 us, 5.2 TB/s; bound by W.
+constexpr int kFused = 8192;  // elements of x, rows padded to groups
+
+template <class TX, class T, bool FUSED>
+__global__ __launch_bounds__(kBlock) void scores_direct(const TX* __restrict__ x, int64_t stride,
+                                                        const uint8_t* __restrict__ xc,
                                                         const uint32_t* __restrict__ xs,
                                                         int64_t xpitch, Mx4View w, int32_t m,
-                                                        int32_t groups,
-                                                        uint32_t ntiles, T* __restrict__ out,
+                                                        int32_t groups, T* __restrict__ out,
                                                         int64_t ldo) {
+  __shared__ __align__(16) uint8_t codes[FUSED ? kFused / 2 : 16];
+  __shared__ __align__(16) uint8_t scales[FUSED ? kFused / kMxBlock : 16];
   const int lane = lane_id(), r = lane % 16, q = lane / 16;
-  const uint32_t nt = blockIdx.x % ntiles, mt = blockIdx.x / ntiles;
-  const int64_t n0 = (int64_t(nt) * kWavesPerBlock + wave_id()) * 16;
-  if (n0 >= w.rows) return;
-  const int m0 = int(mt) * 16;
+  const int64_t n0 = (int64_t(blockIdx.x) * kWavesPerBlock + wave_id()) * 16;
   const int nb = mx4_blocks(w.dim);
   const int64_t wn = min(n0 + r, w.rows - 1);
-  const int xm = min(m0 + r, m - 1);
+  const int xm = min(r, m - 1);
   const uint8_t* wc = w.codes + wn * nb * 16;
   const uint32_t* wsc = reinterpret_cast<const uint32_t*>(w.scales) + wn * groups;
-  const uint8_t* xcr = xc + int64_t(xm) * groups * kGroupBytes;
+
+  u4 b[4];
+  uint32_t sw;
+  auto load_w = [&](int g) {
+    sw = g < groups ? wsc[g] : 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      b[j] = g * 4 + j < nb ? *reinterpret_cast<const u4*>(wc + (g * 4 + j) * 16)
+                            : u4{0u, 0u, 0u, 0u};
+  };
+  load_w(q);
+  if constexpr (FUSED) {
+    const int units = m * groups * 4;
+    for (int u = threadIdx.x / 4; u < units; u += kBlock / 4) {
+      const int row = u / (groups * 4), block = u - row * groups * 4;
+      uint32_t byte;
+      const uint32_t c = quantize8(x + row * stride, block * kMxBlock + int(threadIdx.x % 4) * 8, w.dim, &byte);
+      *reinterpret_cast<uint32_t*>(codes + u * 16 + threadIdx.x % 4 * 4) = c;
+      if (threadIdx.x % 4 == 0) scales[u] = uint8_t(byte);
+    }
+    __syncthreads();
+  }
   f4 c = {0.f, 0.f, 0.f, 0.f};
   for (int g0 = 0; g0 < groups; g0 += 4) {
     const int g = g0 + q;
     const bool in = g < groups;
-    const uint32_t sw = in ? wsc[g] : 0u;
-    const uint32_t sx = in ? xs[g * xpitch + xm] : 0u;
-    u4 a[4], b[4];
+    uint32_t sx = 0u;
+    u4 a[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const u4 none = {0u, 0u, 0u, 0u};
-      a[j] = in ? *reinterpret_cast<const u4*>(xcr + (g * 4 + j) * 16) : none;
-      b[j] = g * 4 + j < nb ? *reinterpret_cast<const u4*>(wc + (g * 4 + j) * 16) : none;
+    for (int j = 0; j < 4; ++j) a[j] = u4{0u, 0u, 0u, 0u};
+    if (in) {
+      const int64_t at = int64_t(xm) * groups + g;
+      sx = FUSED ? *reinterpret_cast<const uint32_t*>(scales + at * 4) : xs[g * xpitch + xm];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        a[j] = FUSED ? *reinterpret_cast<const u4*>(codes + at * kGroupBytes + j * 16)
+                     : *reinterpret_cast<const u4*>(xc + at * kGroupBytes + j * 16);
     }
-#define EMB_MFMA(J)                                                                       \
-  {                                                                                       \
-    const i8v av = {int(a[J].x), int(a[J].y), int(a[J].z), int(a[J].w), 0, 0, 0, 0};      \
-    const i8v bv = {int(b[J].x), int(b[J].y), int(b[J].z), int(b[J].w), 0, 0, 0, 0};      \
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4, 4, J, int(sx), J,  \
-                                                         int(sw));                        \
-  }
-    EMB_MFMA(0);
-    EMB_MFMA(1);
-    EMB_MFMA(2);
-    EMB_MFMA(3);
+    const u4 v[4] = {b[0], b[1], b[2], b[3]};
+    const uint32_t sv = sw;
+    if (g0 + 4 < groups) load_w(g + 4);
+#define EMB_MFMA(J)                                                                          \
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag8(a[J]), frag8(v[J]), c, 4, 4, J, \
+                                                       int(sx), J, int(sv));
+    EMB_MFMA(0)
+    EMB_MFMA(1)
+    EMB_MFMA(2)
+    EMB_MFMA(3)
 #undef EMB_MFMA
   }
   const int64_t n = n0 + r;
   if (n >= w.rows) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int mm = m0 + q * 4 + i;
+    const int mm = q * 4 + i;
     if (mm < m) out[int64_t(mm) * ldo + n] = T(c[i]);
   }
 }
@@ -424,7 +456,11 @@ int64_t padded(int64_t rows) { return (rows + kPad - 1) / kPad * kPad; }
 struct ScoreLayout {
   size_t xs, ws, total;
 };
+// Whether every block rounds x for itself.
+bool fused(int32_t m, int32_t k) { return m <= 16 && m * ((k + kGroup - 1) / kGroup) * kGroup <= kFused; }
+
 ScoreLayout score_layout(int32_t m, int64_t n, int32_t k) {
+  if (fused(m, k)) return {0, 0, 0};
   const size_t groups = size_t((k + kGroup - 1) / kGroup);
   ScoreLayout L;
   L.xs = align256(size_t(m) * groups * kGroupBytes);
@@ -456,6 +492,14 @@ void launch_tile(const uint8_t* xc, const uint32_t* xs, int32_t m, int32_t group
                      ws, padded(w.rows), mtiles, ntiles, out, ldo);
 }
 
+template <bool FUSED, class TX, class T>
+void launch_direct(const TX* x, int64_t stride, const uint8_t* xc, const uint32_t* xs, int32_t m,
+                   int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
+  const dim3 grid(uint32_t((w.rows + 63) / 64));
+  hipLaunchKernelGGL((scores_direct<TX, T, FUSED>), grid, dim3(kBlock), 0, st, x, stride, xc, xs,
+                     padded(m), w, m, groups, out, ldo);
+}
+
 template <class T>
 void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, int32_t m,
                    int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
@@ -484,10 +528,7 @@ void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, in
       launch_tile<1, 1, 2, 2, 4, 3>(xc, xs, m, groups, w, ws, out, ldo, st);
     return;
   }
-  const uint32_t ntiles = uint32_t((w.rows + 63) / 64);
-  const dim3 grid(ntiles * unsigned((m + 15) / 16));
-  hipLaunchKernelGGL(scores_direct<T>, grid, dim3(kBlock), 0, st, xc, xs, padded(m), w, m, groups,
-                     ntiles, out, ldo);
+  launch_direct<false>(static_cast<const T*>(nullptr), 0, xc, xs, m, groups, w, out, ldo, st);
 }
 
 }  // namespace
@@ -504,6 +545,20 @@ hipError_t launch_mx4_matmul(const void* x, bool x_bf16, int64_t x_stride, int32
   uint8_t* xs = xc + L.xs;
   uint32_t* wst = reinterpret_cast<uint32_t*>(ws + L.ws);
   const uint32_t* wsc = reinterpret_cast<const uint32_t*>(w.scales);
+  if (fused(m, w.dim)) {
+    auto run = [&](auto* xp, auto* op) {
+      launch_direct<true>(xp, x_stride, nullptr, nullptr, m, groups, w, op, out_stride, st);
+    };
+    const auto* xb = static_cast<const __bf16*>(x);
+    const auto* xf = static_cast<const float*>(x);
+    auto* ob = static_cast<__bf16*>(out);
+    auto* of = static_cast<float*>(out);
+    if (x_bf16)
+      out_bf16 ? run(xb, ob) : run(xb, of);
+    else
+      out_bf16 ? run(xf, ob) : run(xf, of);
+    return hipGetLastError();
+  }
   const int64_t units = int64_t(m) * groups * 4;
   const uint32_t xblocks = uint32_t((units + kBlock / 4 - 1) / (kBlock / 4));
   const uint32_t wblocks = m > 16 ? uint32_t((w.rows + kWave - 1) / kWave) : 0u;
