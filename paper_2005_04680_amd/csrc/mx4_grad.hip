@@ -12,6 +12,11 @@
 // Where tiles alone leave compute units idle the rows of W are split over blocks as
 // well; the FP32 parts are then added in order by a second kernel.
 //
+// 4096 x 32768 x 1024, BF16: 248 us with the parts' sum, 1.1 PFLOP/s (a BF16 library product of
+// these sizes 398 us, 1.4 PFLOP/s for its best shapes, 1.9 from registers on such data).  Bound by
+// the products and the LDS traffic between them; without the interleaving of `part` 409 us.
+// 200 x 50001 x 256: 22 us, bound by its chain of steps.
+//
 // An FP32 dy is the sum of three BF16 terms of 8 bits each, by truncation; the steps go through
 // the terms one after the other.
 #include "head.hpp"
@@ -329,6 +334,8 @@ struct GradPlan {
 GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
   GradPlan p = {};
   if (m == 0 || n < 8) return p;
+  // 256 rows of x per tile where the product is large; else 64 or 32, which leave more blocks and
+  // fewer bytes of parts (200 x 50001 x 256: 64 22 us, 256 60).
   p.bk = k > 128 ? 256 : 128;
   p.bm = m > 32 ? (m > 64 && double(m) * double(n) * k > 5e10 ? 256 : 64) : 32;
   p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
