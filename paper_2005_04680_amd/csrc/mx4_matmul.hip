@@ -3,10 +3,12 @@
 // Both sides are blocks of 32 codes with a power of two, which the scaled matrix instructions
 // take as they are: the products are exact and the sums FP32.  Three ways, by the rows of x: up to 16
 // stream W straight into the products (bound by W's bytes), more go through LDS in
-// tiles.  4096 x 65536 x 4096, BF16 in and out: 632 us, 3.5 PFLOP/s, of which 18 us round x and
+// tiles.  4096 x 65536 x 4096, BF16 in and out: 613 us, 3.6 PFLOP/s, of which 18 us round x and
 // copy W's scales; the same instructions from registers reach 5.7 PFLOP/s on such data (8.7 on
 // zeros: the clock falls with the bits that toggle, to 1.9 GHz on average here), a BF16 library
-// product of these sizes takes 1548 us.  With k = 256 the output's bytes bound it (148 us for 537 MB).
+// product of these sizes takes 1548 us.  With k = 256 the output's bytes bound it (145 us for 537 MB).
+// Outputs whose rows do not begin at 128-byte lines are slower there: 2889 x 89088 x 64 into BF16 110
+// us, 2889 x 89061 178; the L2s' write requests grow by half.
 #include "head.hpp"
 
 namespace embbag {
@@ -114,19 +116,23 @@ __device__ __forceinline__ void block_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Tiles of 32 rows of W that a wavefront turns around at once: 128 bytes of a row of the output.
+// Tiles of 32 rows of W that a wavefront turns around at once: 256 bytes of a row of the output where
+// it has four of them, 128 else.
 template <class T>
 constexpr int turn_tiles(int tn) {
-  return tn < 4 / int(sizeof(T)) ? tn : 4 / int(sizeof(T));
+  const int most = (tn < 4 ? 4 : 8) / int(sizeof(T));
+  return tn < most ? tn : most;
 }
 
-// Tile number id: strips of 8 m tiles, in a strip n tile after n tile.  An XCD's 32 blocks then
-// hold 8 tiles of x and 4 of W at a time.
-__device__ __forceinline__ void tile_of(uint32_t id, uint32_t mtiles, uint32_t ntiles, uint32_t* mt,
-                                        uint32_t* nt) {
-  constexpr uint32_t kStrip = 8;
-  const uint32_t strip = id / (kStrip * ntiles);
-  const uint32_t m0 = strip * kStrip, width = min(kStrip, mtiles - m0);
+// Tile number id: strips of `width` m tiles, in a strip n tile after n tile.  An XCD's blocks then
+// hold `width` tiles of x at a time and neighbouring rows of W, whose stores meet in whole lines of
+// the output.  Measured, us, width 1 / 2 / 8 / 32: 4096 x 65536 x 4096 628 / 611 / 630 / 671, x 512
+// 176 / 202 / 191 / 212, 4096 x 65537 x 1024 269 / 290 / 286 / 305; smaller tiles, 500 x 50001 x 1024
+// 40 / - / 34, 2000 x 20000 x 1024 53 / - / 49.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t mtiles, uint32_t ntiles,
+                                        uint32_t strip_width, uint32_t* mt, uint32_t* nt) {
+  const uint32_t strip = id / (strip_width * ntiles);
+  const uint32_t m0 = strip * strip_width, width = min(strip_width, mtiles - m0);
   const uint32_t in = id - m0 * ntiles;
   *nt = in / width;
   *mt = m0 + in - *nt * width;
@@ -146,8 +152,8 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t mtiles, uint32_t n
 // steps of all of them: those of the next tile are on their way while a tile is stored.
 //
 // 256 x 256 tiles keep the accumulators of a wavefront in 256 registers and read each fragment
-// from LDS for four products.  Left out one at a time at 4096 x 65536 x 4096 (633 us): loads to LDS
-// 457, stores of the output 533, LDS reads and loads and stores 315.
+// from LDS for four products.  Left out one at a time at 4096 x 65536 x 4096 (633 us with
+// strips of 8): loads to LDS 457, stores of the output 533, LDS reads and loads and stores 315.
 template <int TN, int TM, int WN, int WM, int STAGES, class T>
 __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     const uint8_t* __restrict__ xc, const uint32_t* __restrict__ xs, int64_t xpitch, int32_t m,
@@ -176,6 +182,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   const uint32_t end = min((blockIdx.x % kNumXcd + 1) * range, tiles);
   uint32_t tile = blockIdx.x % kNumXcd * range + blockIdx.x / kNumXcd;
   if (tile >= end) return;
+  const uint32_t strip_width = BM < 256 ? 8 : (steps > 16 ? 2 : 1);
 
   // The loads' own place in the stream of steps: number i of this wavefront brings rows
   // 16 * (i * W + wave) .. + 15 of the stage (W's rows, then x's); rows past the end repeat
@@ -194,7 +201,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   };
   auto load_tile = [&]() {
     uint32_t mt, nt;
-    tile_of(ltile, mtiles, ntiles, &mt, &nt);
+    tile_of(ltile, mtiles, ntiles, strip_width, &mt, &nt);
     const int64_t n0 = int64_t(nt) * BN;
     const int m0 = int(mt) * BM;
     wbase = w.codes + n0 * wrow;
@@ -335,11 +342,11 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
 #pragma unroll
   for (int i = 0; i < TN; ++i) a[1][i] = u4{0u, 0u, 0u, 0u};
 
-  // Each wavefront turns 32 rows of x and COLS of W at a time around in its own part of LDS (lane: row
-  // of x lane % 32, four consecutive rows of W per quarter of its registers), then stores rows of
-  // 128 bytes.
+  // Each wavefront turns 32 rows of x and 32 * TILES of W at a time around in its own part of LDS
+  // (lane: row of x lane % 32, four consecutive rows of W per quarter of its registers), then
+  // stores rows of 128 or 256 bytes.
   uint32_t mt, nt;
-  tile_of(tile, mtiles, ntiles, &mt, &nt);
+  tile_of(tile, mtiles, ntiles, strip_width, &mt, &nt);
   const int64_t n1 = int64_t(nt) * BN + wn * TN * 32;
   const int m1 = int(mt) * BM + wm * TM * 32;
   const int col = lane % PER_ROW * V;
@@ -539,7 +546,7 @@ void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, in
     const int64_t big = tiles(256, 256), mid = tiles(128, 128);
     const int64_t big_rounds = rounds(big, kNumCu);
     if (m > 512 && big_rounds >= 4 && big_rounds * 10 < rounds(mid, 2 * kNumCu) * 7)
-      launch_tile<4, 4, 2, 2, 4, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
+      launch_tile<4, 4, 2, 2, 3, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
     else if (m > 64 && mid >= kNumCu / 2)
       launch_tile<2, 2, 2, 2, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
     else if (tiles(128, 64) >= kNumCu)
