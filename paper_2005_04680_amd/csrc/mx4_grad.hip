@@ -336,11 +336,14 @@ GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
   if (m == 0 || n < 8) return p;
   // 256 rows of x per tile where the product is large; else 64 or 32, which leave more blocks and
   // fewer bytes of parts (200 x 50001 x 256: 64 22 us, 256 60).
+  // 256 columns, but 128 where such tiles, split to 4 steps each, leave compute units idle (100 x
+  // 5000 x 512: 256 12.6 us, 128 10.8; 64 x 50000 x 1024 22.4 and 22.4; 1 x 200003 x 1024 32 and 35).
   p.bk = k > 128 ? 256 : 128;
   p.bm = m > 32 ? (m > 64 && double(m) * double(n) * k > 5e10 ? 256 : 64) : 32;
-  p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
   p.mtiles = uint32_t((m + p.bm - 1) / p.bm);
   const int64_t steps = (n + kRows - 1) / kRows;
+  if (p.bm < 256 && steps / 4 * p.mtiles * ((k + 255) / 256) < kNumCu) p.bk = 128;
+  p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
   const int64_t tiles = int64_t(p.ktiles) * p.mtiles;
   // One block per compute unit, two where their LDS lets them share it.
   const int stage = p.bm * kYRow + kRows * (p.bk * 2 + 32);
