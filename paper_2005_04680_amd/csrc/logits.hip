@@ -12,8 +12,10 @@
 // element is read by one thread, so that `out` may be `logits`.
 //
 // 256 x 131072 BF16 with up to 4096 seen tokens, 300 biases and masks: 46 us (20 us without
-// lists and masks, 6.6 TB/s; 33 us with the seen tokens alone): bound by the lists, which every slice of
-// a row walks.
+// lists and masks, 6.6 TB/s; 33 us with the seen tokens alone): bound by the vector instructions of the
+// lists' walk, which every slice repeats, and of the touched tokens (69% of the cycles), and by the
+// chain.  Blocks that keep the lists in registers over several slices were slower (64 us: fewer of
+// them share a unit), and so were biases added in the stream (47 us; 5000 of them 77 us, 57 here).
 //
 // Rows with more than kListed biases take them in a pass of their own first, with the words as the
 // places of the tokens' last biases.

@@ -168,6 +168,45 @@ def test_pooled_forward(T, rows, dim, batch, longest, pooling, out):
     assert not y.cpu().view(torch.int16 if out == "bf16" else torch.int32).numpy()[empty].any()
 
 
+@pytest.mark.parametrize("pooling", ["sum", "mean", "weighted"])
+def test_pooled_forward_of_every_scale_and_code(pooling):
+    # Row r: all codes twice, scale byte r.  A bag of one row is the row (a sum of one term).
+    t = pk.Mx4Table.empty(256, 32, torch.device(DEV))
+    code = np.tile(np.arange(16), 2)
+    t.codes[:] = torch.from_numpy((code[::2] | code[1::2] << 4).astype(np.uint8)).to(DEV)
+    t.scales.zero_()
+    t.scales[:, 0] = torch.arange(256, device=DEV).to(torch.uint8)
+    want = torch.empty(256, 32, device=DEV)
+    pk.check(pk.embbag_mx4_dequantize(t, want))
+    y = torch.empty(1, 256, 32, device=DEV)
+    idx = torch.arange(256, dtype=torch.int32, device=DEV)
+    o = torch.arange(257, dtype=torch.int32, device=DEV)
+    pk.check(pk.embbag_mx4_forward(
+        pk.Mx4Tables([t]), 256, idx, o, y,
+        torch.ones(256, device=DEV) if pooling == "weighted" else None,
+        pk.EMBBAG_POOL_MEAN if pooling == "mean" else pk.EMBBAG_POOL_SUM))
+    assert torch.equal(torch.isnan(y[0]), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(y[0]), torch.nan_to_num(want))
+
+
+@pytest.mark.parametrize("dim", [4, 32, 36, 256, 1024])
+def test_pooled_forward_of_lists_of_any_length_in_one_wavefront(dim):
+    # Lengths next to each other from none to long: the products of all bags of a wavefront go on
+    # until its longest list ends.
+    lengths = np.array([0, 1, 2, 3, 700, 0, 5, 8, 9, 16, 17, 33, 0, 64, 1, 129] * 5, np.int64)
+    o = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    idx = np.random.default_rng(dim).integers(0, 500, o[-1]).astype(np.int32)
+    t, v = random_table(500, dim, dim)
+    want, mag = ref.pooled([v], lengths.size, idx, o)
+    y = torch.full((1, lengths.size, dim), float("nan"), device=DEV)
+    st = status()
+    pk.check(pk.embbag_mx4_forward(pk.Mx4Tables([t]), lengths.size, torch.from_numpy(idx).to(DEV),
+                                   torch.from_numpy(o).to(DEV), y, d_status=st))
+    pk.check(pk.embbag_status_read(st))
+    close(y, want, (700 + 2) * U * mag * 1.01)
+    assert not y[0].cpu().view(torch.int32).numpy()[lengths == 0].any()
+
+
 def test_pooled_forward_reports_bad_lists():
     t, _ = random_table(10, 32, 1)
     tb = pk.Mx4Tables([t, t])
