@@ -334,15 +334,18 @@ struct GradPlan {
 GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
   GradPlan p = {};
   if (m == 0 || n < 8) return p;
-  // 256 rows of x per tile where the product is large; else 64 or 32, which leave more blocks and
-  // fewer bytes of parts (200 x 50001 x 256: 64 22 us, 256 60).
+  // 256 or 128 rows of x per tile where the product is large, which read W and its LDS tile less often;
+  // else 64 or 32, which leave more blocks and fewer bytes of parts.  Measured, us, 64 / 128 / 256: 1000
+  // x 10007 x 300 26 / 27 / 32; 4000 x 10000 x 256 42 / 38 / 48; 300 x 100000 x 768 80 / 72 / 80; 2000 x
+  // 20000 x 1024 123 / 95 / 91; 4096 x 32768 x 512 223 / 160 / 145.
   // 256 columns, but 128 where such tiles, split to 4 steps each, leave compute units idle (100 x
   // 5000 x 512: 256 12.6 us, 128 10.8; 64 x 50000 x 1024 22.4 and 22.4; 1 x 200003 x 1024 32 and 35).
   p.bk = k > 128 ? 256 : 128;
-  p.bm = m > 32 ? (m > 64 && double(m) * double(n) * k > 5e10 ? 256 : 64) : 32;
+  const double products = double(m) * double(n) * k;
+  p.bm = m <= 32 ? 32 : m <= 64 || products <= 7e9 ? 64 : products <= 3e10 ? 128 : 256;
   p.mtiles = uint32_t((m + p.bm - 1) / p.bm);
   const int64_t steps = (n + kRows - 1) / kRows;
-  if (p.bm < 256 && steps / 4 * p.mtiles * ((k + 255) / 256) < kNumCu) p.bk = 128;
+  if (p.bm < 128 && steps / 4 * p.mtiles * ((k + 255) / 256) < kNumCu) p.bk = 128;
   p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
   const int64_t tiles = int64_t(p.ktiles) * p.mtiles;
   // One block per compute unit, two where their LDS lets them share it.
@@ -376,6 +379,8 @@ void launch_plan(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, cons
   if (p.bk == 256) {
     if (p.bm == 256)
       launch_tile<4, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    else if (p.bm == 128)
+      launch_tile<2, 4, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
     else if (p.bm == 64)
       launch_tile<2, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
     else
@@ -383,6 +388,8 @@ void launch_plan(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, cons
   } else {
     if (p.bm == 256)
       launch_tile<2, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    else if (p.bm == 128)
+      launch_tile<1, 4, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
     else if (p.bm == 64)
       launch_tile<1, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
     else

@@ -310,6 +310,44 @@ def test_scores_of_no_rows():
     pk.check(pk.embbag_mx4_matmul_grad(out, t, x, ws))
 
 
+def coded_table(rows, dim, seed):
+    """A large table of random codes and scales around 1, E a multiple of 4."""
+    rng = np.random.default_rng(seed)
+    nb = (dim + 31) // 32
+    pair = rng.integers(0, 256, (rows, nb * 16), np.uint8)
+    pair[:, dim // 2:] = 0
+    scales = np.zeros((rows, (nb + 3) // 4 * 4), np.uint8)
+    scales[:, :nb] = rng.integers(124, 131, (rows, nb), np.uint8)
+    value = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+    value = np.concatenate([value, -value])
+    both = value[np.arange(256)[:, None] >> np.array([0, 4]) & 15]
+    w = both[pair].reshape(rows, nb, 32) * np.exp2(scales[:, :nb, None] - 127.0)
+    t = pk.Mx4Table(torch.from_numpy(pair).to(DEV), torch.from_numpy(scales).to(DEV), dim)
+    return t, w.reshape(rows, nb * 32)[:, :dim]
+
+
+def some_rows(m):
+    """The first and last rows of tiles of 64, 128 and 256 of m rows, and some between."""
+    at = {0, 1, 31, 32, 63, 64, 127, 128, 255, 256, 300, m // 2, m - 2, m - 1}
+    return sorted(r for r in at if r < m)
+
+
+@pytest.mark.parametrize("m,n,k,out_type", [(600, 5000, 260, "bf16"), (1100, 20003, 1000, "f32"),
+                                            (2048, 20000, 512, "bf16")])
+def test_scores_of_many_rows(m, n, k, out_type):
+    t, w = coded_table(n, k, n)
+    x = source(m, k, m, "bf16", special=False)
+    x = (x.double() / x.double().abs().max(1, keepdim=True).values.clamp(min=1e-30)).to(x.dtype)
+    out = torch.empty(m, n, dtype=DT[out_type], device=DEV)
+    ws = torch.empty(pk.embbag_mx4_matmul_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    pk.check(pk.embbag_mx4_matmul(x.to(DEV), t, out, ws))
+    rows = some_rows(m)
+    q = ref.dequantize(*ref.quantize(x[rows].double().numpy()), k)
+    want = q @ w.T
+    tol = 2 * (k + 8) * U * (np.abs(q) @ np.abs(w).T)
+    close(out[rows], want, tol + rounding(np.abs(want) + tol, out_type), f"{m}x{n}x{k}")
+
+
 # ---- gradient -----------------------------------------------------------------
 def grad_check(m, n, k, y_type, x_type, seed, pad=0):
     t, w = random_table(n, k, seed)
@@ -345,6 +383,24 @@ def test_gradient_ends_of_the_rows(m, n, y_type):
 def test_gradient_with_strides(m, n, k, pad):
     grad_check(m, n, k, "bf16", "bf16", 7, pad)
     grad_check(m, n, k, "f32", "f32", 8, pad)
+
+
+@pytest.mark.parametrize("m,n,k,y_type,x_type", [
+    (700, 16390, 700, "bf16", "bf16"), (900, 8195, 1020, "f32", "f32"), (1500, 50001, 100, "bf16", "f32"),
+    (4300, 7001, 1004, "bf16", "f32"), (2100, 15003, 1000, "f32", "bf16"),
+    (4000, 70000, 128, "bf16", "bf16")])
+def test_gradient_of_many_rows(m, n, k, y_type, x_type):
+    t, w = coded_table(n, k, n)
+    dy = torch.randn(m, n, generator=torch.Generator().manual_seed(m)).to(DT[y_type])
+    dx = torch.empty(m, k, dtype=DT[x_type], device=DEV)
+    ws = torch.empty(pk.embbag_mx4_matmul_grad_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    ws.fill_(0xFF)
+    pk.check(pk.embbag_mx4_matmul_grad(dy.to(DEV), t, dx, ws))
+    rows = some_rows(m)
+    d = dy[rows].double().numpy()
+    want = d @ w
+    tol = 2 * (n + 8) * U * (np.abs(d) @ np.abs(w))
+    close(dx[rows], want, tol + rounding(np.abs(want) + tol, x_type), f"{m}x{n}x{k}")
 
 
 @pytest.mark.parametrize("y_type", ["f32", "bf16"])
