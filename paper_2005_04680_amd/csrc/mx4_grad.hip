@@ -17,8 +17,9 @@
 // the products and the LDS traffic between them; without the interleaving of `part` 409 us.
 // 200 x 50001 x 256: 22 us, bound by its chain of steps.
 //
-// An FP32 dy is the sum of three BF16 terms of 8 bits each, by truncation; the steps go through
-// the terms one after the other.
+// An FP32 dy is the sum of three BF16 terms of 8 bits each, by truncation: three tiles of dy for one of
+// W, whose fragments meet all three (1024 x 20000 x 1024 152 us, with a step of its own for each term 317;
+// 64 x 100000 x 256 26, 43).
 #include "head.hpp"
 
 namespace embbag {
@@ -34,23 +35,22 @@ constexpr int kYRow = kRows * 2;            // bytes of a row of dy's tile
 
 template <int BK>
 constexpr int kWRow = BK * 2 + 32;          // bytes of a row of W's tile
-template <int BK, int BM>
-constexpr int kStage = BM * kYRow + kRows * kWRow<BK>;
+template <int BK, int BM, int TERMS>
+constexpr int kStage = TERMS * BM * kYRow + kRows * kWRow<BK>;
 
-// Term t of x (t = 0, 1, 2): its 8 highest bits, the next 8, the rest, as a BF16 pattern.
-// An infinity or a NaN is its own first term and leaves nothing.
-__device__ __forceinline__ uint32_t bf16_term(float x, int t) {
+// x as the sum of three terms: its 8 highest bits, the next 8, the rest, as BF16 patterns in the upper
+// halves.  An infinity or a NaN is its own first term and leaves nothing.
+__device__ __forceinline__ void bf16_terms(float x, uint32_t (&t)[3]) {
   uint32_t u = __float_as_uint(x);
   const bool special = (u & 0x7F800000u) == 0x7F800000u;
   if (special) u |= (u & 0x007FFFFFu) != 0u ? 0x00400000u : 0u;
-  for (int i = 0; i < t; ++i) {
-    const float rest = __uint_as_float(u) - __uint_as_float(u & 0xFFFF0000u);
-    u = special ? 0u : __float_as_uint(rest);
-  }
-  return u >> 16;
+  t[0] = u & 0xFFFF0000u;
+  const float rest = special ? 0.f : __uint_as_float(u) - __uint_as_float(t[0]);
+  t[1] = __float_as_uint(rest) & 0xFFFF0000u;
+  t[2] = __float_as_uint(rest - __uint_as_float(t[1])) & 0xFFFF0000u;
 }
 
-// 8 elements of a row of dy on their way to LDS, and as BF16 (`term` of FP32 ones).
+// 8 elements of a row of dy on their way to LDS, and as BF16 (three terms of FP32 ones).
 struct Raw16 {
   u4 v;
 };
@@ -63,12 +63,17 @@ __device__ __forceinline__ Raw16 load8(const __bf16* p) {
 __device__ __forceinline__ Raw32 load8(const float* p) {
   return {*reinterpret_cast<const f4_el*>(p), *reinterpret_cast<const f4_el*>(p + 4)};
 }
-__device__ __forceinline__ u4 to_bf16(const Raw16& r, int) { return r.v; }
-__device__ __forceinline__ u4 to_bf16(const Raw32& r, int term) {
-  return u4{bf16_term(r.a.x, term) | (bf16_term(r.a.y, term) << 16),
-            bf16_term(r.a.z, term) | (bf16_term(r.a.w, term) << 16),
-            bf16_term(r.b.x, term) | (bf16_term(r.b.y, term) << 16),
-            bf16_term(r.b.z, term) | (bf16_term(r.b.w, term) << 16)};
+__device__ __forceinline__ void to_bf16(const Raw16& r, u4 (&t)[1]) { t[0] = r.v; }
+__device__ __forceinline__ void to_bf16(const Raw32& r, u4 (&t)[3]) {
+  const float x[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t lo[3], hi[3];
+    bf16_terms(x[2 * i], lo);
+    bf16_terms(x[2 * i + 1], hi);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) t[q][i] = lo[q] >> 16 | hi[q];
+  }
 }
 // A word of codes as 8 BF16 values.
 __device__ __forceinline__ u4 bf16_values8(uint32_t c, float scale) {
@@ -92,11 +97,11 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
                                                        int64_t part_stride) {
   static_assert(WK * WM == kWavesPerBlock, "four wavefronts");
   constexpr int BK = 32 * TK * WK, BM = 32 * TM * WM;
-  constexpr int STAGE = kStage<BK, BM>;
   constexpr int YL = BM / 32;              // loads of dy per thread
   constexpr int WL = kRows * BK / 32 / kBlock;  // blocks of W per thread
   static_assert(WL >= 1 && YL >= 1, "a load of each per thread");
-  constexpr bool kTerms = sizeof(TY) == 4;
+  constexpr int TERMS = sizeof(TY) == 4 ? 3 : 1;
+  constexpr int STAGE = kStage<BK, BM, TERMS>;
   extern __shared__ __align__(16) uint8_t lds[];
 
   const int lane = lane_id(), wave = wave_id();
@@ -108,7 +113,6 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   const int64_t n0 = int64_t(z) * per * kRows;
   const int rows = int(min(w.rows - n0, int64_t(per) * kRows));  // of W, in this block (>= 1)
   const int steps = (rows + kRows - 1) / kRows;
-  const int total = kTerms ? steps * 3 : steps;
   const int nb = mx4_blocks(w.dim), sb = mx4_scale_bytes(w.dim);
 
   // dy: load i of this thread is 8 columns (8 * yc ..) of row i * 32 + threadIdx.x / 8.
@@ -124,14 +128,13 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   u4 wv[WL];
   uint32_t ws[WL];
   int64_t wrow = 0;
-  int ycol = 0, term = 0;
+  int ycol = 0;
   bool win = false;
 
   // Places of step s's loads.
   const int last = rows - 8;  // of the last 8 rows, the first (in the split before, if rows < 8)
   auto place = [&](int s) {
-    const int step = kTerms ? s / 3 : s;
-    const int r0 = step * kRows;
+    const int r0 = s * kRows;
     ycol = min(r0 + yc * 8, last);
     const int c = r0 + wr / 8 * 8;  // the first row of wr's 8
     const int r = min(c, last) + wr % 8;
@@ -146,11 +149,15 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   };
   bool in = false;  // whether the loads that are stored next were of a row to be added
   auto store_y = [&](uint8_t* st, int i) {
-    *reinterpret_cast<u4*>(st + (i * 32 + yr) * kYRow + (yc ^ (yr & 7)) * 16) = to_bf16(yv[i], term);
+    u4 t[TERMS];
+    to_bf16(yv[i], t);
+#pragma unroll
+    for (int q = 0; q < TERMS; ++q)
+      *reinterpret_cast<u4*>(st + (q * BM + i * 32 + yr) * kYRow + (yc ^ (yr & 7)) * 16) = t[q];
   };
   auto store_w = [&](uint8_t* st, int i) {
     const float s = mx4_scale(in ? ws[i] : 0u);
-    u4* p = reinterpret_cast<u4*>(st + BM * kYRow + wr * kWRow<BK> + (wb + PER * i) * 64);
+    u4* p = reinterpret_cast<u4*>(st + TERMS * BM * kYRow + wr * kWRow<BK> + (wb + PER * i) * 64);
     p[0] = bf16_values8(in ? wv[i].x : 0u, s);
     p[1] = bf16_values8(in ? wv[i].y : 0u, s);
     p[2] = bf16_values8(in ? wv[i].z : 0u, s);
@@ -169,35 +176,36 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   // 8 * (l / 32).  W's come from two transposing reads: 16 lanes bring 4 rows of 16 columns
   // and each leaves with its column.
   const int yfrag = (wm * TM * 32 + row) * kYRow;
-  const int wfrag = BM * kYRow + (half * 8 + (lane % 16) / 4) * kWRow<BK> +
+  const int wfrag = TERMS * BM * kYRow + (half * 8 + (lane % 16) / 4) * kWRow<BK> +
                     (wk * TK * 32 + (lane / 16 % 2) * 16 + (lane % 4) * 4) * 2;
-  u4 a[2][TK] = {}, b[2][TM] = {};
+  constexpr int YF = TERMS * TM;  // fragments of dy
+  u4 a[2][TK] = {}, b[2][YF] = {};
   auto fetch = [&](const uint8_t* st, int p, int i) {
-    if (i < TM) {
-      b[p & 1][i] = *reinterpret_cast<const u4*>(st + yfrag + i * 32 * kYRow +
+    if (i < YF) {
+      b[p & 1][i] = *reinterpret_cast<const u4*>(st + yfrag + (i / TM * BM + i % TM * 32) * kYRow +
                                                  ((p * 2 + half) ^ (row & 7)) * 16);
     } else {
-      const uint8_t* q = st + wfrag + p * 16 * kWRow<BK> + (i - TM) * 64;
+      const uint8_t* q = st + wfrag + p * 16 * kWRow<BK> + (i - YF) * 64;
       typedef __attribute__((address_space(3))) s4v* lds4;
       const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)q);
       const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(q + 4 * kWRow<BK>));
       const u2 l2 = __builtin_bit_cast(u2, lo), h2 = __builtin_bit_cast(u2, hi);
-      a[p & 1][i - TM] = u4{l2.x, l2.y, h2.x, h2.y};
+      a[p & 1][i - YF] = u4{l2.x, l2.y, h2.x, h2.y};
     }
   };
   // The products of part p, and between their rows: the reads of the next part's fragments
   // (part `next` of `cur`), and in the first three parts of a step the stores of the next
   // stage, each followed by the load that takes its registers.
   auto part = [&](const uint8_t* cur, uint8_t* nxt, int p, int next, int turn) {
-    constexpr int N = TK + TM, READS = TK > 1 ? TK - 1 : 1;
+    constexpr int N = TK + YF, READS = TK > 1 ? TK - 1 : 1;
     constexpr int MOVES = YL + WL, SLOTS = 3 * TK;
 #pragma unroll
     for (int i = 0; i < TK; ++i) {
 #pragma unroll
-      for (int j = 0; j < TM; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf8, a[p & 1][i]), __builtin_bit_cast(bf8, b[p & 1][j]), acc[i][j], 0,
-            0, 0);
+      for (int j = 0; j < YF; ++j)
+        acc[i][j % TM] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf8, a[p & 1][i]), __builtin_bit_cast(bf8, b[p & 1][j]),
+            acc[i][j % TM], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < N; ++r)
@@ -226,19 +234,18 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
 #pragma unroll
   for (int i = 0; i < WL; ++i) store_w(lds, i);
   // (Steps past the last one load it again and are not used.)
-  place(min(1, total - 1));
+  place(min(1, steps - 1));
   in = win;
 #pragma unroll
   for (int i = 0; i < YL; ++i) load_y(i);
 #pragma unroll
   for (int i = 0; i < WL; ++i) load_w(i);
-  for (int s = 0; s < total; ++s) {
+  for (int s = 0; s < steps; ++s) {
     uint8_t* cur = lds + (s & 1) * STAGE;
     uint8_t* nxt = lds + (~s & 1) * STAGE;
     // The stage is in LDS, and every wavefront holds the last fragments of the other one.
     __syncthreads();
-    term = kTerms ? (s + 1) % 3 : 0;
-    place(min(s + 2, total - 1));
+    place(min(s + 2, steps - 1));
     part(cur, nxt, 3, 0, 0);
     part(cur, nxt, 0, 1, 1);
     part(cur, nxt, 1, 2, 2);
@@ -331,7 +338,7 @@ struct GradPlan {
   uint32_t ktiles, mtiles, splits;
   int32_t per;  // steps per split
 };
-GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
+GradPlan grad_plan(int32_t m, int64_t n, int32_t k, bool y_bf16) {
   GradPlan p = {};
   if (m == 0 || n < 8) return p;
   // 256 or 128 rows of x per tile where the product is large, which read W and its LDS tile less often;
@@ -341,15 +348,16 @@ GradPlan grad_plan(int32_t m, int64_t n, int32_t k) {
   // 256 columns, but 128 where such tiles, split to 4 steps each, leave compute units idle (100 x
   // 5000 x 512: 256 12.6 us, 128 10.8; 64 x 50000 x 1024 22.4 and 22.4; 1 x 200003 x 1024 32 and 35).
   p.bk = k > 128 ? 256 : 128;
+  // An FP32 dy has three tiles of its rows in LDS, and products, for each: 64 rows.
   const double products = double(m) * double(n) * k;
-  p.bm = m <= 32 ? 32 : m <= 64 || products <= 7e9 ? 64 : products <= 3e10 ? 128 : 256;
+  p.bm = m <= 32 ? 32 : m <= 64 || products <= 7e9 || !y_bf16 ? 64 : products <= 3e10 ? 128 : 256;
   p.mtiles = uint32_t((m + p.bm - 1) / p.bm);
   const int64_t steps = (n + kRows - 1) / kRows;
   if (p.bm < 128 && steps / 4 * p.mtiles * ((k + 255) / 256) < kNumCu) p.bk = 128;
   p.ktiles = uint32_t((k + p.bk - 1) / p.bk);
   const int64_t tiles = int64_t(p.ktiles) * p.mtiles;
   // One block per compute unit, two where their LDS lets them share it.
-  const int stage = p.bm * kYRow + kRows * (p.bk * 2 + 32);
+  const int stage = (y_bf16 ? 1 : 3) * p.bm * kYRow + kRows * (p.bk * 2 + 32);
   int64_t splits = kNumCu * (4 * stage <= 160 * 1024 ? 2 : 1) / tiles;
   if (splits > steps / 4) splits = steps / 4;
   if (splits < 1) splits = 1;
@@ -364,7 +372,7 @@ template <int TK, int TM, int WK, int WM, class TY, class TX>
 void launch_tile(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, const Mx4View& w,
                  TX* dx, int64_t ldx, int64_t part_stride, hipStream_t st) {
   auto kernel = grad_tile<TK, TM, WK, WM, TY, TX>;
-  constexpr int lds = 2 * kStage<32 * TK * WK, 32 * TM * WM>;
+  constexpr int lds = 2 * kStage<32 * TK * WK, 32 * TM * WM, sizeof(TY) == 4 ? 3 : 1>;
   if (lds > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -376,25 +384,22 @@ void launch_tile(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, cons
 template <class TY, class TX>
 void launch_plan(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, const Mx4View& w,
                  TX* dx, int64_t ldx, int64_t ps, hipStream_t st) {
-  if (p.bk == 256) {
-    if (p.bm == 256)
-      launch_tile<4, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
-    else if (p.bm == 128)
-      launch_tile<2, 4, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
-    else if (p.bm == 64)
-      launch_tile<2, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
-    else
-      launch_tile<2, 1, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
-  } else {
-    if (p.bm == 256)
-      launch_tile<2, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
-    else if (p.bm == 128)
-      launch_tile<1, 4, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
-    else if (p.bm == 64)
-      launch_tile<1, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
-    else
-      launch_tile<1, 1, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+  if constexpr (sizeof(TY) == 2) {
+    if (p.bm == 256 && p.bk == 256)
+      return launch_tile<4, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    if (p.bm == 256) return launch_tile<2, 4, 2, 2, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    if (p.bm == 128 && p.bk == 256)
+      return launch_tile<2, 4, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+    if (p.bm == 128) return launch_tile<1, 4, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
   }
+  if (p.bm == 64 && p.bk == 256)
+    launch_tile<2, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+  else if (p.bm == 64)
+    launch_tile<1, 2, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+  else if (p.bk == 256)
+    launch_tile<2, 1, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
+  else
+    launch_tile<1, 1, 4, 1, TY>(p, dy, ldy, m, w, dx, ldx, ps, st);
 }
 
 template <class TX>
@@ -435,15 +440,15 @@ void launch_grad(const GradPlan& p, const void* dy, bool dy_bf16, int64_t ldy, i
 }  // namespace
 
 size_t mx4_matmul_grad_workspace(int32_t m, int64_t n, int32_t k) {
-  const GradPlan p = grad_plan(m, n, k);
-  return p.splits > 1 ? (size_t(p.splits) * size_t(m) * size_t(k) * 4 + 255) / 256 * 256 : 0;
+  const uint32_t splits = max(grad_plan(m, n, k, true).splits, grad_plan(m, n, k, false).splits);
+  return splits > 1 ? (size_t(splits) * size_t(m) * size_t(k) * 4 + 255) / 256 * 256 : 0;
 }
 
 hipError_t launch_mx4_matmul_grad(const void* dy, bool dy_bf16, int64_t dy_stride, int32_t m,
                                   const Mx4View& w, void* dx, bool dx_bf16, int64_t dx_stride,
                                   char* ws, hipStream_t st) {
   if (m == 0) return hipSuccess;
-  const GradPlan p = grad_plan(m, w.rows, w.dim);
+  const GradPlan p = grad_plan(m, w.rows, w.dim, dy_bf16);
   float* parts = reinterpret_cast<float*>(ws);
   if (dx_bf16)
     launch_grad(p, dy, dy_bf16, dy_stride, m, w, static_cast<__bf16*>(dx), dx_stride, parts, st);
