@@ -266,8 +266,8 @@ void dispatch(int lpr, bool four, dim3 grid, hipStream_t st, const TableDesc& d,
     if constexpr (MODE == kPoolWeighted)                                                         \
       hipLaunchKernelGGL((mx4_weighted_kernel<L, T>), grid, dim3(kBlock), 0, st, d, I, O,   \
                          NS, B, inv_b, split, bags, Y, status, A);                               \
-    else if (four && L > 4)                                                                      \
-      hipLaunchKernelGGL((mx4_sum_kernel<L / 2, (L > 4 ? 4 : 2), MODE, T>), grid, dim3(kBlock), 0, \
+    else if (four)                                                                               \
+      hipLaunchKernelGGL((mx4_sum_kernel<L / 2, 4, MODE, T>), grid, dim3(kBlock), 0, \
                          st, d, I, O, NS, B, inv_b, split, bags, Y, status);                     \
     else                                                                                         \
       hipLaunchKernelGGL((mx4_sum_kernel<L / 2, 2, MODE, T>), grid, dim3(kBlock), 0, st, d, I,   \
@@ -310,18 +310,21 @@ hipError_t launch_mx4_forward(const TableDesc& d, int32_t B, const int32_t* I, c
   while (lpr < mx4_blocks(d.dim) * 2) lpr *= 2;
   const int groups = kWave / lpr;
   // Groups that share a bag: two for `list` look-ups or more each, four for twice that and so on, while
-  // the wavefronts do not fill the chip's slots.  Measured, us, shared / not: 64 bags of up to 64 in each
-  // of 8 tables, E = 64 8.9 / 10.7; 9000 of 40, E = 100 10.0 / 10.8; weighted ones 12.4 / 15.3; 33K of 10,
-  // E = 16, weighted, shared by four 9.6, not 8.1.
+  // the wavefronts do not fill the chip's slots.  Lists of 8, but of 16 in the sums, which take two
+  // look-ups at a time, once there are two wavefronts for each vector unit.  Measured, us, 8 / 16: 64
+  // ragged bags of 32 in each of 8 tables, E = 64 5.4 / 6.2; 9000 of 40, E = 100 11.7 / 9.5; 8 x 2048
+  // ragged of 32, E = 128 11.5 / 10.4.
   const int64_t avg = NS / bags;
-  const int64_t list = pool.mode == kPoolWeighted ? 8 : 16;
   int split = 1;
-  while (split < groups && avg > split * list && bags * split * lpr < int64_t(kNumCu) * 32 * kWave)
+  auto few = [&]() { return bags * split * lpr < int64_t(kNumCu) * 8 * kWave; };
+  auto list = [&]() { return pool.mode == kPoolWeighted || few() ? 8 : 16; };
+  while (split < groups && avg > split * list() && bags * split * lpr < int64_t(kNumCu) * 32 * kWave)
     split *= 2;
   // Rows in flight per lane of the sums: four, two where lists are short or rows narrow (which leaves
-  // more wavefronts on a unit).  Measured, us, four / two: 8 tables, 8192 bags of 100, E = 256 123.5 /
-  // 127; 26 tables, 8192 of 1, E = 128 30.5 / 27.8; 8192 of 100, E = 64 19.8 / 18.5.
-  const bool four = lpr > 4 && avg > 4 * split;
+  // more wavefronts on a unit) unless there are few.  Measured, us, four / two: 8 tables, 8192 bags of
+  // 100, E = 256 123.5 / 127; 26 tables, 8192 of 1, E = 128 30.5 / 27.8; 8192 of 100 among 18M rows, E =
+  // 64 19.8 / 18.5; 8 x 64 ragged of 32, E = 64 5.4 / 6.0.
+  const bool four = avg > 4 * split && (lpr > 4 || few());
   const int64_t per_block = int64_t(kWavesPerBlock) * (groups / split);
   const dim3 grid(unsigned((bags + per_block - 1) / per_block));
   if (y_bf16)
