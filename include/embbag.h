@@ -343,7 +343,11 @@ int embbag_baseline_touch_rows_split(int32_t batch, int64_t num_indices,
  * model's scores (next item, next token): 4-bit storage of its rows, bags and
  * scores from that storage, what may be answered, and training against a
  * teacher.  Conventions (streams, ownership, argument and data errors) are
- * those of the header comment. */
+ * those of the header comment.
+ * Limits, beyond those below: tables and matrices of at most 2^31 - 1 rows, x, dy
+ * of less than 2^23 rows, m * n and rows * vocab of at most 2^40.  A
+ * *_workspace_bytes is 0 for sizes out of range, and where a call of valid sizes
+ * needs none (a null workspace is right then). */
 
 /* Element types of the buffers that take more than one. */
 #define EMBBAG_F32 0
@@ -479,8 +483,9 @@ int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStr
  * row strides in elements and no alignment beyond the elements'; grad may be
  * `logits` itself with the same stride, and must not overlap it otherwise.
  * ids: device int32 [rows][top] (negative: no entry), teacher: [rows][top] of
- * teacher_type, 1 <= top <= 1024, 1e-6 <= temperature <= 1e6.  loss: FP32 [rows].  An id >= vocab is a data
- * error; the row's outputs are then unspecified.  Sums are FP32. */
+ * teacher_type, 1 <= top <= 1024, 1e-6 <= temperature <= 1e6.  loss: FP32 [rows].
+ * An id >= vocab is a data error; the row's outputs are then unspecified.  Sums
+ * are FP32. */
 typedef struct {
   int32_t rows;
   int32_t vocab;
