@@ -11,6 +11,7 @@ and gradient against a teacher's top logits).
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 from . import (EMBBAG_POOL_SUM, _check_bags, _check_numel, _dt, _I32, _need, _ptr, _status_ptr,
                _stream, _U32, lib)
@@ -45,12 +46,31 @@ class _Distill(C.Structure):
                 ("grad", C.c_void_p), ("grad_stride", C.c_int64)]
 
 
+# A call's arguments as the bytes of its structure (0.2 us; a ctypes object of 22 fields 1.0).
+_CODES = {C.c_int32: "i", C.c_int64: "q", C.c_void_p: "P", C.c_float: "f"}
+
+
+def _packer(cls):
+    fmt = struct.Struct("@" + "".join(_CODES[t] for _, t in cls._fields_))
+    assert fmt.size == C.sizeof(cls), cls
+
+    def pack(*fields):
+        try:
+            return fmt.pack(*fields)
+        except struct.error as e:
+            raise ValueError(f"an argument is out of range: {e}") from None
+    return pack
+
+
+_pack_logits, _pack_distill = _packer(_Logits), _packer(_Distill)
+
 _ready = None
 
 
 def _lib():
     global _ready
     if _ready is None:
+        _load_types()
         L = lib()
         p, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
         L.embbag_mx4_quantize.argtypes = [p, i32, i64, i64, i32, p, i64, p, p, p, p]
@@ -113,10 +133,10 @@ def _matrix(t, cols, name):
 
 
 def _vector(t, n, name, dtype):
-    """Pointer of a contiguous GPU tensor of n elements of `dtype` (None: null; n
+    """Pointer of a contiguous GPU tensor of n elements of `dtype` (None: 0; n
     None: any number)."""
     if t is None:
-        return None
+        return 0
     if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (n is None or t.numel() == n):
         return t.data_ptr()
     if n is not None:
@@ -125,13 +145,26 @@ def _vector(t, n, name, dtype):
 
 
 def _list(entries, offsets, rows, name):
-    """Pointers and length of a list per row (None, None: none)."""
+    """Pointers and length of a list per row (None: 0)."""
     if offsets is None:
-        _need(entries is None, f"{name}: entries without offsets")
-        return None, None, 0
-    _need(entries is not None, f"{name}: offsets without entries")
+        if entries is not None:
+            raise ValueError(f"{name}: entries without offsets")
+        return 0, 0, 0
+    if entries is None:
+        raise ValueError(f"{name}: offsets without entries")
     return (_vector(entries, None, name, _I32_T),
-            _vector(offsets, rows + 1, f"{name} offsets", _I32_T), entries.numel())
+            _vector(offsets, rows + 1, name + " offsets", _I32_T), entries.numel())
+
+
+def _status(t):
+    if t is not None and t.dtype is _I32_T and t.is_cuda and t.is_contiguous() and t.numel() >= 1:
+        return t.data_ptr()
+    return _status_ptr(t)
+
+
+def _check_rows(t, rows, name):
+    if t.shape[0] != rows:
+        raise ValueError(f"{name}: {t.shape[0]} rows, expected {rows}")
 
 
 def _ws(workspace):
@@ -207,19 +240,19 @@ def embbag_mx4_quantize(src, table, row_ids=None, d_status=None, stream=None) ->
     """Rows of ``src`` ([M, dim] FP32 or BF16) into ``table``: all of them, or those
     that the int32 tensor ``row_ids`` names."""
     p, ty, ld = _matrix(src, table.dim, "src")
-    _need(src.shape[0] == table.rows, f"src: {src.shape[0]} rows, expected {table.rows}")
+    _check_rows(src, table.rows, "src")
     ids = _ptr(row_ids, _dt(*_I32), "row_ids")
     n = 0 if row_ids is None else row_ids.numel()
     if row_ids is not None and n == 0:
         return 0
     return _lib().embbag_mx4_quantize(p, ty, ld, table.rows, table.dim, ids, n, table.codes_ptr,
-                                      table.scales_ptr, _status_ptr(d_status), _stream(stream))
+                                      table.scales_ptr, _status(d_status), _stream(stream))
 
 
 def embbag_mx4_dequantize(table, dst, stream=None) -> int:
     """All rows of ``table`` as values into ``dst`` ([M, dim] FP32 or BF16)."""
     p, ty, ld = _matrix(dst, table.dim, "dst")
-    _need(dst.shape[0] == table.rows, f"dst: {dst.shape[0]} rows, expected {table.rows}")
+    _check_rows(dst, table.rows, "dst")
     return _lib().embbag_mx4_dequantize(table.codes_ptr, table.scales_ptr, table.rows, table.dim, p,
                                         ty, ld, _stream(stream))
 
@@ -236,7 +269,7 @@ def embbag_mx4_forward(tables, batch, indices, offsets, pooled_out, per_sample_w
         C.byref(tables.struct), int(batch), _ptr(indices, _dt(*_I32), "indices"),
         _ptr(offsets, _dt(*_I32), "offsets"), indices.numel(),
         _ptr(per_sample_weights, _dt("float32"), "per_sample_weights"), int(pooling), out,
-        EMBBAG_BF16 if pooled_out.element_size() == 2 else EMBBAG_F32, _status_ptr(d_status),
+        EMBBAG_BF16 if pooled_out.element_size() == 2 else EMBBAG_F32, _status(d_status),
         _stream(stream))
 
 
@@ -249,7 +282,7 @@ def embbag_mx4_matmul(x, table, out, workspace, stream=None) -> int:
     p, ty, ld = _matrix(x, table.dim, "x")
     q, tq, lq = _matrix(out, table.rows, "out")
     m = x.shape[0]
-    _need(out.shape[0] == m, f"out: {out.shape[0]} rows, expected {m}")
+    _check_rows(out, m, "out")
     w, n = _ws(workspace)
     return _lib().embbag_mx4_matmul(p, ty, ld, m, table.codes_ptr, table.scales_ptr, table.rows,
                                     table.dim, q, tq, lq, w, n, _stream(stream))
@@ -264,7 +297,7 @@ def embbag_mx4_matmul_grad(dy, table, dx, workspace, stream=None) -> int:
     p, ty, ld = _matrix(dy, table.rows, "dy")
     q, tq, lq = _matrix(dx, table.dim, "dx")
     m = dy.shape[0]
-    _need(dx.shape[0] == m, f"dx: {dx.shape[0]} rows, expected {m}")
+    _check_rows(dx, m, "dx")
     w, n = _ws(workspace)
     return _lib().embbag_mx4_matmul_grad(p, ty, ld, m, table.codes_ptr, table.scales_ptr,
                                          table.rows, table.dim, q, tq, lq, w, n, _stream(stream))
@@ -282,12 +315,12 @@ def embbag_logits_process(logits, out, seen=None, seen_offsets=None, prompt_lens
     if tq != ty:
         raise TypeError(f"out: dtype {out.dtype}, expected {logits.dtype} like logits")
     rows = logits.shape[0]
-    _need(out.shape[0] == rows, f"out: {out.shape[0]} rows, expected {rows}")
+    _check_rows(out, rows, "out")
     seen_p, seen_o, num_seen = _list(seen, seen_offsets, rows, "seen")
     bias_p, bias_o, num_biases = _list(bias_ids, bias_offsets, rows, "bias_ids")
     if bias_ids is not None and biases is None:
         raise ValueError("bias_ids without biases")
-    masks_p, num_masks, mask_stride = None, 0, 0
+    masks_p, num_masks, mask_stride = 0, 0, 0
     if masks is not None:
         if len(masks.shape) != 2 or masks.shape[1] * 32 < vocab:
             raise ValueError(f"masks: shape {tuple(masks.shape)}, expected 2-D with at least "
@@ -296,14 +329,15 @@ def embbag_logits_process(logits, out, seen=None, seen_offsets=None, prompt_lens
         num_masks, mask_stride = masks.shape
         if mask_ids is None and num_masks < rows:
             raise ValueError(f"masks: {num_masks} for {rows} rows and no mask_ids")
-    a = _Logits(rows, vocab, ty, p, ld, q, lq, seen_p, seen_o, num_seen,
-                _vector(prompt_lens, rows, "prompt_lens", _I32_T),
-                _vector(repetition, rows, "repetition", _F32_T),
-                _vector(frequency, rows, "frequency", _F32_T),
-                _vector(presence, rows, "presence", _F32_T), bias_p, bias_o,
-                _vector(biases, num_biases, "biases", _F32_T), num_biases, masks_p, mask_stride,
-                num_masks, _vector(mask_ids, rows, "mask_ids", _I32_T))
-    return _lib().embbag_logits_process(C.byref(a), _status_ptr(d_status), _stream(stream))
+    a = _pack_logits(
+        rows, vocab, ty, p, ld, q, lq, seen_p, seen_o, num_seen,
+        _vector(prompt_lens, rows, "prompt_lens", _I32_T),
+        _vector(repetition, rows, "repetition", _F32_T),
+        _vector(frequency, rows, "frequency", _F32_T),
+        _vector(presence, rows, "presence", _F32_T), bias_p, bias_o,
+        _vector(biases, num_biases, "biases", _F32_T), num_biases, masks_p, mask_stride,
+        num_masks, _vector(mask_ids, rows, "mask_ids", _I32_T))
+    return _lib().embbag_logits_process(a, _status(d_status), _stream(stream))
 
 
 def embbag_distill_workspace_bytes(rows, vocab, top) -> int:
@@ -318,22 +352,22 @@ def embbag_distill(logits, teacher_ids, teacher_logits, temperature, loss, works
     vocab = logits.shape[1] if len(logits.shape) == 2 else -1
     p, ty, ld = _matrix(logits, vocab, "logits")
     rows = logits.shape[0]
-    _need(len(teacher_ids.shape) == 2 and teacher_ids.shape[0] == rows,
-          f"teacher_ids: shape {tuple(teacher_ids.shape)}, expected [{rows}, top]")
+    if len(teacher_ids.shape) != 2 or teacher_ids.shape[0] != rows:
+        raise ValueError(f"teacher_ids: shape {tuple(teacher_ids.shape)}, expected [{rows}, top]")
     top = teacher_ids.shape[1]
     if teacher_logits.numel() != rows * top:
         _check_numel(teacher_logits, rows * top, "teacher_logits")
-    q, lq = None, 0
+    q, lq = 0, 0
     if grad is not None:
         q, tq, lq = _matrix(grad, vocab, "grad")
         if tq != ty:
             raise TypeError(f"grad: dtype {grad.dtype}, expected {logits.dtype} like logits")
-        _need(grad.shape[0] == rows, f"grad: {grad.shape[0]} rows, expected {rows}")
-    a = _Distill(rows, vocab, ty, p, ld, top,
-                 _vector(teacher_ids, None, "teacher_ids", _I32_T),
-                 EMBBAG_BF16 if teacher_logits.element_size() == 2 else EMBBAG_F32,
-                 _ptr(teacher_logits, _dt("float32", "bfloat16"), "teacher_logits"),
-                 float(temperature), _vector(row_weights, rows, "row_weights", _F32_T),
-                 _vector(loss, rows, "loss", _F32_T), q, lq)
+        _check_rows(grad, rows, "grad")
+    a = _pack_distill(
+        rows, vocab, ty, p, ld, top, _vector(teacher_ids, None, "teacher_ids", _I32_T),
+        EMBBAG_BF16 if teacher_logits.element_size() == 2 else EMBBAG_F32,
+        _ptr(teacher_logits, _dt("float32", "bfloat16"), "teacher_logits"),
+        C.c_float(temperature).value, _vector(row_weights, rows, "row_weights", _F32_T),
+        _vector(loss, rows, "loss", _F32_T), q, lq)
     w, n = _ws(workspace)
-    return _lib().embbag_distill(C.byref(a), w, n, _status_ptr(d_status), _stream(stream))
+    return _lib().embbag_distill(a, w, n, _status(d_status), _stream(stream))
