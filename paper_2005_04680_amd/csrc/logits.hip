@@ -11,7 +11,7 @@
 // come in batches of 16 entries per thread and many blocks share a compute unit.  Every
 // element is read by one thread, so that `out` may be `logits`.
 //
-// 256 x 131072 BF16 with up to 4096 seen tokens, 300 biases and masks: 46 us (20 us without
+// 256 x 131072 BF16 with up to 4096 seen tokens, 300 biases and masks: 45 us (20 us without
 // lists and masks, 6.6 TB/s; 33 us with the seen tokens alone): bound by the vector instructions of the
 // lists' walk, which every slice repeats, and of the touched tokens (69% of the cycles), and by the
 // chain.  Blocks that keep the lists in registers over several slices were slower (64 us: fewer of
@@ -27,7 +27,7 @@ namespace {
 constexpr uint32_t kPrompt = 0x80000000u;
 constexpr uint32_t kBiased = 0x40000000u;
 constexpr int kSliceTokens = 4096;
-constexpr int kListed = 1024;  // biases of a row that go to the list (16 bits hold their places)
+constexpr int kListed = 4 * kBlock;  // biases of a row that go to the list (16 bits hold their places)
 
 struct LogitsDev {
   embbag_logits_t a;
@@ -97,7 +97,8 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
   constexpr int PER = kListed / kBlock;            // listed biases per thread
   constexpr bool ANY = SEEN || BIAS;
   __shared__ __align__(16) uint32_t words[ANY ? kSliceTokens : 4];
-  __shared__ uint32_t listed[BIAS ? kListed : 1];  // token of the slice << 16 | place in the row's list
+  // Token of the slice << 16 | place in the row's list.
+  __shared__ __align__(16) uint32_t listed[BIAS ? kListed : 4];
   __shared__ uint32_t num_listed;
   const embbag_logits_t& a = dv.a;
   const int r = int(blockIdx.x / dv.slices);
@@ -168,6 +169,7 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
 
   if constexpr (ANY) {
     clear();
+    if constexpr (BIAS) *reinterpret_cast<u4*>(listed + threadIdx.x * 4) = u4{0u, 0u, 0u, 0u};
     if (threadIdx.x == 0) num_listed = 0u;
     __syncthreads();
   }
@@ -197,7 +199,8 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
   }
   if constexpr (ANY) __syncthreads();
 
-  // The last listed bias of a token finds itself: no entry of the token has a later place.
+  // The last listed bias of a token finds itself: no entry of the token has a later place.  (Four at
+  // a time; the list's unused entries are 0, which is later than none.)
   const int n = BIAS ? int(num_listed) : 0;
   float bias[PER];
   int token[PER];
@@ -208,7 +211,11 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
     if (!BIAS || q * kBlock >= n || e >= n) continue;
     const uint32_t mine = listed[e];
     bool lastly = true;
-    for (int i = 0; i < n; ++i) lastly = lastly && (listed[i] <= mine || (listed[i] >> 16) != (mine >> 16));
+    for (int i = 0; i < n; i += 4) {
+      const u4 o = *reinterpret_cast<const u4*>(listed + i);
+      auto before = [&](uint32_t other) { return other <= mine || (other >> 16) != (mine >> 16); };
+      lastly = lastly && before(o.x) && before(o.y) && before(o.z) && before(o.w);
+    }
     if (lastly) {
       token[q] = int(mine >> 16);
       bias[q] = a.biases[int64_t(b0) + (mine & 0xFFFFu)];
@@ -245,9 +252,13 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
         for (int e = 0; e < V; ++e) l[e] += add[i * V + e];
       }
     }
+    if (mask != nullptr) {
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (((bits[i] >> e) & 1u) == 0u) l[e] = low();
+      for (int e = 0; e < V; ++e) {
+        const uint32_t keep = uint32_t(__builtin_amdgcn_sbfe(int(bits[i]), uint32_t(e), 1u));
+        l[e] = __uint_as_float((__float_as_uint(l[e]) & keep) | (__float_as_uint(low()) & ~keep));
+      }
+    }
     store_vec(y + v, len - v, l);
   }
   if constexpr (BIAS) {
