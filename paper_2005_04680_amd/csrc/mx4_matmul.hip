@@ -338,9 +338,12 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   }
 #undef EMB_ROW
 
-  // (The next tile's first products take no fragments.)
+  // The next tile's first products take no fragments, and no scale: the byte 255 makes NaN of zeros
+  // too, and that of a bad block, or of a row past the end, would stay in the new tile's sums.
 #pragma unroll
-  for (int i = 0; i < TN; ++i) a[1][i] = u4{0u, 0u, 0u, 0u};
+  for (int i = 0; i < TN; ++i) a[1][i] = u4{0u, 0u, 0u, 0u}, cw[i] = 0u;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) cx[i] = 0u;
 
   // Each wavefront turns 32 rows of x and 32 * TILES of W at a time around in its own part of LDS
   // (lane: row of x lane % 32, four consecutive rows of W per quarter of its registers), then
