@@ -10,7 +10,8 @@
 // Bound by memory: 4096 x 131072 BF16 458 us, 2.04 GB (a twentieth of the rows is left out), 4.5 TB/s;
 // few rows by the chain of load, sum, store: 33 x 32001 FP32 10.8 us.
 //
-// exp(x) is taken as 2^((x - largest) * log2(e) / temperature).  The teacher's entries are few: one
+// exp(x) is taken as 2^((x - largest) * log2(e) / temperature), and the loss sums p (x - largest): an
+// offset that a row's logits share costs no digits.  The teacher's entries are few: one
 // wavefront makes their softmax while the row is on its way.  The entry that names an id
 // first subtracts all its entries' probabilities, after the row has been written: no atomics on
 // sums.  A table in LDS shows whether any id comes twice; only then are the entries compared with
@@ -26,8 +27,10 @@ constexpr int kPer = kMaxTeacher / kBlock;  // entries per thread of the smalles
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Of a slice: the largest logit, the sum of the exponentials and the teacher's probabilities times the
+// logits, both relative to that logit, and those probabilities' sum.
 struct Part {
-  float top, sum, cross;
+  float top, sum, cross, mass;
 };
 
 struct DistillDev {
@@ -55,7 +58,7 @@ struct Teacher {
   int repeated;
   float plogp;
   int live;
-  float red[3][kRowThreads / kWave];
+  float red[4][kRowThreads / kWave];
 };
 
 // The softmax of row r's entries, by one wavefront: ids (-1: none), probabilities, the sum of
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(THREADS) void distill_row(DistillDev dv, int32_t* _
   for (int j = 0; j < PER; ++j) {
     const int k = j * THREADS + tid;
     xk[j] = k < a.top && t.ids[k] >= 0 ? to_f32(x[t.ids[k]]) : 0.f;
-    if (k < a.top && t.p[k] != 0.f) cross += t.p[k] * xk[j];
+    if (k < a.top && t.p[k] != 0.f) cross += t.p[k] * (xk[j] - ref);
   }
   sum = wave_sum(sum);
   cross = wave_sum(cross);
@@ -240,7 +243,7 @@ __global__ __launch_bounds__(THREADS) void distill_row(DistillDev dv, int32_t* _
   const bool live = t.live && !(sum == 0.f);
   if (tid == 0) {
     const float T1 = a.temperature;
-    a.loss[r] = live ? w * T1 * T1 * (t.plogp - (cross - ref) / T1 + __builtin_logf(sum)) : 0.f;
+    a.loss[r] = live ? w * T1 * T1 * (t.plogp - cross / T1 + __builtin_logf(sum)) : 0.f;
   }
   if (g == nullptr) return;
   if (!live) {
@@ -314,14 +317,18 @@ __global__ __launch_bounds__(kBlock) void distill_sums(DistillDev dv, int32_t* _
   for (int i = 0; i < kWavesPerBlock; ++i) top = fmaxf(top, t.red[0][i]);
   const float ref = top == low() ? 0.f : top;
   sum = sum == 0.f ? 0.f : sum * exp2_of(((mine == low() ? 0.f : mine) - ref) * c);
-  float cross = 0.f;
+  float cross = 0.f, mass = 0.f;
   for (int k = threadIdx.x; k < a.top; k += kBlock) {
     const int64_t at = t.ids[k] - base;
-    if (t.ids[k] >= 0 && at >= 0 && at < len && t.p[k] != 0.f) cross += t.p[k] * to_f32(x[at]);
+    if (t.ids[k] >= 0 && at >= 0 && at < len && t.p[k] != 0.f) {
+      cross += t.p[k] * (to_f32(x[at]) - ref);
+      mass += t.p[k];
+    }
   }
   sum = block_sum(sum, t.red[1]);
   cross = block_sum(cross, t.red[2]);
-  if (threadIdx.x == 0) dv.parts[int64_t(r) * dv.slices + sl] = {top, sum, cross};
+  mass = block_sum(mass, t.red[3]);
+  if (threadIdx.x == 0) dv.parts[int64_t(r) * dv.slices + sl] = {top, sum, cross, mass};
 }
 
 // Few rows: joins a row's parts, and the gradient of a slice.
@@ -347,13 +354,14 @@ __global__ __launch_bounds__(kBlock) void distill_grad(DistillDev dv) {
   for (uint32_t i = 0; i < dv.slices; ++i) {
     const float m = q[i].top == low() ? 0.f : q[i].top;
     sum += q[i].sum == 0.f ? 0.f : q[i].sum * exp2_of((m - ref) * c);
-    cross += q[i].cross;
+    // (A slice without entries adds nothing, however far its largest logit is.)
+    if (q[i].mass != 0.f) cross += q[i].cross + (m - ref) * q[i].mass;
   }
   __syncthreads();
   const bool live = w != 0.f && t.live && !(sum == 0.f);
   if (sl == 0 && threadIdx.x == 0) {
     const float T1 = a.temperature;
-    a.loss[r] = live ? w * T1 * T1 * (t.plogp - (cross - ref) / T1 + __builtin_logf(sum)) : 0.f;
+    a.loss[r] = live ? w * T1 * T1 * (t.plogp - cross / T1 + __builtin_logf(sum)) : 0.f;
   }
   if (g == nullptr) return;
   if (!live) {
