@@ -62,7 +62,8 @@ struct Teacher {
 };
 
 // The softmax of row r's entries, by one wavefront: ids (-1: none), probabilities, the sum of
-// p log p, and whether the row has any entry that is not -infinity.
+// p log p, and whether the row has any entry that is not -infinity.  The temperature divides the distances
+// to the largest entry: divided first, entries of 20 at 1e-4 would be off by 0.008 in the exponent.
 __device__ __forceinline__ void teacher_row(const embbag_distill_t& a, int r, Teacher& t,
                                             int32_t* status) {
   const float inv_t = 1.f / a.temperature;
@@ -77,8 +78,8 @@ __device__ __forceinline__ void teacher_row(const embbag_distill_t& a, int r, Te
                         ? to_f32(static_cast<const __bf16*>(a.teacher)[row + k])
                         : static_cast<const float*>(a.teacher)[row + k];
     t.ids[k] = id;
-    t.p[k] = id >= 0 ? x * inv_t : low();
-    if (id >= 0) top = fmaxf(top, x * inv_t);
+    t.p[k] = id >= 0 ? x : low();
+    if (id >= 0) top = fmaxf(top, x);
     some = some || (id >= 0 && x != low());  // (a NaN as well)
   }
   if (bad && status != nullptr) atomicMin(status, EMBBAG_ERR_INDEX_RANGE);
@@ -86,12 +87,12 @@ __device__ __forceinline__ void teacher_row(const embbag_distill_t& a, int r, Te
   const float ref = top == low() ? 0.f : top;
   float sum = 0.f;
   for (int k = lane_id(); k < a.top; k += kWave)
-    sum += t.ids[k] >= 0 ? exp2_of((t.p[k] - ref) * kLog2e) : 0.f;
+    sum += t.ids[k] >= 0 ? exp2_of((t.p[k] - ref) * inv_t * kLog2e) : 0.f;
   sum = wave_sum(sum);
   const float inv = 1.f / sum, log_sum = __builtin_logf(sum);
   float pl = 0.f;
   for (int k = lane_id(); k < a.top; k += kWave) {
-    const float z = t.p[k] - ref;
+    const float z = (t.p[k] - ref) * inv_t;
     const float q = t.ids[k] >= 0 ? exp2_of(z * kLog2e) * inv : 0.f;
     t.p[k] = q;
     if (q != 0.f) pl += q * (z - log_sum);

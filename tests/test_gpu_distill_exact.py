@@ -1,6 +1,6 @@
 """The digits of distillation's loss and gradient: logits that share an offset, against the 64-bit
-reference, with bounds that follow from the distances to a row's largest logit, not from the
-logits' own size."""
+reference, and low temperatures, with bounds that follow from the distances to a row's largest
+logit, not from the logits' own size."""
 import numpy as np
 import pytest
 import torch
@@ -102,3 +102,42 @@ def test_slices_far_apart(rows, vocab):
     ids[0, 0] = vocab // 2 - 1
     loss, grad, _ = run(x, ids, t, 1.0)
     assert loss[0] == float("inf") and torch.isfinite(loss[1:]).all() and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(4, 900), (200, 333), (2, 33001)])
+@pytest.mark.parametrize("temperature", [1e-2, 1e-4, 1e-6, 1e4])
+@pytest.mark.parametrize("offset", [20.0, -3.0])
+def test_low_temperatures(rows, vocab, temperature, offset):
+    """Logits a few temperatures apart around an offset (as FP32 has them)."""
+    rng = np.random.default_rng(vocab)
+    spread = temperature * 2
+    x = torch.from_numpy((rng.normal(size=(rows, vocab)) * spread + offset).astype(np.float32))
+    t = torch.from_numpy((rng.normal(size=(rows, 20)) * spread + offset).astype(np.float32))
+    ids = np.stack([rng.choice(vocab, size=20, replace=False) for _ in range(rows)]).astype(np.int32)
+    ids[1, 3:9] = -1
+    want, wgrad, ltol, gtol = bounds(x, ids, t, temperature, "f32")
+    loss, grad, _ = run(x, ids, t, temperature)
+    close(loss, want, ltol, "loss")
+    close(grad, wgrad, gtol, "gradient")
+
+
+@pytest.mark.parametrize("rows,vocab", [(2, 900), (2, 33001)])
+def test_a_teacher_that_the_temperature_would_overflow(rows, vocab):
+    rng = np.random.default_rng(1)
+    T = 1e-6
+    x = torch.from_numpy((rng.normal(size=(rows, vocab)) * T).astype(np.float32))
+    t = torch.tensor([[1e33, 1e33, -1e33, -np.inf], [3e38, -3e38, 3e38, 0.0]])
+    ids = np.array([[5, 7, 1, 2], [10, 3, vocab - 1, 0]], np.int32)
+    loss, grad, _ = run(x, ids, t, T)
+    p = np.array([[0.5, 0.5, 0.0, 0.0], [0.5, 0.0, 0.5, 0.0]])
+    z = x.double().numpy() / T
+    q = np.exp(z - z.max(1, keepdims=True))
+    q /= q.sum(1, keepdims=True)
+    want, wgrad = np.zeros(rows), T * q
+    for r in range(rows):
+        want[r] = T * T * sum(a * (np.log(a) - np.log(q[r, v])) for a, v in zip(p[r], ids[r]) if a)
+        wgrad[r, ids[r]] -= T * p[r]
+    # (Exponents up to 10, a sum of vocab terms, and T itself as FP32 has it.)
+    rel = U * (8 * 10 + vocab / 64 + 200)
+    close(loss, want, rel * T * T * 20, "loss")
+    close(grad, wgrad, rel * (T * q + np.abs(wgrad)), "gradient")
