@@ -177,6 +177,11 @@ __global__ __launch_bounds__(THREADS) void distill_row(DistillDev dv, int32_t* _
   T* g = a.grad != nullptr ? static_cast<T*>(a.grad) + int64_t(r) * a.grad_stride : nullptr;
   const float w = a.row_weights != nullptr ? a.row_weights[r] : 1.f;
   if (w == 0.f) {
+    // (A bad id of a row that is left out is an error all the same, as it is in the slices.)
+    bool bad = false;
+    for (int k = threadIdx.x; k < a.top; k += THREADS)
+      bad = bad || a.ids[int64_t(r) * a.top + k] >= a.vocab;
+    if (bad && status != nullptr) atomicMin(status, EMBBAG_ERR_INDEX_RANGE);
     if (threadIdx.x == 0) a.loss[r] = 0.f;
     if (g != nullptr) zero_row(g, a.vocab);
     return;

@@ -141,3 +141,24 @@ def test_a_teacher_that_the_temperature_would_overflow(rows, vocab):
     rel = U * (8 * 10 + vocab / 64 + 200)
     close(loss, want, rel * T * T * 20, "loss")
     close(grad, wgrad, rel * (T * q + np.abs(wgrad)), "gradient")
+
+
+@pytest.mark.parametrize("rows,vocab,top", [(2, 50, 3), (2, 5000, 300), (2, 40003, 3), (300, 50, 3), (130, 9000, 1024)])
+@pytest.mark.parametrize("left_out", ["weight", "teacher", "logits", "no"])
+def test_a_bad_id_is_reported_whatever_its_row(rows, vocab, top, left_out):
+    """Also in a row that is left out, and however many rows there are."""
+    x = torch.randn(rows, vocab, generator=torch.Generator().manual_seed(1))
+    ids = np.tile(np.arange(top, dtype=np.int32) % vocab, (rows, 1))
+    t, w = torch.zeros(rows, top), np.ones(rows, np.float32)
+    if left_out == "weight":
+        w[1] = 0
+    elif left_out == "teacher":
+        t[1] = float("-inf")
+    elif left_out == "logits":
+        x[1] = float("-inf")
+    for grad in (True, False):
+        assert run(x, ids, t, 1.0, w, grad)[2] == 0
+        for at in (0, top - 1):
+            bad = ids.copy()
+            bad[1, at] = vocab
+            assert run(x, bad, t, 1.0, w, grad)[2] == pk.EMBBAG_ERR_INDEX_RANGE
