@@ -355,8 +355,10 @@ def embbag_distill(logits, teacher_ids, teacher_logits, temperature, loss, works
     if len(teacher_ids.shape) != 2 or teacher_ids.shape[0] != rows:
         raise ValueError(f"teacher_ids: shape {tuple(teacher_ids.shape)}, expected [{rows}, top]")
     top = teacher_ids.shape[1]
-    if teacher_logits.numel() != rows * top:
-        _check_numel(teacher_logits, rows * top, "teacher_logits")
+    if teacher_logits.shape != teacher_ids.shape and (len(teacher_logits.shape) == 2 or
+                                                      teacher_logits.numel() != rows * top):
+        raise ValueError(f"teacher_logits: shape {tuple(teacher_logits.shape)}, expected "
+                         f"{tuple(teacher_ids.shape)} like teacher_ids")
     q, lq = 0, 0
     if grad is not None:
         q, tq, lq = _matrix(grad, vocab, "grad")
