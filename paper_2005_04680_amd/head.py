@@ -94,6 +94,12 @@ def _lib():
 
 
 # ---- marshalling helpers ---------------------------------------------------
+def _i32(n):
+    """A size as the C ABI's 32 bits take it: ctypes would wrap a larger one into their range, -1 is out
+    of every size's."""
+    return n if -2 ** 31 <= n < 2 ** 31 else -1
+
+
 def _types():
     import torch
     return {torch.float32: EMBBAG_F32, torch.bfloat16: EMBBAG_BF16}
@@ -190,6 +196,7 @@ class Mx4Table:
 
     def __init__(self, codes, scales, dim):
         dim = int(dim)
+        _need(dim < 2 ** 31, f"dim: {dim} does not fit 32 bits")
         _need(len(codes.shape) == 2 and codes.shape[1] == mx4_code_bytes(dim),
               f"codes: shape {tuple(codes.shape)}, expected [rows, {mx4_code_bytes(dim)}]")
         _need(tuple(scales.shape) == (codes.shape[0], mx4_scale_bytes(dim)),
@@ -266,7 +273,7 @@ def embbag_mx4_forward(tables, batch, indices, offsets, pooled_out, per_sample_w
     _check_numel(per_sample_weights, indices.numel(), "per_sample_weights")
     out = _ptr(pooled_out, _dt("float32", "bfloat16"), "pooled_out")
     return _lib().embbag_mx4_forward(
-        C.byref(tables.struct), int(batch), _ptr(indices, _dt(*_I32), "indices"),
+        C.byref(tables.struct), _i32(int(batch)), _ptr(indices, _dt(*_I32), "indices"),
         _ptr(offsets, _dt(*_I32), "offsets"), indices.numel(),
         _ptr(per_sample_weights, _dt("float32"), "per_sample_weights"), int(pooling), out,
         EMBBAG_BF16 if pooled_out.element_size() == 2 else EMBBAG_F32, _status(d_status),
@@ -274,7 +281,7 @@ def embbag_mx4_forward(tables, batch, indices, offsets, pooled_out, per_sample_w
 
 
 def embbag_mx4_matmul_workspace_bytes(m, n, k) -> int:
-    return int(_lib().embbag_mx4_matmul_workspace_bytes(int(m), int(n), int(k)))
+    return int(_lib().embbag_mx4_matmul_workspace_bytes(_i32(int(m)), int(n), _i32(int(k))))
 
 
 def embbag_mx4_matmul(x, table, out, workspace, stream=None) -> int:
@@ -284,12 +291,12 @@ def embbag_mx4_matmul(x, table, out, workspace, stream=None) -> int:
     m = x.shape[0]
     _check_rows(out, m, "out")
     w, n = _ws(workspace)
-    return _lib().embbag_mx4_matmul(p, ty, ld, m, table.codes_ptr, table.scales_ptr, table.rows,
+    return _lib().embbag_mx4_matmul(p, ty, ld, _i32(m), table.codes_ptr, table.scales_ptr, table.rows,
                                     table.dim, q, tq, lq, w, n, _stream(stream))
 
 
 def embbag_mx4_matmul_grad_workspace_bytes(m, n, k) -> int:
-    return int(_lib().embbag_mx4_matmul_grad_workspace_bytes(int(m), int(n), int(k)))
+    return int(_lib().embbag_mx4_matmul_grad_workspace_bytes(_i32(int(m)), int(n), _i32(int(k))))
 
 
 def embbag_mx4_matmul_grad(dy, table, dx, workspace, stream=None) -> int:
@@ -299,7 +306,7 @@ def embbag_mx4_matmul_grad(dy, table, dx, workspace, stream=None) -> int:
     m = dy.shape[0]
     _check_rows(dx, m, "dx")
     w, n = _ws(workspace)
-    return _lib().embbag_mx4_matmul_grad(p, ty, ld, m, table.codes_ptr, table.scales_ptr,
+    return _lib().embbag_mx4_matmul_grad(p, ty, ld, _i32(m), table.codes_ptr, table.scales_ptr,
                                          table.rows, table.dim, q, tq, lq, w, n, _stream(stream))
 
 
@@ -341,7 +348,7 @@ def embbag_logits_process(logits, out, seen=None, seen_offsets=None, prompt_lens
 
 
 def embbag_distill_workspace_bytes(rows, vocab, top) -> int:
-    return int(_lib().embbag_distill_workspace_bytes(int(rows), int(vocab), int(top)))
+    return int(_lib().embbag_distill_workspace_bytes(_i32(int(rows)), _i32(int(vocab)), _i32(int(top))))
 
 
 def embbag_distill(logits, teacher_ids, teacher_logits, temperature, loss, workspace, grad=None,
