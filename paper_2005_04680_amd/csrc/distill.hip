@@ -38,6 +38,7 @@ struct DistillDev {
   int32_t slice;    // elements per slice
   uint32_t slices;  // per row
   Part* parts;
+  uint32_t first;   // row that the launch begins with, where a block takes a whole one
 };
 
 __device__ __forceinline__ float wave_max(float v) {
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(THREADS) void distill_row(DistillDev dv, int32_t* _
   constexpr int PER = kMaxTeacher / THREADS;
   __shared__ Teacher t;
   const embbag_distill_t& a = dv.a;
-  const int r = int(blockIdx.x);
+  const int r = int(dv.first + blockIdx.x);
   const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride;
   T* g = a.grad != nullptr ? static_cast<T*>(a.grad) + int64_t(r) * a.grad_stride : nullptr;
   const float w = a.row_weights != nullptr ? a.row_weights[r] : 1.f;
@@ -419,26 +420,27 @@ int32_t slice_of(int32_t rows, int32_t vocab) {
   return int32_t(s < kLeastSlice ? kLeastSlice : s);
 }
 
-template <class T, int NV>
-void launch_row(const DistillDev& dv, int32_t* status, hipStream_t st) {
-  hipLaunchKernelGGL((distill_row<T, kRowThreads, NV>), dim3(uint32_t(dv.a.rows)),
-                     dim3(kRowThreads), 0, st, dv, status);
+template <class T, int THREADS, int NV>
+void launch_row(DistillDev& dv, int32_t* status, hipStream_t st) {
+  for_launches(dv.a.rows, THREADS, [&](uint32_t first, dim3 grid) {
+    dv.first = first;
+    hipLaunchKernelGGL((distill_row<T, THREADS, NV>), grid, dim3(THREADS), 0, st, dv, status);
+  });
 }
 
 template <class T>
-void launch_type(const DistillDev& dv, int32_t* status, hipStream_t st) {
+void launch_type(DistillDev& dv, int32_t* status, hipStream_t st) {
   const embbag_distill_t& a = dv.a;
   const int64_t vecs = (int64_t(a.vocab) + kVec<T> - 1) / kVec<T>;
   if (a.rows >= kWholeRows || vecs <= kWholeVecs) {
     if (vecs <= kBlock * 4)
-      hipLaunchKernelGGL((distill_row<T, kBlock, 4>), dim3(uint32_t(a.rows)), dim3(kBlock), 0, st,
-                         dv, status);
+      launch_row<T, kBlock, 4>(dv, status, st);
     else if (vecs <= kRowThreads * 4)
-      launch_row<T, 4>(dv, status, st);
+      launch_row<T, kRowThreads, 4>(dv, status, st);
     else if (vecs <= kRowThreads * 8)
-      launch_row<T, 8>(dv, status, st);
+      launch_row<T, kRowThreads, 8>(dv, status, st);
     else
-      launch_row<T, 16>(dv, status, st);
+      launch_row<T, kRowThreads, 16>(dv, status, st);
     return;
   }
   const dim3 grid(dv.slices * uint32_t(a.rows));
@@ -465,6 +467,7 @@ hipError_t launch_distill(const embbag_distill_t& a, char* ws, int32_t* status, 
   dv.slice = slice_of(a.rows, a.vocab);
   dv.slices = slices_of(a.vocab, dv.slice);
   dv.parts = reinterpret_cast<Part*>(ws);
+  dv.first = 0;
   if (a.type == EMBBAG_BF16)
     launch_type<__bf16>(dv, status, st);
   else

@@ -146,6 +146,15 @@ __device__ __forceinline__ uint32_t quotient(uint32_t u, const FastDiv& f) {
   return uint32_t((uint64_t(u) * f.mul) >> f.shift);
 }
 
+// HIP takes fewer than 2^32 threads a launch.  Calls fn(first block, grid) for the launches, one but for
+// the largest sizes, that make up `blocks` blocks.
+template <class Fn>
+void for_launches(int64_t blocks, int threads, Fn fn) {
+  const int64_t most = (int64_t(1) << 31) / threads;
+  for (int64_t b = 0; b < blocks; b += most)
+    fn(uint32_t(b), dim3(uint32_t(blocks - b < most ? blocks - b : most)));
+}
+
 // One microscaled table.
 struct Mx4View {
   const uint8_t* codes;

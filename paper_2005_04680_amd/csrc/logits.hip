@@ -32,6 +32,7 @@ constexpr int kListed = 4 * kBlock;  // biases of a row that go to the list (16 
 struct LogitsDev {
   embbag_logits_t a;
   uint32_t slices;  // per row
+  uint32_t first;   // block that the launch begins with
 };
 
 // [o[r], o[r+1]) of a list of n entries, empty (and an error) where it is none.
@@ -101,8 +102,9 @@ __global__ __launch_bounds__(kBlock) void logits_kernel(LogitsDev dv,
   __shared__ __align__(16) uint32_t listed[BIAS ? kListed : 4];
   __shared__ uint32_t num_listed;
   const embbag_logits_t& a = dv.a;
-  const int r = int(blockIdx.x / dv.slices);
-  const int base = int(blockIdx.x - uint32_t(r) * dv.slices) * kSliceTokens;
+  const uint32_t block = dv.first + blockIdx.x;
+  const int r = int(block / dv.slices);
+  const int base = int(block - uint32_t(r) * dv.slices) * kSliceTokens;
   const int len = min(kSliceTokens, a.vocab - base);
   const T* x = static_cast<const T*>(a.logits) + int64_t(r) * a.logits_stride + base;
   T* y = static_cast<T*>(a.out) + int64_t(r) * a.out_stride + base;
@@ -296,11 +298,13 @@ hipError_t launch_logits(const embbag_logits_t& a, int32_t* status, hipStream_t 
   LogitsDev dv;
   dv.a = a;
   dv.slices = uint32_t((int64_t(a.vocab) + kSliceTokens - 1) / kSliceTokens);
-  const dim3 grid(dv.slices * uint32_t(a.rows));
-  if (a.type == EMBBAG_BF16)
-    launch_type<__bf16>(dv, grid, status, st);
-  else
-    launch_type<float>(dv, grid, status, st);
+  for_launches(int64_t(dv.slices) * a.rows, kBlock, [&](uint32_t first, dim3 grid) {
+    dv.first = first;
+    if (a.type == EMBBAG_BF16)
+      launch_type<__bf16>(dv, grid, status, st);
+    else
+      launch_type<float>(dv, grid, status, st);
+  });
   return hipGetLastError();
 }
 

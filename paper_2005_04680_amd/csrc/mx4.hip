@@ -14,8 +14,9 @@
 namespace embbag {
 namespace {
 
-// Units (blocks) per launch: the kernels number them in 31 bits.
-constexpr int64_t kMaxUnits = int64_t(1) << 30;
+// Units (blocks) per launch, four threads each, of which a launch takes fewer than 2^32.  (The kernels
+// number them in 31 bits.)
+constexpr int64_t kMaxUnits = int64_t(1) << 29;
 
 // Unit u of the launch is block (u + first) % nb of row row0 + (u + first) / nb, or of
 // the row that the list names there.

@@ -36,7 +36,7 @@ template <int LPR, class T>
 __global__ __launch_bounds__(kBlock) void mx4_weighted_kernel(
     TableDesc d, const int32_t* __restrict__ I, const int32_t* __restrict__ O, int32_t NS,
     int32_t B, float inv_b, int32_t split, int32_t bags, T* __restrict__ Y,
-    int32_t* __restrict__ status, const float* __restrict__ A) {
+    int32_t* __restrict__ status, const float* __restrict__ A, uint32_t first_block) {
   constexpr int R = kWave / LPR;
   constexpr int U = 4;  // rows in flight per lane
   __shared__ TableLds tl;
@@ -46,7 +46,8 @@ __global__ __launch_bounds__(kBlock) void mx4_weighted_kernel(
   const int rg = lane / LPR, rl = lane % LPR;
   const int per_wave = R / split;  // bags of a wavefront
   const int64_t first =
-      (int64_t(xcd_remap(blockIdx.x, gridDim.x)) * (blockDim.x / kWave) + wave_id()) * per_wave;
+      (int64_t(first_block + xcd_remap(blockIdx.x, gridDim.x)) * (blockDim.x / kWave) + wave_id()) *
+      per_wave;
   const int64_t k64 = first + rg / split;
   const bool live = k64 < bags;
   const int k = live ? int(k64) : bags - 1;
@@ -144,7 +145,7 @@ template <int P, int U, int MODE, class T>
 __global__ __launch_bounds__(kBlock) void mx4_sum_kernel(
     TableDesc d, const int32_t* __restrict__ I, const int32_t* __restrict__ O, int32_t NS,
     int32_t B, float inv_b, int32_t split, int32_t bags, T* __restrict__ Y,
-    int32_t* __restrict__ status) {
+    int32_t* __restrict__ status, uint32_t first_block) {
   constexpr int R = 32 / P;
   __shared__ TableLds tl;
   stage_tables(d, tl);
@@ -154,7 +155,8 @@ __global__ __launch_bounds__(kBlock) void mx4_sum_kernel(
   const int rg = col / P, b = col % P;
   const int per_wave = R / split;  // bags of a wavefront
   const int64_t first =
-      (int64_t(xcd_remap(blockIdx.x, gridDim.x)) * (blockDim.x / kWave) + wave_id()) * per_wave;
+      (int64_t(first_block + xcd_remap(blockIdx.x, gridDim.x)) * (blockDim.x / kWave) + wave_id()) *
+      per_wave;
   const int64_t k64 = first + rg / split;
   const bool live = k64 < bags;
   const int k = live ? int(k64) : bags - 1;
@@ -259,19 +261,19 @@ __global__ void mx4_empty_check(const int32_t* __restrict__ O, int32_t NS,
 template <int MODE, class T>
 void dispatch(int lpr, bool four, dim3 grid, hipStream_t st, const TableDesc& d, const int32_t* I,
               const int32_t* O, int32_t NS, int32_t B, int32_t split, int32_t bags, T* Y,
-              int32_t* status, const float* A) {
+              int32_t* status, const float* A, uint32_t first) {
   const float inv_b = 1.f / float(B);
 #define EMB_MX4(L)                                                                               \
   case L:                                                                                        \
     if constexpr (MODE == kPoolWeighted)                                                         \
       hipLaunchKernelGGL((mx4_weighted_kernel<L, T>), grid, dim3(kBlock), 0, st, d, I, O,   \
-                         NS, B, inv_b, split, bags, Y, status, A);                               \
+                         NS, B, inv_b, split, bags, Y, status, A, first);                        \
     else if (four)                                                                               \
       hipLaunchKernelGGL((mx4_sum_kernel<L / 2, 4, MODE, T>), grid, dim3(kBlock), 0, \
-                         st, d, I, O, NS, B, inv_b, split, bags, Y, status);                     \
+                         st, d, I, O, NS, B, inv_b, split, bags, Y, status, first);              \
     else                                                                                         \
       hipLaunchKernelGGL((mx4_sum_kernel<L / 2, 2, MODE, T>), grid, dim3(kBlock), 0, st, d, I,   \
-                         O, NS, B, inv_b, split, bags, Y, status);                               \
+                         O, NS, B, inv_b, split, bags, Y, status, first);                        \
     break
   switch (lpr) {
     EMB_MX4(2);
@@ -287,13 +289,13 @@ void dispatch(int lpr, bool four, dim3 grid, hipStream_t st, const TableDesc& d,
 template <class T>
 void dispatch_mode(int mode, int lpr, bool four, dim3 grid, hipStream_t st, const TableDesc& d,
                    const int32_t* I, const int32_t* O, int32_t NS, int32_t B, int32_t split,
-                   int32_t bags, T* Y, int32_t* status, const float* A) {
+                   int32_t bags, T* Y, int32_t* status, const float* A, uint32_t first) {
   if (mode == kPoolWeighted)
-    dispatch<kPoolWeighted>(lpr, four, grid, st, d, I, O, NS, B, split, bags, Y, status, A);
+    dispatch<kPoolWeighted>(lpr, four, grid, st, d, I, O, NS, B, split, bags, Y, status, A, first);
   else if (mode == kPoolMean)
-    dispatch<kPoolMean>(lpr, four, grid, st, d, I, O, NS, B, split, bags, Y, status, A);
+    dispatch<kPoolMean>(lpr, four, grid, st, d, I, O, NS, B, split, bags, Y, status, A, first);
   else
-    dispatch<kPoolPlain>(lpr, four, grid, st, d, I, O, NS, B, split, bags, Y, status, A);
+    dispatch<kPoolPlain>(lpr, four, grid, st, d, I, O, NS, B, split, bags, Y, status, A, first);
 }
 
 }  // namespace
@@ -326,13 +328,14 @@ hipError_t launch_mx4_forward(const TableDesc& d, int32_t B, const int32_t* I, c
   // 64 19.8 / 18.5; 8 x 64 ragged of 32, E = 64 5.4 / 6.0.
   const bool four = avg > 4 * split && (lpr > 4 || few());
   const int64_t per_block = int64_t(kWavesPerBlock) * (groups / split);
-  const dim3 grid(unsigned((bags + per_block - 1) / per_block));
-  if (y_bf16)
-    dispatch_mode(pool.mode, lpr, four, grid, st, d, I, O, int32_t(NS), B, split, int32_t(bags),
-                  static_cast<__bf16*>(Y), status, pool.weights);
-  else
-    dispatch_mode(pool.mode, lpr, four, grid, st, d, I, O, int32_t(NS), B, split, int32_t(bags),
-                  static_cast<float*>(Y), status, pool.weights);
+  for_launches((bags + per_block - 1) / per_block, kBlock, [&](uint32_t first, dim3 grid) {
+    if (y_bf16)
+      dispatch_mode(pool.mode, lpr, four, grid, st, d, I, O, int32_t(NS), B, split, int32_t(bags),
+                    static_cast<__bf16*>(Y), status, pool.weights, first);
+    else
+      dispatch_mode(pool.mode, lpr, four, grid, st, d, I, O, int32_t(NS), B, split, int32_t(bags),
+                    static_cast<float*>(Y), status, pool.weights, first);
+  });
   return hipGetLastError();
 }
 

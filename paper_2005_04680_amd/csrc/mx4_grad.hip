@@ -84,7 +84,8 @@ __device__ __forceinline__ u4 bf16_values8(uint32_t c, float scale) {
 }
 
 // WK x WM wavefronts, each TK x TM products of 32 x 32.  Block: split z of the rows of W
-// (`per` steps each), k tile, m tile.  `dx` is the output, or part z of the parts.
+// (`per` steps each), k tile, m tile, from block `first` of them on.  `dx` is the output, or part z of
+// the parts.
 //
 // The last rows of all may be less than a step.  dy's 8 columns of a load that would pass its row
 // are then the row's last 8: W's tile takes the same rows there, without those that
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
                                                        int32_t m, Mx4View w, uint32_t ktiles,
                                                        uint32_t mtiles, int32_t per,
                                                        TX* __restrict__ dx, int64_t ldx,
-                                                       int64_t part_stride) {
+                                                       int64_t part_stride, uint32_t first) {
   static_assert(WK * WM == kWavesPerBlock, "four wavefronts");
   constexpr int BK = 32 * TK * WK, BM = 32 * TM * WM;
   constexpr int YL = BM / 32;              // loads of dy per thread
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(kBlock, 1) void grad_tile(const TY* __restrict__ dy
   extern __shared__ __align__(16) uint8_t lds[];
 
   const int lane = lane_id(), wave = wave_id();
-  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t id = first + xcd_remap(blockIdx.x, gridDim.x);
   const uint32_t tiles = ktiles * mtiles;
   const uint32_t z = id / tiles, tile = id - z * tiles;
   const uint32_t mt = tile / ktiles, kt = tile - mt * ktiles;
@@ -331,12 +332,14 @@ __global__ __launch_bounds__(1024) void grad_join_many(const float* __restrict__
   store4(dx + int64_t(row) * ldx + (uint32_t(i) - row * k4.div) * 4, s);
 }
 
-// Tables of fewer than 8 rows, which the tiles' loads of 8 columns would pass.
+// Tables of fewer than 8 rows, which the tiles' loads of 8 columns would pass.  The launch begins with
+// block `first`.
 template <class TY, class TX>
 __global__ __launch_bounds__(kBlock) void grad_few(const TY* __restrict__ dy, int64_t ldy, int32_t m,
-                                                   Mx4View w, TX* __restrict__ dx, int64_t ldx) {
+                                                   Mx4View w, TX* __restrict__ dx, int64_t ldx,
+                                                   uint32_t first) {
   const int64_t k4 = w.dim / 4;
-  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+  const int64_t i = (int64_t(first) + blockIdx.x) * kBlock + threadIdx.x;
   if (i >= m * k4) return;
   const int64_t row = i / k4;
   const int e0 = int(i - row * k4) * 4;
@@ -396,9 +399,10 @@ void launch_tile(const GradPlan& p, const void* dy, int64_t ldy, int32_t m, cons
   if (lds > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  hipLaunchKernelGGL(kernel, dim3(p.ktiles * p.mtiles * p.splits), dim3(kBlock), lds, st,
-                     static_cast<const TY*>(dy), ldy, m, w, p.ktiles, p.mtiles, p.per, dx, ldx,
-                     part_stride);
+  for_launches(int64_t(p.ktiles) * p.mtiles * p.splits, kBlock, [&](uint32_t first, dim3 grid) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, st, static_cast<const TY*>(dy), ldy, m, w,
+                       p.ktiles, p.mtiles, p.per, dx, ldx, part_stride, first);
+  });
 }
 
 template <class TY, class TX>
@@ -426,13 +430,15 @@ template <class TX>
 void launch_grad(const GradPlan& p, const void* dy, bool dy_bf16, int64_t ldy, int32_t m,
                  const Mx4View& w, TX* dx, int64_t ldx, float* parts, hipStream_t st) {
   if (p.splits == 0) {  // fewer than 8 rows
-    const dim3 grid(unsigned((int64_t(m) * (w.dim / 4) + kBlock - 1) / kBlock));
-    if (dy_bf16)
-      hipLaunchKernelGGL((grad_few<__bf16, TX>), grid, dim3(kBlock), 0, st,
-                         static_cast<const __bf16*>(dy), ldy, m, w, dx, ldx);
-    else
-      hipLaunchKernelGGL((grad_few<float, TX>), grid, dim3(kBlock), 0, st,
-                         static_cast<const float*>(dy), ldy, m, w, dx, ldx);
+    const int64_t blocks = (int64_t(m) * (w.dim / 4) + kBlock - 1) / kBlock;
+    for_launches(blocks, kBlock, [&](uint32_t first, dim3 grid) {
+      if (dy_bf16)
+        hipLaunchKernelGGL((grad_few<__bf16, TX>), grid, dim3(kBlock), 0, st,
+                           static_cast<const __bf16*>(dy), ldy, m, w, dx, ldx, first);
+      else
+        hipLaunchKernelGGL((grad_few<float, TX>), grid, dim3(kBlock), 0, st,
+                           static_cast<const float*>(dy), ldy, m, w, dx, ldx, first);
+    });
     return;
   }
   if (p.splits == 1) {

@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t quantize8(const T* row, int e0, int k, uint3
 
 // x rounded to the storage of the table: codes [m][groups * 64] (zeros past k), scales as words of
 // 4 blocks [groups][xpitch].  Four lanes per block, as mx4_quantize.  Blocks from `xblocks` on
-// copy W's scales to words [groups][wpitch].
+// copy W's scales to words [groups][wpitch].  The launch begins with block `first`.
 template <class T>
 __global__ __launch_bounds__(kBlock) void pack_x(const T* __restrict__ x, int64_t stride, int32_t m,
                                                  int32_t k, FastDiv groups,
@@ -58,11 +58,12 @@ __global__ __launch_bounds__(kBlock) void pack_x(const T* __restrict__ x, int64_
                                                  uint8_t* __restrict__ scales, int64_t xpitch,
                                                  uint32_t xblocks, const uint32_t* __restrict__ ws,
                                                  int64_t n, uint32_t* __restrict__ ws_out,
-                                                 int64_t wpitch) {
+                                                 int64_t wpitch, uint32_t first) {
   const int G = int(groups.div);
-  if (blockIdx.x >= xblocks) {
+  const uint32_t block = first + blockIdx.x;
+  if (block >= xblocks) {
     // 64 rows, a quarter of the groups for each wavefront, 4 groups at a time.
-    const int64_t row = int64_t(blockIdx.x - xblocks) * kWave + lane_id();
+    const int64_t row = int64_t(block - xblocks) * kWave + lane_id();
     if (row >= n) return;
     const uint32_t* src = ws + row * G;
     for (int g = wave_id() * 4; g < G; g += kWavesPerBlock * 4) {
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(kBlock) void pack_x(const T* __restrict__ x, int64_
     }
     return;
   }
-  const int64_t u = int64_t(blockIdx.x) * (kBlock / 4) + threadIdx.x / 4;
+  const int64_t u = int64_t(block) * (kBlock / 4) + threadIdx.x / 4;
   const int part = threadIdx.x % 4;
   const int64_t g4 = u / 4;
   if (g4 >= int64_t(m) * G) return;
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
 // row l % 16, and of every 4 groups of 128 elements the group l / 16; the four blocks
 // of its group go through four products whose scales are the bytes of one word.  Few elements of x
 // (kFused) are rounded by every block for itself, others by pack_x before.  One row of x, 200003 x
-// 1024: 21 us, 5.2 TB/s; bound by W.
+// 1024: 21 us, 5.2 TB/s; bound by W.  The launch begins with block `first`.
 constexpr int kFused = 8192;  // elements of x, rows padded to groups
 
 template <class TX, class T, bool FUSED>
@@ -405,11 +406,11 @@ __global__ __launch_bounds__(kBlock) void scores_direct(const TX* __restrict__ x
                                                         const uint32_t* __restrict__ xs,
                                                         int64_t xpitch, Mx4View w, int32_t m,
                                                         int32_t groups, T* __restrict__ out,
-                                                        int64_t ldo) {
+                                                        int64_t ldo, uint32_t first) {
   __shared__ __align__(16) uint8_t codes[FUSED ? kFused / 2 : 16];
   __shared__ __align__(16) uint8_t scales[FUSED ? kFused / kMxBlock : 16];
   const int lane = lane_id(), r = lane % 16, q = lane / 16;
-  const int64_t n0 = (int64_t(blockIdx.x) * kWavesPerBlock + wave_id()) * 16;
+  const int64_t n0 = ((int64_t(first) + blockIdx.x) * kWavesPerBlock + wave_id()) * 16;
   const int nb = mx4_blocks(w.dim);
   const int64_t wn = min(n0 + r, w.rows - 1);
   const int xm = min(r, m - 1);
@@ -525,9 +526,10 @@ void launch_tile(const uint8_t* xc, const uint32_t* xs, int32_t m, int32_t group
 template <bool FUSED, class TX, class T>
 void launch_direct(const TX* x, int64_t stride, const uint8_t* xc, const uint32_t* xs, int32_t m,
                    int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
-  const dim3 grid(uint32_t((w.rows + 63) / 64));
-  hipLaunchKernelGGL((scores_direct<TX, T, FUSED>), grid, dim3(kBlock), 0, st, x, stride, xc, xs,
-                     padded(m), w, m, groups, out, ldo);
+  for_launches((w.rows + 63) / 64, kBlock, [&](uint32_t first, dim3 grid) {
+    hipLaunchKernelGGL((scores_direct<TX, T, FUSED>), grid, dim3(kBlock), 0, st, x, stride, xc, xs,
+                       padded(m), w, m, groups, out, ldo, first);
+  });
 }
 
 template <class T>
@@ -592,16 +594,17 @@ hipError_t launch_mx4_matmul(const void* x, bool x_bf16, int64_t x_stride, int32
   const int64_t units = int64_t(m) * groups * 4;
   const uint32_t xblocks = uint32_t((units + kBlock / 4 - 1) / (kBlock / 4));
   const uint32_t wblocks = m > 16 ? uint32_t((w.rows + kWave - 1) / kWave) : 0u;
-  const dim3 pgrid(xblocks + wblocks);
   const FastDiv f = fast_div(uint32_t(groups));
-  if (x_bf16)
-    hipLaunchKernelGGL(pack_x<__bf16>, pgrid, dim3(kBlock), 0, st, static_cast<const __bf16*>(x),
-                       x_stride, m, w.dim, f, xc, xs, padded(m), xblocks, wsc, w.rows, wst,
-                       padded(w.rows));
-  else
-    hipLaunchKernelGGL(pack_x<float>, pgrid, dim3(kBlock), 0, st, static_cast<const float*>(x),
-                       x_stride, m, w.dim, f, xc, xs, padded(m), xblocks, wsc, w.rows, wst,
-                       padded(w.rows));
+  for_launches(int64_t(xblocks) + wblocks, kBlock, [&](uint32_t first, dim3 pgrid) {
+    if (x_bf16)
+      hipLaunchKernelGGL(pack_x<__bf16>, pgrid, dim3(kBlock), 0, st, static_cast<const __bf16*>(x),
+                         x_stride, m, w.dim, f, xc, xs, padded(m), xblocks, wsc, w.rows, wst,
+                         padded(w.rows), first);
+    else
+      hipLaunchKernelGGL(pack_x<float>, pgrid, dim3(kBlock), 0, st, static_cast<const float*>(x),
+                         x_stride, m, w.dim, f, xc, xs, padded(m), xblocks, wsc, w.rows, wst,
+                         padded(w.rows), first);
+  });
   const uint32_t* xsw = reinterpret_cast<const uint32_t*>(xs);
   if (out_bf16)
     launch_scores(xc, xsw, wst, m, groups, w, static_cast<__bf16*>(out), out_stride, st);

@@ -1,5 +1,6 @@
 """Sizes at and past the output head's limits, on the host: what the binding hands to the C ABI."""
 import os
+import subprocess
 from types import SimpleNamespace
 
 import pytest
@@ -56,3 +57,19 @@ def test_a_table_wider_than_32_bits_is_refused():
     dim = 2 ** 32 + 64
     with pytest.raises(ValueError):
         pk.Mx4Table(Fake(1, pk.mx4_code_bytes(dim)), Fake(1, pk.mx4_scale_bytes(dim)), dim)
+
+
+def test_every_launch_is_one_that_hip_takes(tmp_path):
+    """At the limits of every size, by a driver that counts the library's launches instead of making them."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    inc = os.path.join(os.path.dirname(here), "include")
+    rocm, exe = "/opt/rocm", str(tmp_path / "launches")
+    r = subprocess.run(["g++", "-O1", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-rdynamic", "-I", inc, "-I",
+                        os.path.join(rocm, "include"), os.path.join(here, "launch_driver.cpp"), pk.LIB_PATH,
+                        "-L", os.path.join(rocm, "lib"), "-lamdhip64", "-Wl,-rpath," + os.path.dirname(pk.LIB_PATH),
+                        "-Wl,-rpath," + os.path.join(rocm, "lib"), "-Wno-unused-result", "-o", exe],
+                       capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-4000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, (r.stdout[-2000:], r.stderr[-4000:])
+    assert "all launches fit" in r.stdout
