@@ -2,8 +2,8 @@
 top logits, keep a 4-bit copy of it up to date, and serve from the copy.
 
 A request's history (a bag of item ids) is pooled from the FP32 table `items`; its
-scores are the products with all rows of a catalogue kept in 4-bit microscaled
-storage.  A training step is
+scores are the products with all rows of a catalogue (which is not trained) kept in
+4-bit microscaled storage.  A training step is
   embbag_forward -> embbag_mx4_matmul -> embbag_distill -> embbag_mx4_matmul_grad
   -> embbag_backward_sgd -> embbag_mx4_quantize (of the rows the batch touched),
 and serving is

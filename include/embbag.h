@@ -417,7 +417,8 @@ int embbag_mx4_matmul(const void* x, int32_t x_type, int64_t x_stride, int32_t m
  *   dx[i][e] = sum over j of dy[i][j] * W[j][e].
  * `dy`: [m][n] of dy_type, dy_stride >= n, no alignment beyond its elements';
  * `dx`: [m][k] of dx_type, dx_stride and alignment as embbag_mx4_quantize's src.
- * An FP32 dy enters with all its bits (as three BF16 terms); sums are FP32. */
+ * An FP32 dy enters with its bits down to 2^-133 (as three BF16 terms); sums are
+ * FP32. */
 size_t embbag_mx4_matmul_grad_workspace_bytes(int32_t m, int64_t n, int32_t k);
 int embbag_mx4_matmul_grad(const void* dy, int32_t dy_type, int64_t dy_stride, int32_t m,
                            const uint8_t* codes, const uint8_t* scales, int64_t n, int32_t k,

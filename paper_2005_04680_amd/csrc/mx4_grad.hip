@@ -17,9 +17,9 @@
 // the products and the LDS traffic between them; without the interleaving of `part` 409 us.
 // 200 x 50001 x 256: 22 us, bound by its chain of steps.
 //
-// An FP32 dy is the sum of three BF16 terms of 8 bits each, by truncation: three tiles of dy for one of
-// W, whose fragments meet all three (1024 x 20000 x 1024 152 us, with a step of its own for each term 317;
-// 64 x 100000 x 256 26, 43).
+// An FP32 dy is the sum of three BF16 terms of 8 bits each, by truncation (bits below 2^-133, which no
+// BF16 number has, are dropped): three tiles of dy for one of W, whose fragments meet all three (1024 x
+// 20000 x 1024 148 us, with a step of its own for each term 317; 64 x 100000 x 256 25, 43).
 #include "head.hpp"
 
 namespace embbag {

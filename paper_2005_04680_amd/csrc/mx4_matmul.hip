@@ -3,7 +3,7 @@
 // Both sides are blocks of 32 codes with a power of two, which the scaled matrix instructions
 // take as they are: the products are exact and the sums FP32.  Three ways, by the rows of x: up to 16
 // stream W straight into the products (bound by W's bytes), more go through LDS in
-// tiles.  4096 x 65536 x 4096, BF16 in and out: 605 us, 3.6 PFLOP/s, of which 18 us round x and
+// tiles.  4096 x 65536 x 4096, BF16 in and out: 611 us, 3.6 PFLOP/s, of which 18 us round x and
 // copy W's scales; the same instructions from registers reach 5.7 PFLOP/s on such data (8.7 on
 // zeros: the clock falls with the bits that toggle, to 1.9 GHz on average here), a BF16 library
 // product of these sizes takes 1548 us.  With k = 256 the output's bytes bound it (145 us for 537 MB).
