@@ -425,6 +425,91 @@ int embbag_mx4_matmul_grad(const void* dy, int32_t dy_type, int64_t dy_stride, i
                            void* dx, int32_t dx_type, int64_t dx_stride, void* workspace,
                            size_t workspace_bytes, hipStream_t stream);
 
+/* Microscaled 8-bit rows: storage of the head's inputs (OCP Microscaling Formats
+ * v1.0: FP8 E4M3 elements, E8M0 scales, blocks of 32).  `rows` rows of dimension E
+ * (4 <= E <= 16384, E % 4 == 0) are two row-major device arrays:
+ *   codes  [rows][EMBBAG_MX8_CODE_BYTES(E)] uint8, 16-byte aligned: element e in byte
+ *          e; bytes past E are 0 (rows are whole groups of four blocks).
+ *   scales [rows][EMBBAG_MX4_SCALE_BYTES(E)] uint8, 4-byte aligned, as a table's.
+ * A block whose largest magnitude is a has the scale 2^e with the smallest e >= -127
+ * for which a <= 448 * 2^e, and each element x the code nearest to x * 2^-e, ties to
+ * the even code: no element is off by more than half a step.  All-zero blocks and
+ * blocks with an infinity or a NaN as embbag_mx4_quantize's. */
+#define EMBBAG_MX8_CODE_BYTES(E) ((((int64_t)(E) + 127) / 128) * 128)
+
+/* Reads 8-bit rows back as values of dst_type ([rows][dim], dst_stride and alignment
+ * as embbag_mx4_dequantize).  BF16 holds them exactly (above 2^-126). */
+int embbag_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t dim,
+                          void* dst, int32_t dst_type, int64_t dst_stride, hipStream_t stream);
+
+/* RMS norm of rows with the residual's addition.  For every row, in FP32 (the sum of
+ * squares in FP64):
+ *   h = x + residual,   sum_out = h,   out = h / sqrt(mean(h^2) + eps) * weight,
+ * and the 8-bit rows (codes, scales) hold `out` before its own rounding.  Each output
+ * is rounded once, from FP32; `out` comes from the sum before it is rounded.
+ * x [rows][dim] of x_type, residual and sum_out of residual_type, out of out_type:
+ * row strides in elements and alignments as embbag_mx4_quantize's src.  weight [dim]
+ * of weight_type, aligned as a row, null for ones.  eps: positive.  residual, sum_out,
+ * out and the 8-bit rows (both arrays) may each be null, but not all outputs.
+ * sum_out may be residual itself, and out may be x or residual, of the same type and
+ * stride; otherwise outputs must not overlap anything. */
+typedef struct {
+  int64_t rows;
+  int32_t dim;
+  float eps;
+  int32_t x_type;
+  const void* x;
+  int64_t x_stride;
+  int32_t residual_type;
+  const void* residual;
+  int64_t residual_stride;
+  void* sum_out;
+  int64_t sum_stride;
+  int32_t weight_type;
+  const void* weight;
+  int32_t out_type;
+  void* out;
+  int64_t out_stride;
+  uint8_t* codes;
+  uint8_t* scales;
+} embbag_rmsnorm_t;
+
+int embbag_rmsnorm(const embbag_rmsnorm_t* args, hipStream_t stream);
+
+/* Its gradients.  With n = h / sqrt(mean(h^2) + eps) and g = dy * weight,
+ *   dh = (g - n * mean(n * g)) / sqrt(mean(h^2) + eps) + dsum,
+ *   dweight = sum over the rows of dy * n,
+ * where h is the sum that the norm was taken of (sum_out, or x without a residual), dy
+ * the gradient of `out` and dsum that of sum_out (null: 0).  dh is the gradient of x
+ * and of the residual alike.  dy [rows][dim] of dy_type; h, dsum and dh of h_type;
+ * strides and alignments as above; weight as above; dweight [dim] of weight_type (of
+ * dy_type where weight is null), null if it is not wanted.  dh may be dsum, h or dy
+ * itself, of the same type and stride.  FP32 arithmetic, row sums in FP64, dweight
+ * summed in an order that the sizes determine.  `workspace`: 256-byte aligned, needed
+ * for dweight alone. */
+typedef struct {
+  int64_t rows;
+  int32_t dim;
+  float eps;
+  int32_t dy_type;
+  const void* dy;
+  int64_t dy_stride;
+  int32_t h_type;
+  const void* h;
+  int64_t h_stride;
+  int32_t weight_type;
+  const void* weight;
+  const void* dsum;
+  int64_t dsum_stride;
+  void* dh;
+  int64_t dh_stride;
+  void* dweight;
+} embbag_rmsnorm_grad_t;
+
+size_t embbag_rmsnorm_grad_workspace_bytes(int64_t rows, int32_t dim);
+int embbag_rmsnorm_grad(const embbag_rmsnorm_grad_t* args, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+
 /* What may be answered: for every row r and token v of `logits` ([rows][vocab] of
  * `type`, row strides in elements, no alignment beyond the elements'),
  *   l = logits[r][v];

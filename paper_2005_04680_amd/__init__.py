@@ -649,13 +649,15 @@ def embbag_status_read(d_status, stream=None) -> int:
 
 
 # The output head over a table: 4-bit storage, scores, logits, distillation.
-from .head import (EMBBAG_BF16, EMBBAG_F32, Mx4Table, Mx4Tables,  # noqa: E402,F401
+from .head import (EMBBAG_BF16, EMBBAG_F32, Mx4Table, Mx4Tables, Mx8Rows,  # noqa: E402,F401
                    embbag_distill, embbag_distill_workspace_bytes, embbag_logits_process,
                    embbag_mx4_dequantize, embbag_mx4_forward, embbag_mx4_matmul,
                    embbag_mx4_matmul_grad, embbag_mx4_matmul_grad_workspace_bytes,
-                   embbag_mx4_matmul_workspace_bytes, embbag_mx4_quantize, mx4_code_bytes,
-                   mx4_scale_bytes)
+                   embbag_mx4_matmul_workspace_bytes, embbag_mx4_quantize,
+                   embbag_mx8_dequantize, embbag_rmsnorm, embbag_rmsnorm_grad,
+                   embbag_rmsnorm_grad_workspace_bytes, mx4_code_bytes, mx4_scale_bytes,
+                   mx8_code_bytes)
 
 __all__ = [n for n in dir() if n.startswith("embbag_") or n.startswith("EMBBAG_")] + [
-    "lib", "check", "EmbbagError", "LIB_PATH", "Mx4Table", "Mx4Tables",
-    "mx4_code_bytes", "mx4_scale_bytes"]
+    "lib", "check", "EmbbagError", "LIB_PATH", "Mx4Table", "Mx4Tables", "Mx8Rows",
+    "mx4_code_bytes", "mx4_scale_bytes", "mx8_code_bytes"]

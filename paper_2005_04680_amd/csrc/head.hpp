@@ -184,6 +184,48 @@ hipError_t launch_mx4_matmul_grad(const void* dy, bool dy_bf16, int64_t dy_strid
 
 hipError_t launch_logits(const embbag_logits_t& a, int32_t* status, hipStream_t st);
 
+// RMS norm: h = x + residual; sum_out = h, out and 8-bit rows = h / sqrt(mean(h^2) + eps) * weight.
+// Null outputs, residual and weight are left out; per = 1 / dim.
+struct NormArgs {
+  int64_t rows;
+  int32_t dim;
+  bool weight_bf16;
+  double per, eps;
+  const void* x;
+  int64_t x_stride;
+  const void* residual;
+  int64_t residual_stride;
+  void* sum_out;
+  int64_t sum_stride;
+  const void* weight;
+  void* out;
+  int64_t out_stride;
+  uint8_t* codes;
+  uint8_t* scales;
+};
+struct NormGradArgs {
+  int64_t rows;
+  int32_t dim;
+  bool weight_bf16;
+  double per, eps;
+  const void* dy;
+  int64_t dy_stride;
+  const void* h;
+  int64_t h_stride;
+  const void* weight;
+  const void* dsum;
+  int64_t dsum_stride;
+  void* dh;
+  int64_t dh_stride;
+  float* parts;
+};
+hipError_t launch_rmsnorm(const NormArgs& a, bool x_bf16, bool r_bf16, bool out_bf16, hipStream_t st);
+size_t rmsnorm_grad_workspace(int64_t rows, int32_t dim);
+hipError_t launch_rmsnorm_grad(NormGradArgs a, bool y_bf16, bool h_bf16, void* dweight, char* ws,
+                               hipStream_t st);
+hipError_t launch_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
+                                 int32_t dim, void* dst, bool bf16, int64_t dst_stride, hipStream_t st);
+
 size_t distill_workspace(int32_t rows, int32_t vocab, int32_t top);
 hipError_t launch_distill(const embbag_distill_t& a, char* ws, int32_t* status, hipStream_t st);
 

@@ -39,6 +39,15 @@ bool product_ok(int32_t m, int64_t n, int32_t k) {
   return m >= 0 && m <= kMaxRowsX && n >= 1 && n <= kInt32Max && dim_ok(k) && m * n <= kMaxMatrix;
 }
 
+bool mx8_ok(const uint8_t* codes, const uint8_t* scales) {
+  return codes != nullptr && scales != nullptr && aligned(codes, 16) && aligned(scales, 4);
+}
+
+// The vector of a norm's weights or of their gradient (null: none).
+bool weight_ok(const void* p, int32_t type) { return aligned(p, 4 * type_size(type)); }
+
+bool eps_ok(float eps) { return eps > 0.f && eps <= 3.4028234663852886e38f; }
+
 // A list per row (offsets, entries) of n entries, fewer than 2^30: occurrences are counted in
 // 30 bits.
 int check_list(int32_t rows, const int32_t* offsets, const void* entries, int64_t n) {
@@ -153,6 +162,90 @@ int embbag_mx4_matmul_grad(const void* dy, int32_t dy_type, int64_t dy_stride, i
   return hip_status(launch_mx4_matmul_grad(dy, dy_type == EMBBAG_BF16, dy_stride, m,
                                            {codes, scales, n, k}, dx, dx_type == EMBBAG_BF16,
                                            dx_stride, static_cast<char*>(workspace), stream));
+}
+
+int embbag_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t dim,
+                          void* dst, int32_t dst_type, int64_t dst_stride, hipStream_t stream) {
+  if (rows < 0 || rows > kInt32Max || !dim_ok(dim)) return EMBBAG_ERR_INVALID_ARG;
+  if (rows > 0 && (!mx8_ok(codes, scales) || !rows_ok(dst, dst_type, dst_stride, dim)))
+    return EMBBAG_ERR_INVALID_ARG;
+  return hip_status(launch_mx8_dequantize(codes, scales, rows, dim, dst, dst_type == EMBBAG_BF16,
+                                          dst_stride, stream));
+}
+
+int embbag_rmsnorm(const embbag_rmsnorm_t* args, hipStream_t stream) {
+  if (args == nullptr) return EMBBAG_ERR_INVALID_ARG;
+  const embbag_rmsnorm_t& a = *args;
+  if (a.rows < 0 || a.rows > kInt32Max || !dim_ok(a.dim) || !eps_ok(a.eps) || !type_ok(a.x_type) ||
+      !type_ok(a.residual_type) || !type_ok(a.weight_type) || !type_ok(a.out_type))
+    return EMBBAG_ERR_INVALID_ARG;
+  if (a.rows == 0) return EMBBAG_OK;
+  if (a.sum_out == nullptr && a.out == nullptr && a.codes == nullptr) return EMBBAG_ERR_INVALID_ARG;
+  if (!rows_ok(a.x, a.x_type, a.x_stride, a.dim) ||
+      (a.residual != nullptr && !rows_ok(a.residual, a.residual_type, a.residual_stride, a.dim)) ||
+      (a.sum_out != nullptr && !rows_ok(a.sum_out, a.residual_type, a.sum_stride, a.dim)) ||
+      (a.out != nullptr && !rows_ok(a.out, a.out_type, a.out_stride, a.dim)) ||
+      !weight_ok(a.weight, a.weight_type))
+    return EMBBAG_ERR_INVALID_ARG;
+  if ((a.codes != nullptr || a.scales != nullptr) && !mx8_ok(a.codes, a.scales))
+    return EMBBAG_ERR_INVALID_ARG;
+  // An output that is an input: the same rows.
+  auto same = [&](const void* p, int32_t pt, int64_t ps, const void* q, int32_t qt, int64_t qs) {
+    return p == nullptr || p != q || (pt == qt && (ps == qs || a.rows == 1));
+  };
+  if (!same(a.sum_out, a.residual_type, a.sum_stride, a.residual, a.residual_type, a.residual_stride) ||
+      !same(a.sum_out, a.residual_type, a.sum_stride, a.x, a.x_type, a.x_stride) ||
+      !same(a.out, a.out_type, a.out_stride, a.x, a.x_type, a.x_stride) ||
+      !same(a.out, a.out_type, a.out_stride, a.residual, a.residual_type, a.residual_stride) ||
+      (a.out != nullptr && a.out == a.sum_out))
+    return EMBBAG_ERR_INVALID_ARG;
+  NormArgs n = {a.rows,       a.dim,        a.weight_type == EMBBAG_BF16,
+                1.0 / a.dim,  double(a.eps), a.x,
+                a.x_stride,   a.residual,   a.residual_stride,
+                a.sum_out,    a.sum_stride, a.weight,
+                a.out,        a.out_stride, a.codes,
+                a.scales};
+  return hip_status(launch_rmsnorm(n, a.x_type == EMBBAG_BF16, a.residual_type == EMBBAG_BF16,
+                                   a.out_type == EMBBAG_BF16, stream));
+}
+
+size_t embbag_rmsnorm_grad_workspace_bytes(int64_t rows, int32_t dim) {
+  return rows >= 0 && rows <= kInt32Max && dim_ok(dim) ? rmsnorm_grad_workspace(rows, dim) : 0;
+}
+
+int embbag_rmsnorm_grad(const embbag_rmsnorm_grad_t* args, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+  if (args == nullptr) return EMBBAG_ERR_INVALID_ARG;
+  const embbag_rmsnorm_grad_t& a = *args;
+  if (a.rows < 0 || a.rows > kInt32Max || !dim_ok(a.dim) || !eps_ok(a.eps) || !type_ok(a.dy_type) ||
+      !type_ok(a.h_type) || !type_ok(a.weight_type) || !weight_ok(a.weight, a.weight_type))
+    return EMBBAG_ERR_INVALID_ARG;
+  const int32_t dw_type = a.weight != nullptr ? a.weight_type : a.dy_type;
+  if (!weight_ok(a.dweight, dw_type)) return EMBBAG_ERR_INVALID_ARG;
+  if (a.rows > 0) {
+    if (!rows_ok(a.dy, a.dy_type, a.dy_stride, a.dim) || !rows_ok(a.h, a.h_type, a.h_stride, a.dim) ||
+        !rows_ok(a.dh, a.h_type, a.dh_stride, a.dim) ||
+        (a.dsum != nullptr && !rows_ok(a.dsum, a.h_type, a.dsum_stride, a.dim)))
+      return EMBBAG_ERR_INVALID_ARG;
+    auto same = [&](const void* q, int32_t qt, int64_t qs) {
+      return a.dh != q || (a.h_type == qt && (a.dh_stride == qs || a.rows == 1));
+    };
+    if (!same(a.dy, a.dy_type, a.dy_stride) || !same(a.h, a.h_type, a.h_stride) ||
+        !same(a.dsum, a.h_type, a.dsum_stride))
+      return EMBBAG_ERR_INVALID_ARG;
+  }
+  if (a.dweight != nullptr) {
+    const size_t need = rmsnorm_grad_workspace(a.rows, a.dim);
+    if (workspace_bytes < need || !aligned(workspace, kWsAlign) || (workspace == nullptr && need > 0))
+      return EMBBAG_ERR_WORKSPACE;
+  }
+  NormGradArgs n = {a.rows,      a.dim,         dw_type == EMBBAG_BF16,
+                    1.0 / a.dim, double(a.eps), a.dy,
+                    a.dy_stride, a.h,           a.h_stride,
+                    a.weight,    a.dsum,        a.dsum_stride,
+                    a.dh,        a.dh_stride,   nullptr};
+  return hip_status(launch_rmsnorm_grad(n, a.dy_type == EMBBAG_BF16, a.h_type == EMBBAG_BF16, a.dweight,
+                                        static_cast<char*>(workspace), stream));
 }
 
 int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStream_t stream) {

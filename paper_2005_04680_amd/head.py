@@ -4,7 +4,9 @@ other entry points (device pointers and the current HIP stream to the C ABI of
 
 4-bit microscaled tables (``Mx4Table``, ``Mx4Tables``): ``embbag_mx4_quantize``,
 ``embbag_mx4_dequantize``, ``embbag_mx4_forward`` (bags), ``embbag_mx4_matmul``
-(scores of every row) and ``embbag_mx4_matmul_grad``.  Logits:
+(scores of every row) and ``embbag_mx4_matmul_grad``.  Between rows and scores:
+``embbag_rmsnorm`` (into FP32, BF16 or 8-bit rows, ``Mx8Rows``), ``embbag_rmsnorm_grad``,
+``embbag_mx8_dequantize``.  Logits:
 ``embbag_logits_process`` (penalties, biases, masks) and ``embbag_distill`` (loss
 and gradient against a teacher's top logits).
 """
@@ -46,6 +48,25 @@ class _Distill(C.Structure):
                 ("grad", C.c_void_p), ("grad_stride", C.c_int64)]
 
 
+class _RmsNorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("eps", C.c_float),
+                ("x_type", C.c_int32), ("x", C.c_void_p), ("x_stride", C.c_int64),
+                ("residual_type", C.c_int32), ("residual", C.c_void_p),
+                ("residual_stride", C.c_int64), ("sum_out", C.c_void_p), ("sum_stride", C.c_int64),
+                ("weight_type", C.c_int32), ("weight", C.c_void_p), ("out_type", C.c_int32),
+                ("out", C.c_void_p), ("out_stride", C.c_int64), ("codes", C.c_void_p),
+                ("scales", C.c_void_p)]
+
+
+class _RmsNormGrad(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("eps", C.c_float),
+                ("dy_type", C.c_int32), ("dy", C.c_void_p), ("dy_stride", C.c_int64),
+                ("h_type", C.c_int32), ("h", C.c_void_p), ("h_stride", C.c_int64),
+                ("weight_type", C.c_int32), ("weight", C.c_void_p), ("dsum", C.c_void_p),
+                ("dsum_stride", C.c_int64), ("dh", C.c_void_p), ("dh_stride", C.c_int64),
+                ("dweight", C.c_void_p)]
+
+
 # A call's arguments as the bytes of its structure (0.2 us; a ctypes object of 22 fields 1.0).
 _CODES = {C.c_int32: "i", C.c_int64: "q", C.c_void_p: "P", C.c_float: "f"}
 
@@ -63,6 +84,7 @@ def _packer(cls):
 
 
 _pack_logits, _pack_distill = _packer(_Logits), _packer(_Distill)
+_pack_norm, _pack_norm_grad = _packer(_RmsNorm), _packer(_RmsNormGrad)
 
 _ready = None
 
@@ -84,10 +106,14 @@ def _lib():
         L.embbag_logits_process.argtypes = [p, p, p]
         L.embbag_distill_workspace_bytes.argtypes = [i32, i32, i32]
         L.embbag_distill.argtypes = [p, p, sz, p, p]
-        for n in ("mx4_quantize", "mx4_dequantize", "mx4_forward", "mx4_matmul",
+        L.embbag_mx8_dequantize.argtypes = [p, p, i64, i32, p, i32, i64, p]
+        L.embbag_rmsnorm.argtypes = [p, p]
+        L.embbag_rmsnorm_grad_workspace_bytes.argtypes = [i64, i32]
+        L.embbag_rmsnorm_grad.argtypes = [p, p, sz, p]
+        for n in ("mx8_dequantize", "rmsnorm", "rmsnorm_grad", "mx4_quantize", "mx4_dequantize", "mx4_forward", "mx4_matmul",
                   "mx4_matmul_grad", "logits_process", "distill"):
             getattr(L, "embbag_" + n).restype = C.c_int
-        for n in ("mx4_matmul", "mx4_matmul_grad", "distill"):
+        for n in ("rmsnorm_grad", "mx4_matmul", "mx4_matmul_grad", "distill"):
             getattr(L, f"embbag_{n}_workspace_bytes").restype = sz
         _ready = L
     return _ready
@@ -214,6 +240,36 @@ class Mx4Table:
                    torch.zeros(rows, mx4_scale_bytes(dim), dtype=torch.uint8, device=device), dim)
 
 
+def mx8_code_bytes(dim: int) -> int:
+    """Bytes of a row of 8-bit codes (EMBBAG_MX8_CODE_BYTES)."""
+    return (dim + 127) // 128 * 128
+
+
+class Mx8Rows:
+    """8-bit microscaled rows: ``codes`` [rows, mx8_code_bytes(dim)] and ``scales``
+    [rows, mx4_scale_bytes(dim)], contiguous uint8 GPU tensors, which must keep
+    their storage while the object is in use."""
+
+    def __init__(self, codes, scales, dim):
+        dim = int(dim)
+        _need(dim < 2 ** 31, f"dim: {dim} does not fit 32 bits")
+        _need(len(codes.shape) == 2 and codes.shape[1] == mx8_code_bytes(dim),
+              f"codes: shape {tuple(codes.shape)}, expected [rows, {mx8_code_bytes(dim)}]")
+        _need(tuple(scales.shape) == (codes.shape[0], mx4_scale_bytes(dim)),
+              f"scales: shape {tuple(scales.shape)}, expected "
+              f"[{codes.shape[0]}, {mx4_scale_bytes(dim)}]")
+        self.codes_ptr = _ptr(codes, _dt("uint8"), "codes")
+        self.scales_ptr = _ptr(scales, _dt("uint8"), "scales")
+        self.codes, self.scales, self.dim, self.rows = codes, scales, dim, int(codes.shape[0])
+
+    @classmethod
+    def empty(cls, rows, dim, device="cuda"):
+        """Rows of zeros."""
+        import torch
+        return cls(torch.zeros(rows, mx8_code_bytes(dim), dtype=torch.uint8, device=device),
+                   torch.zeros(rows, mx4_scale_bytes(dim), dtype=torch.uint8, device=device), dim)
+
+
 class Mx4Tables:
     """Microscaled tables of one width with their C descriptor built once."""
 
@@ -308,6 +364,78 @@ def embbag_mx4_matmul_grad(dy, table, dx, workspace, stream=None) -> int:
     w, n = _ws(workspace)
     return _lib().embbag_mx4_matmul_grad(p, ty, ld, _i32(m), table.codes_ptr, table.scales_ptr,
                                          table.rows, table.dim, q, tq, lq, w, n, _stream(stream))
+
+
+def embbag_mx8_dequantize(rows8, dst, stream=None) -> int:
+    """All rows of ``rows8`` (``Mx8Rows``) as values into ``dst`` ([rows, dim] FP32 or BF16)."""
+    p, ty, ld = _matrix(dst, rows8.dim, "dst")
+    _check_rows(dst, rows8.rows, "dst")
+    return _lib().embbag_mx8_dequantize(rows8.codes_ptr, rows8.scales_ptr, rows8.rows, rows8.dim, p,
+                                        ty, ld, _stream(stream))
+
+
+def _weight(t, dim, name):
+    """(pointer, type) of a vector of `dim` weights (None: none)."""
+    if t is None:
+        return 0, EMBBAG_F32
+    code = _type_of.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected float32 or bfloat16")
+    return _vector(t, dim, name, t.dtype), code
+
+
+def _same_rows(t, rows, cols, name, code=None, like=""):
+    """_matrix of a tensor of `rows` rows, of the type `code` (None: any; no tensor: zeros)."""
+    if t is None:
+        return 0, EMBBAG_F32 if code is None else code, 0
+    m = _matrix(t, cols, name)
+    _check_rows(t, rows, name)
+    if code is not None and m[1] != code:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected that of {like}")
+    return m
+
+
+def embbag_rmsnorm(x, weight, eps, out=None, mx8=None, residual=None, sum_out=None, stream=None) -> int:
+    """RMS norm of ``x`` [rows, dim] plus ``residual``, times ``weight`` ([dim], None: ones), into
+    ``out`` and/or the 8-bit rows ``mx8`` (``Mx8Rows``); the sum itself into ``sum_out`` (which may
+    be ``residual``, and has its type)."""
+    dim = x.shape[1] if len(x.shape) == 2 else -1
+    p, ty, ld = _matrix(x, dim, "x")
+    rows = x.shape[0]
+    r, tr, lr = _same_rows(residual, rows, dim, "residual")
+    s, ts, ls = _same_rows(sum_out, rows, dim, "sum_out", None if residual is None else tr, "residual")
+    q, tq, lq = _same_rows(out, rows, dim, "out")
+    w, tw = _weight(weight, dim, "weight")
+    codes = scales = 0
+    if mx8 is not None:
+        if mx8.rows != rows or mx8.dim != dim:
+            raise ValueError(f"mx8: {mx8.rows} rows of {mx8.dim}, expected {rows} of {dim}")
+        codes, scales = mx8.codes_ptr, mx8.scales_ptr
+    a = _pack_norm(rows, dim, eps, ty, p, ld, ts, r, lr, s, ls, tw, w, tq, q, lq, codes, scales)
+    return _lib().embbag_rmsnorm(a, _stream(stream))
+
+
+def embbag_rmsnorm_grad_workspace_bytes(rows, dim) -> int:
+    return int(_lib().embbag_rmsnorm_grad_workspace_bytes(int(rows), _i32(int(dim))))
+
+
+def embbag_rmsnorm_grad(dy, h, weight, eps, dh, workspace, dweight=None, dsum=None, stream=None) -> int:
+    """Gradients of ``embbag_rmsnorm``: ``dh`` (that of x and of the residual) and ``dweight`` from the
+    output's gradient ``dy``, the sum ``h`` and the sum's own gradient ``dsum``."""
+    dim = h.shape[1] if len(h.shape) == 2 else -1
+    p, th, lh = _matrix(h, dim, "h")
+    rows = h.shape[0]
+    y, ty, ly = _same_rows(dy, rows, dim, "dy")
+    d, _, ld = _same_rows(dh, rows, dim, "dh", th, "h")
+    s, _, ls = _same_rows(dsum, rows, dim, "dsum", th, "h")
+    w, tw = _weight(weight, dim, "weight")
+    g, tg = _weight(dweight, dim, "dweight")
+    if dweight is not None and tg != (ty if weight is None else tw):
+        raise TypeError(f"dweight: dtype {dweight.dtype}, expected that of "
+                        f"{'dy' if weight is None else 'weight'}")
+    a = _pack_norm_grad(rows, dim, eps, ty, y, ly, th, p, lh, tw, w, s, ls, d, ld, g)
+    ws, n = _ws(workspace)
+    return _lib().embbag_rmsnorm_grad(a, ws, n, _stream(stream))
 
 
 def embbag_logits_process(logits, out, seen=None, seen_offsets=None, prompt_lens=None,
