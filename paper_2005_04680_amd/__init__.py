@@ -653,7 +653,8 @@ from .head import (EMBBAG_BF16, EMBBAG_F32, Mx4Table, Mx4Tables, Mx8Rows,  # noq
                    embbag_distill, embbag_distill_workspace_bytes, embbag_logits_process,
                    embbag_mx4_dequantize, embbag_mx4_forward, embbag_mx4_matmul,
                    embbag_mx4_matmul_grad, embbag_mx4_matmul_grad_workspace_bytes,
-                   embbag_mx4_matmul_workspace_bytes, embbag_mx4_quantize,
+                   embbag_mx4_matmul_workspace_bytes, embbag_mx4_matmul_x8,
+                   embbag_mx4_matmul_x8_workspace_bytes, embbag_mx4_quantize,
                    embbag_mx8_dequantize, embbag_rmsnorm, embbag_rmsnorm_grad,
                    embbag_rmsnorm_grad_workspace_bytes, mx4_code_bytes, mx4_scale_bytes,
                    mx8_code_bytes)

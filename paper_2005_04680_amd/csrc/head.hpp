@@ -177,6 +177,11 @@ size_t mx4_matmul_workspace(int32_t m, int64_t n, int32_t k);
 hipError_t launch_mx4_matmul(const void* x, bool x_bf16, int64_t x_stride, int32_t m,
                              const Mx4View& w, void* out, bool out_bf16, int64_t out_stride,
                              char* ws, hipStream_t st);
+// The same from 8-bit rows.
+size_t mx4_matmul_x8_workspace(int32_t m, int64_t n, int32_t k);
+hipError_t launch_mx4_matmul_x8(const uint8_t* xc, const uint8_t* xs, int32_t m, const Mx4View& w,
+                                void* out, bool out_bf16, int64_t out_stride, char* ws,
+                                hipStream_t st);
 size_t mx4_matmul_grad_workspace(int32_t m, int64_t n, int32_t k);
 hipError_t launch_mx4_matmul_grad(const void* dy, bool dy_bf16, int64_t dy_stride, int32_t m,
                                   const Mx4View& w, void* dx, bool dx_bf16, int64_t dx_stride,

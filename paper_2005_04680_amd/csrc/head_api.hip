@@ -144,6 +144,26 @@ int embbag_mx4_matmul(const void* x, int32_t x_type, int64_t x_stride, int32_t m
                                       static_cast<char*>(workspace), stream));
 }
 
+size_t embbag_mx4_matmul_x8_workspace_bytes(int32_t m, int64_t n, int32_t k) {
+  return product_ok(m, n, k) ? mx4_matmul_x8_workspace(m, n, k) : 0;
+}
+
+int embbag_mx4_matmul_x8(const uint8_t* x_codes, const uint8_t* x_scales, int32_t m,
+                         const uint8_t* codes, const uint8_t* scales, int64_t n, int32_t k, void* out,
+                         int32_t out_type, int64_t out_stride, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  if (!product_ok(m, n, k) || !table_ok(codes, scales, n, k) || !type_ok(out_type))
+    return EMBBAG_ERR_INVALID_ARG;
+  if (m > 0 && (!mx8_ok(x_codes, x_scales) || !matrix_ok(out, out_type, out_stride, n)))
+    return EMBBAG_ERR_INVALID_ARG;
+  const size_t need = mx4_matmul_x8_workspace(m, n, k);
+  if (workspace_bytes < need || !aligned(workspace, kWsAlign) || (workspace == nullptr && need > 0))
+    return EMBBAG_ERR_WORKSPACE;
+  return hip_status(launch_mx4_matmul_x8(x_codes, x_scales, m, {codes, scales, n, k}, out,
+                                         out_type == EMBBAG_BF16, out_stride,
+                                         static_cast<char*>(workspace), stream));
+}
+
 size_t embbag_mx4_matmul_grad_workspace_bytes(int32_t m, int64_t n, int32_t k) {
   return product_ok(m, n, k) ? mx4_matmul_grad_workspace(m, n, k) : 0;
 }

@@ -9,6 +9,15 @@
 // product of these sizes takes 1548 us.  With k = 256 the output's bytes bound it (145 us for 537 MB).
 // Outputs whose rows do not begin at 128-byte lines are slower there: 2889 x 89088 x 64 into BF16 110
 // us, 2889 x 89061 178; the L2s' write requests grow by half.
+//
+// x may come as 8-bit rows instead (E4M3 codes, twice the bytes): the same kernels with X8.  Products
+// of an 8-bit and a 4-bit side run at the 8-bit rate, half the 4-bit one, but the scaled instructions
+// add eight products at a time, aligned to the largest of them, and drop what lies more than 13 bits below
+// it (measured).  4-bit sides have no such bits; an 8-bit side does: sums over a norm's rows are off by 3e-6 of
+// themselves, far below a BF16 output's rounding.  Into FP32 the values of both sides, which BF16 holds
+// exactly, go through the BF16 instructions.
+#include <type_traits>
+
 #include "head.hpp"
 
 namespace embbag {
@@ -22,6 +31,22 @@ typedef u4 u4_word __attribute__((aligned(4)));
 __device__ __forceinline__ i8v frag8(const u4& v) {
   return i8v{int(v.x), int(v.y), int(v.z), int(v.w), 0, 0, 0, 0};
 }
+// One of 32 8-bit codes: of a product's elements in order, 16 bytes per lane group of its first half,
+// then of its second.
+struct Bytes32 {
+  u4 lo, hi;
+};
+__device__ __forceinline__ i8v frag8(const Bytes32& v) {
+  return i8v{int(v.lo.x), int(v.lo.y), int(v.lo.z), int(v.lo.w),
+             int(v.hi.x), int(v.hi.y), int(v.hi.z), int(v.hi.w)};
+}
+// The side of x: 8-bit rows (X8) or codes of 4 bits.
+template <bool X8>
+using XFrag = std::conditional_t<X8, Bytes32, u4>;
+template <bool X8>
+constexpr int kXFormat = X8 ? 0 : 4;  // E4M3, E2M1
+template <bool X8>
+constexpr int kXRow = X8 ? 128 : 64;  // bytes of a row per step
 
 constexpr int kGroup = 128;      // elements of a step: 4 blocks, whose scales are one word
 constexpr int kGroupBytes = 64;  // their codes
@@ -48,6 +73,56 @@ __device__ __forceinline__ uint32_t quantize8(const T* row, int e0, int k, uint3
   return *byte == 255u ? 0u : mx4_codes8(y);
 }
 
+// Whether the products run on BF16 values of both sides.
+template <bool X8, class T>
+constexpr bool kExact = X8 && sizeof(T) == 4;
+
+// Values of 32 codes, in order, as the operands of four BF16 products.
+__device__ __forceinline__ void bf16_values(const u4& c, uint32_t scale, u4 (&v)[4]) {
+  const float s = mx4_scale(scale);
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    v[t] = u4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[t], s, 0)),
+              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[t], s, 1)),
+              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[t], s, 2)),
+              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[t], s, 3))};
+}
+__device__ __forceinline__ void bf16_values(const Bytes32& c, uint32_t scale, u4 (&v)[4]) {
+  const float s = mx4_scale(scale);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const u4& q = t < 2 ? c.lo : c.hi;
+    const uint32_t a = q[t % 2 * 2], b = q[t % 2 * 2 + 1];
+    v[t] = u4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false)),
+              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true)),
+              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, false)),
+              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true))};
+  }
+}
+
+// Block number `block` of a copy of scales [rows][G] to words [G][pitch]: 64 rows, a quarter of the
+// groups for each wavefront, 4 groups at a time.
+__device__ __forceinline__ void copy_scales(uint32_t block, const uint32_t* __restrict__ scales,
+                                            int64_t rows, int G, uint32_t* __restrict__ out,
+                                            int64_t pitch) {
+  const int64_t row = int64_t(block) * kWave + lane_id();
+  if (row >= rows) return;
+  const uint32_t* src = scales + row * G;
+  for (int g = wave_id() * 4; g < G; g += kWavesPerBlock * 4) {
+    uint32_t v[4];
+    if (G % 4 == 0) {
+      const u4 q = *reinterpret_cast<const u4_word*>(src + g);
+      v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = g + i < G ? src[g + i] : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (g + i < G) out[(g + i) * pitch + row] = v[i];
+  }
+}
+
 // x rounded to the storage of the table: codes [m][groups * 64] (zeros past k), scales as words of
 // 4 blocks [groups][xpitch].  Four lanes per block, as mx4_quantize.  Blocks from `xblocks` on
 // copy W's scales to words [groups][wpitch].  The launch begins with block `first`.
@@ -62,23 +137,7 @@ __global__ __launch_bounds__(kBlock) void pack_x(const T* __restrict__ x, int64_
   const int G = int(groups.div);
   const uint32_t block = first + blockIdx.x;
   if (block >= xblocks) {
-    // 64 rows, a quarter of the groups for each wavefront, 4 groups at a time.
-    const int64_t row = int64_t(block - xblocks) * kWave + lane_id();
-    if (row >= n) return;
-    const uint32_t* src = ws + row * G;
-    for (int g = wave_id() * 4; g < G; g += kWavesPerBlock * 4) {
-      uint32_t v[4];
-      if (G % 4 == 0) {
-        const u4 q = *reinterpret_cast<const u4_word*>(src + g);
-        v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = g + i < G ? src[g + i] : 0u;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (g + i < G) ws_out[(g + i) * wpitch + row] = v[i];
-    }
+    copy_scales(block - xblocks, ws, n, G, ws_out, wpitch);
     return;
   }
   const int64_t u = int64_t(block) * (kBlock / 4) + threadIdx.x / 4;
@@ -91,6 +150,19 @@ __global__ __launch_bounds__(kBlock) void pack_x(const T* __restrict__ x, int64_
   const uint32_t c = quantize8(x + int64_t(row) * stride, g * kGroup + j * kMxBlock + part * 8, k, &byte);
   *reinterpret_cast<uint32_t*>(codes + (int64_t(row) * G + g) * kGroupBytes + j * 16 + part * 4) = c;
   if (part == 0) scales[(int64_t(g) * xpitch + row) * 4 + j] = uint8_t(byte);
+}
+
+// The scales of 8-bit rows, and from block `xblocks` on W's, to words of 4 blocks [groups][pitch].
+__global__ __launch_bounds__(kBlock) void pack_scales(const uint32_t* __restrict__ xs, int64_t m,
+                                                      uint32_t* __restrict__ xs_out, int64_t xpitch,
+                                                      uint32_t xblocks, const uint32_t* __restrict__ ws,
+                                                      int64_t n, uint32_t* __restrict__ ws_out,
+                                                      int64_t wpitch, int G, uint32_t first) {
+  const uint32_t block = first + blockIdx.x;
+  if (block < xblocks)
+    copy_scales(block, xs, m, G, xs_out, xpitch);
+  else
+    copy_scales(block - xblocks, ws, n, G, ws_out, wpitch);
 }
 
 // 16 or 4 bytes per lane from memory to LDS, lane l's at `dst` + 16 l (4 l).
@@ -153,20 +225,26 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t mtiles, uint32_t n
 // steps of all of them: those of the next tile are on their way while a tile is stored.
 //
 // 256 x 256 tiles keep the accumulators of a wavefront in 256 registers and read each fragment
-// from LDS for four products.  Left out one at a time at 4096 x 65536 x 4096 (633 us with
+// from LDS for four products.
+//
+// 8-bit rows (X8): a load brings 8 rows of 128 bytes, place j of row r holds chunk j ^ (r % 8); a
+// fragment is two chunks, 16 elements of the product's first block and 16 of its second.
+//
+// Left out one at a time at 4096 x 65536 x 4096 (633 us with
 // strips of 8): loads to LDS 457, stores of the output 533, LDS reads and loads and stores 315.
-template <int TN, int TM, int WN, int WM, int STAGES, class T>
+template <bool X8, int TN, int TM, int WN, int WM, int STAGES, class T>
 __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     const uint8_t* __restrict__ xc, const uint32_t* __restrict__ xs, int64_t xpitch, int32_t m,
     int32_t steps, Mx4View w, const uint32_t* __restrict__ ws, int64_t wpitch, uint32_t mtiles,
     uint32_t ntiles, T* __restrict__ out, int64_t ldo) {
   constexpr int BN = 32 * TN * WN, BM = 32 * TM * WM, W = WN * WM;
-  constexpr int LOADS = (BN + BM) / 16 / W;   // codes, per wavefront and step
+  constexpr int XROW = kXRow<X8>, XROWS = 1024 / XROW;  // bytes per row, rows per load of x
+  constexpr int LOADS = (BN / 16 + BM / XROWS) / W;     // codes, per wavefront and step
   constexpr int SALL = (BN + BM) / 64;        // of scales, in the block
   constexpr int SLOADS = (SALL + W - 1) / W;  // per wavefront (the last ones may come twice)
-  static_assert(BN % (16 * W) == 0 && BM % (16 * W) == 0 && BN % 64 == 0, "whole loads");
+  static_assert(BN % (16 * W) == 0 && BM % (XROWS * W) == 0 && BN % 64 == 0, "whole loads");
   constexpr int WLOADS = BN / 16 / W;         // codes of W's rows, which come first
-  constexpr int CODES = (BN + BM) * kGroupBytes;
+  constexpr int CODES = BN * kGroupBytes + BM * XROW;
   constexpr int STAGE = CODES + (BN + BM) * 4;
   constexpr int V = kVec<T>;
   constexpr int TILES = turn_tiles<T>(TN), PITCH = 32 * TILES + V;
@@ -176,7 +254,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   const int lane = lane_id(), wave = wave_id();
   T* turn = reinterpret_cast<T*>(lds + STAGES * STAGE) + wave * 32 * PITCH;
   const int nb = mx4_blocks(w.dim);
-  const int64_t xrow = int64_t(steps) * kGroupBytes, wrow = int64_t(nb) * 16;
+  const int64_t xrow = int64_t(steps) * XROW, wrow = int64_t(nb) * 16;
   // This block's tiles: from `tile` on every `stride`-th below `end`.
   const uint32_t tiles = mtiles * ntiles, range = (tiles + kNumXcd - 1) / kNumXcd;
   const uint32_t stride = gridDim.x / kNumXcd;
@@ -189,6 +267,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   // 16 * (i * W + wave) .. + 15 of the stage (W's rows, then x's); rows past the end repeat
   // the last one.
   const int c = (lane % 4) ^ (lane / 16);
+  const int cx8 = (lane % 8) ^ (lane / 8);
   uint32_t ltile = tile;
   int lstep = 0;
   const uint8_t *wbase, *xbase;
@@ -214,9 +293,13 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     }
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int r = 16 * (i * W + wave) + lane / 4;
-      off[i] = i < WLOADS ? uint32_t(min(int64_t(r), w.rows - 1 - n0) * wrow)
-                          : uint32_t(min(r - BN, m - 1 - m0) * xrow + c * 16);
+      if (i < WLOADS) {
+        const int r = 16 * (i * W + wave) + lane / 4;
+        off[i] = uint32_t(min(int64_t(r), w.rows - 1 - n0) * wrow);
+      } else {
+        const int r = XROWS * ((i - WLOADS) * W + wave) + lane / (64 / XROWS);
+        off[i] = uint32_t(min(r, m - 1 - m0) * xrow + (X8 ? cx8 : c) * 16);
+      }
     }
   };
   // Before a step's loads.  After the last tile its steps are loaded again, so that the number
@@ -235,11 +318,12 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   constexpr int PER = LOADS + SLOADS;
   auto load = [&](uint8_t* dst, int i) {
     if (i < LOADS) {
-      const int r0 = 16 * (i * W + wave);
       // (A block past W's row is its last one: x's codes are 0 there, and W's scale.)
       const uint32_t wk = uint32_t(min(lstep * 4 + c, nb - 1)) * 16;
-      const uint32_t xk = uint32_t(lstep) * kGroupBytes;
-      to_lds16(i < WLOADS ? wbase + (off[i] + wk) : xbase + (off[i] + xk), dst + r0 * kGroupBytes);
+      const uint32_t xk = uint32_t(lstep) * XROW;
+      to_lds16(i < WLOADS ? wbase + (off[i] + wk) : xbase + (off[i] + xk),
+               dst + (i < WLOADS ? (i * W + wave) * 1024
+                                 : BN * kGroupBytes + ((i - WLOADS) * W + wave) * 1024));
     } else {
       const int r0 = 64 * (((i - LOADS) * W + wave) % SALL);
       to_lds4(sbase[i - LOADS] + lstep * (of_w(i - LOADS) ? wpitch : xpitch), dst + CODES + r0 * 4);
@@ -250,11 +334,18 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   const int half = lane / 32, row = lane % 32;
   f16v acc[TN][TM];
   const int frag_w = (wn * TN * 32 + row) * kGroupBytes;
-  const int frag_x = (BN + wm * TM * 32 + row) * kGroupBytes;
+  const int frag_x = BN * kGroupBytes + (wm * TM * 32 + row) * XROW;
   const int scale_w = CODES + (wn * TN * 32 + row) * 4;
   const int scale_x = CODES + (BN + wm * TM * 32 + row) * 4;
   const int at0 = ((2 * half) ^ (row / 4 % 4)) * 16;  // place of part j's block: at0 ^ (16 j)
-  u4 a[2][TN] = {}, b[2][TM] = {};
+  // Of 8-bit rows: part j's two chunks.  The scaled products take half `half` of blocks j and 2 + j,
+  // the BF16 ones both halves of W's block 2 * half + j.
+  constexpr bool EXACT = kExact<X8, T>;
+  constexpr int HI8 = EXACT ? 16 : 64;
+  const int at8 = ((EXACT ? 4 * half : half) ^ (row & 7)) * 16;
+  u4 xv[EXACT ? TM : 1][4];
+  u4 a[2][TN] = {};
+  XFrag<X8> b[2][TM] = {};
   uint32_t cw[TN] = {}, cx[TM] = {}, nw[TN], nx[TM];  // scales of this step and the next
   // Everything is issued between the products, a few instructions after every row of TM of them,
   // which a wavefront's in-order issue would otherwise put in front of them: the reads of the
@@ -262,11 +353,18 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
   // before) and the loads of a later step.  Those go to `nxt`, not the memory of `cur`: the
   // reads need not wait for them.
   auto fetch = [&](const uint8_t* __restrict__ cur, int j, int i) {
-    if (i < TM)
-      b[j][i] = *reinterpret_cast<const u4*>(cur + frag_x + i * 32 * kGroupBytes + (at0 ^ (16 * j)));
-    else
+    if (i < TM) {
+      const uint8_t* p = cur + frag_x + i * 32 * XROW;
+      if constexpr (X8) {
+        b[j][i].lo = *reinterpret_cast<const u4*>(p + (at8 ^ (32 * j)));
+        b[j][i].hi = *reinterpret_cast<const u4*>(p + (at8 ^ (32 * j) ^ HI8));
+      } else {
+        b[j][i] = *reinterpret_cast<const u4*>(p + (at0 ^ (16 * j)));
+      }
+    } else {
       a[j][i - TM] =
           *reinterpret_cast<const u4*>(cur + frag_w + (i - TM) * 32 * kGroupBytes + (at0 ^ (16 * j)));
+    }
   };
   auto fetch_scale = [&](const uint8_t* __restrict__ cur, int i) {
     if (i < TM)
@@ -274,10 +372,27 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     else
       nw[i - TM] = *reinterpret_cast<const uint32_t*>(cur + scale_w + (i - TM) * 128);
   };
-#define EMB_ROW(J, I)                                                                        \
-  _Pragma("unroll") for (int j = 0; j < TM; ++j) acc[I][j] =                                 \
-      __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag8(a[J][I]), frag8(b[J][j]), acc[I][j], \
-                                                      4, 4, J, int(cw[I]), J, int(cx[j]));   \
+  // (The scales' bytes are chosen in the instruction: a constant each.)
+#define EMB_ROW(J, I)                                                                          \
+  if constexpr (EXACT) {                                                                       \
+    u4 wv[4];                                                                                  \
+    if (I == 0) {                                                                              \
+      _Pragma("unroll") for (int j = 0; j < TM; ++j)                                           \
+          bf16_values(b[J][j], cx[j] >> (8 * J) & 255u, xv[j]);                                \
+    }                                                                                          \
+    bf16_values(a[J][I], cw[I] >> (8 * J) & 255u, wv);                                         \
+    _Pragma("unroll") for (int t = 0; t < 4; ++t) {                                            \
+      _Pragma("unroll") for (int j = 0; j < TM; ++j) acc[I][j] =                               \
+          __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, wv[t]),              \
+                                                  __builtin_bit_cast(bf8, xv[j][t]), acc[I][j], \
+                                                  0, 0, 0);                                    \
+    }                                                                                          \
+  } else {                                                                                     \
+    _Pragma("unroll") for (int j = 0; j < TM; ++j) acc[I][j] =                                 \
+        __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag8(a[J][I]), frag8(b[J][j]),        \
+                                                        acc[I][j], 4, kXFormat<X8>, J,         \
+                                                        int(cw[I]), J, int(cx[j]));            \
+  }                                                                                            \
   __builtin_amdgcn_sched_barrier(0);
   auto step_of = [&](const uint8_t* __restrict__ cur, uint8_t* __restrict__ nxt) {
     constexpr int N = TN + TM;  // fragments of a part, read before its last row's products
@@ -344,7 +459,10 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
 #pragma unroll
   for (int i = 0; i < TN; ++i) a[1][i] = u4{0u, 0u, 0u, 0u}, cw[i] = 0u;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) cx[i] = 0u;
+  for (int i = 0; i < TM; ++i) {
+    cx[i] = 0u;
+    if constexpr (X8) b[1][i] = {};  // (8-bit codes have a NaN of their own)
+  }
 
   // Each wavefront turns 32 rows of x and 32 * TILES of W at a time around in its own part of LDS
   // (lane: row of x lane % 32, four consecutive rows of W per quarter of its registers), then
@@ -475,6 +593,79 @@ __global__ __launch_bounds__(kBlock) void scores_direct(const TX* __restrict__ x
   }
 }
 
+// The same from 8-bit rows, read in place.  Into BF16, of product j's four blocks (one of each group) lane
+// group q takes half q % 2 of the first or second (q / 2) and of the third or fourth, and gives the scale
+// of block q; into FP32 it takes block q of x as of W.
+template <class T>
+__global__ __launch_bounds__(kBlock) void scores8_direct(const uint8_t* __restrict__ xc,
+                                                         const uint32_t* __restrict__ xs, Mx4View w,
+                                                         int32_t m, int32_t groups,
+                                                         T* __restrict__ out, int64_t ldo,
+                                                         uint32_t first) {
+  const int lane = lane_id(), r = lane % 16, q = lane / 16;
+  const int64_t n0 = ((int64_t(first) + blockIdx.x) * kWavesPerBlock + wave_id()) * 16;
+  const int nb = mx4_blocks(w.dim);
+  const int64_t wn = min(n0 + r, w.rows - 1);
+  const int xm = min(r, m - 1);
+  const uint8_t* wc = w.codes + wn * nb * 16;
+  const uint32_t* wsc = reinterpret_cast<const uint32_t*>(w.scales) + wn * groups;
+  constexpr bool EXACT = kExact<true, T>;
+  const uint8_t* xr = xc + int64_t(xm) * groups * 128 + (EXACT ? 0 : q % 2 * 16);
+  const uint32_t* xsc = xs + int64_t(xm) * groups;
+
+  const u4 none = {0u, 0u, 0u, 0u};
+  u4 b[4];
+  Bytes32 a[4];
+  uint32_t sw, sx;
+  auto load = [&](int g0) {
+    const int g = g0 + q, ga = EXACT ? g : g0 + q / 2, gb = EXACT ? g : ga + 2;
+    sw = g < groups ? wsc[g] : 0u;
+    sx = g < groups ? xsc[g] : 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      b[j] = g * 4 + j < nb ? *reinterpret_cast<const u4*>(wc + (g * 4 + j) * 16) : none;
+      a[j].lo = ga < groups ? *reinterpret_cast<const u4*>(xr + ga * 128 + j * 32) : none;
+      a[j].hi = gb < groups ? *reinterpret_cast<const u4*>(xr + gb * 128 + j * 32 + (EXACT ? 16 : 0)) : none;
+    }
+  };
+  load(0);
+  f4 c = {0.f, 0.f, 0.f, 0.f};
+  for (int g0 = 0; g0 < groups; g0 += 4) {
+    const u4 v[4] = {b[0], b[1], b[2], b[3]};
+    const Bytes32 u[4] = {a[0], a[1], a[2], a[3]};
+    const uint32_t tw = sw, tx = sx;
+    if (g0 + 4 < groups) load(g0 + 4);
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        u4 xv[4], wv[4];
+        bf16_values(u[j], tx >> (8 * j) & 255u, xv);
+        bf16_values(v[j], tw >> (8 * j) & 255u, wv);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, xv[t]),
+                                                      __builtin_bit_cast(bf8, wv[t]), c, 0, 0, 0);
+      }
+    } else {
+#define EMB_MFMA(J)                                                                            \
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag8(u[J]), frag8(v[J]), c, 0, 4, J,   \
+                                                       int(tx), J, int(tw));
+      EMB_MFMA(0)
+      EMB_MFMA(1)
+      EMB_MFMA(2)
+      EMB_MFMA(3)
+#undef EMB_MFMA
+    }
+  }
+  const int64_t n = n0 + r;
+  if (n >= w.rows) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int mm = q * 4 + i;
+    if (mm < m) out[int64_t(mm) * ldo + n] = T(c[i]);
+  }
+}
+
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
@@ -500,18 +691,18 @@ ScoreLayout score_layout(int32_t m, int64_t n, int32_t k) {
   return L;
 }
 
-template <int TN, int TM, int WN, int WM, int STAGES, int RESIDENT, class T>
+template <bool X8, int TN, int TM, int WN, int WM, int STAGES, int RESIDENT, class T>
 void launch_tile(const uint8_t* xc, const uint32_t* xs, int32_t m, int32_t groups,
                  const Mx4View& w, const uint32_t* ws, T* out, int64_t ldo, hipStream_t st) {
   constexpr int BN = 32 * TN * WN, BM = 32 * TM * WM;
   static_assert(kPad % BN == 0 && kPad % BM == 0, "padded scales");
-  constexpr size_t stage = size_t(BN + BM) * (kGroupBytes + 4);
+  constexpr size_t stage = size_t(BN) * (kGroupBytes + 4) + size_t(BM) * (kXRow<X8> + 4);
   constexpr size_t turn = size_t(WN) * WM * 32 * (32 * turn_tiles<T>(TN) + kVec<T>)*sizeof(T);
   constexpr size_t lds = STAGES * stage + turn;
   static_assert(lds <= kLdsPerCu / RESIDENT, "blocks that share a compute unit");
   const uint32_t mtiles = uint32_t((m + BM - 1) / BM);
   const uint32_t ntiles = uint32_t((w.rows + BN - 1) / BN);
-  auto kernel = scores_tile<TN, TM, WN, WM, STAGES, T>;
+  auto kernel = scores_tile<X8, TN, TM, WN, WM, STAGES, T>;
   if (lds > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                               hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
@@ -532,10 +723,11 @@ void launch_direct(const TX* x, int64_t stride, const uint8_t* xc, const uint32_
   });
 }
 
-template <class T>
-void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, int32_t m,
-                   int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
-  if (m > 16) {
+// More than 16 rows of x.
+template <bool X8, class T>
+void launch_tiles(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, int32_t m,
+                  int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
+  {
     auto tiles = [&](int64_t bn, int64_t bm) {
       return (w.rows + bn - 1) / bn * ((m + bm - 1) / bm);
     };
@@ -550,17 +742,59 @@ void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, in
     // 55 / 26 / 23 / 19.
     const int64_t big = tiles(256, 256), mid = tiles(128, 128);
     const int64_t big_rounds = rounds(big, kNumCu);
-    if (m > 512 && big_rounds >= 4 && big_rounds * 10 < rounds(mid, 2 * kNumCu) * 7)
-      launch_tile<4, 4, 2, 2, 3, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
-    else if (m > 64 && mid >= kNumCu / 2)
-      launch_tile<2, 2, 2, 2, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
+    if constexpr (!kExact<X8, T>) {
+      if (m > 512 && big_rounds >= 4 && big_rounds * 10 < rounds(mid, 2 * kNumCu) * 7)
+        return launch_tile<X8, 4, 4, 2, 2, X8 ? 2 : 3, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
+    }
+    if (m > 64 && mid >= kNumCu / 2)
+      launch_tile<X8, 2, 2, 2, 2, X8 ? 2 : 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
     else if (tiles(128, 64) >= kNumCu)
-      launch_tile<1, 2, 4, 1, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
+      launch_tile<X8, 1, 2, 4, 1, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
     else
-      launch_tile<1, 1, 2, 2, 4, 3>(xc, xs, m, groups, w, ws, out, ldo, st);
+      launch_tile<X8, 1, 1, 2, 2, X8 ? 3 : 4, X8 ? 2 : 3>(xc, xs, m, groups, w, ws, out, ldo, st);
+  }
+}
+
+template <class T>
+void launch_scores(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, int32_t m,
+                   int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
+  if (m > 16) return launch_tiles<false>(xc, xs, ws, m, groups, w, out, ldo, st);
+  launch_direct<false>(static_cast<const T*>(nullptr), 0, xc, xs, m, groups, w, out, ldo, st);
+}
+
+// Scales of both sides in the workspace; none for up to 16 rows, which are read in place.
+struct Score8Layout {
+  size_t ws, total;
+};
+Score8Layout score8_layout(int32_t m, int64_t n, int32_t k) {
+  if (m <= 16) return {0, 0};
+  const size_t groups = size_t((k + kGroup - 1) / kGroup);
+  Score8Layout L;
+  L.ws = size_t(padded(m)) * groups * 4;
+  L.total = L.ws + size_t(padded(n)) * groups * 4;
+  return L;
+}
+
+template <class T>
+void launch_scores8(const uint8_t* xc, const uint32_t* xs, int32_t m, int32_t groups, const Mx4View& w,
+                    T* out, int64_t ldo, char* ws, hipStream_t st) {
+  if (m <= 16) {
+    for_launches((w.rows + 63) / 64, kBlock, [&](uint32_t first, dim3 grid) {
+      hipLaunchKernelGGL(scores8_direct<T>, grid, dim3(kBlock), 0, st, xc, xs, w, m, groups, out, ldo,
+                         first);
+    });
     return;
   }
-  launch_direct<false>(static_cast<const T*>(nullptr), 0, xc, xs, m, groups, w, out, ldo, st);
+  uint32_t* xst = reinterpret_cast<uint32_t*>(ws);
+  uint32_t* wst = reinterpret_cast<uint32_t*>(ws + score8_layout(m, w.rows, w.dim).ws);
+  const uint32_t xblocks = uint32_t((m + kWave - 1) / kWave);
+  const uint32_t wblocks = uint32_t((w.rows + kWave - 1) / kWave);
+  for_launches(int64_t(xblocks) + wblocks, kBlock, [&](uint32_t first, dim3 grid) {
+    hipLaunchKernelGGL(pack_scales, grid, dim3(kBlock), 0, st, xs, int64_t(m), xst, padded(m), xblocks,
+                       reinterpret_cast<const uint32_t*>(w.scales), w.rows, wst, padded(w.rows), groups,
+                       first);
+  });
+  launch_tiles<true>(xc, xst, wst, m, groups, w, out, ldo, st);
 }
 
 }  // namespace
@@ -610,6 +844,21 @@ hipError_t launch_mx4_matmul(const void* x, bool x_bf16, int64_t x_stride, int32
     launch_scores(xc, xsw, wst, m, groups, w, static_cast<__bf16*>(out), out_stride, st);
   else
     launch_scores(xc, xsw, wst, m, groups, w, static_cast<float*>(out), out_stride, st);
+  return hipGetLastError();
+}
+
+size_t mx4_matmul_x8_workspace(int32_t m, int64_t n, int32_t k) { return score8_layout(m, n, k).total; }
+
+hipError_t launch_mx4_matmul_x8(const uint8_t* xc, const uint8_t* xs, int32_t m, const Mx4View& w,
+                                void* out, bool out_bf16, int64_t out_stride, char* ws,
+                                hipStream_t st) {
+  if (m == 0) return hipSuccess;
+  const int groups = (w.dim + kGroup - 1) / kGroup;
+  const uint32_t* xsw = reinterpret_cast<const uint32_t*>(xs);
+  if (out_bf16)
+    launch_scores8(xc, xsw, m, groups, w, static_cast<__bf16*>(out), out_stride, ws, st);
+  else
+    launch_scores8(xc, xsw, m, groups, w, static_cast<float*>(out), out_stride, ws, st);
   return hipGetLastError();
 }
 

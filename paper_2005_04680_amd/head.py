@@ -4,7 +4,8 @@ other entry points (device pointers and the current HIP stream to the C ABI of
 
 4-bit microscaled tables (``Mx4Table``, ``Mx4Tables``): ``embbag_mx4_quantize``,
 ``embbag_mx4_dequantize``, ``embbag_mx4_forward`` (bags), ``embbag_mx4_matmul``
-(scores of every row) and ``embbag_mx4_matmul_grad``.  Between rows and scores:
+(scores of every row; ``embbag_mx4_matmul_x8`` from 8-bit rows) and
+``embbag_mx4_matmul_grad``.  Between rows and scores:
 ``embbag_rmsnorm`` (into FP32, BF16 or 8-bit rows, ``Mx8Rows``), ``embbag_rmsnorm_grad``,
 ``embbag_mx8_dequantize``.  Logits:
 ``embbag_logits_process`` (penalties, biases, masks) and ``embbag_distill`` (loss
@@ -100,6 +101,8 @@ def _lib():
         L.embbag_mx4_forward.argtypes = [p, i32, p, p, i64, p, i32, p, i32, p, p]
         L.embbag_mx4_matmul_workspace_bytes.argtypes = [i32, i64, i32]
         L.embbag_mx4_matmul.argtypes = [p, i32, i64, i32, p, p, i64, i32, p, i32, i64, p, sz, p]
+        L.embbag_mx4_matmul_x8_workspace_bytes.argtypes = [i32, i64, i32]
+        L.embbag_mx4_matmul_x8.argtypes = [p, p, i32, p, p, i64, i32, p, i32, i64, p, sz, p]
         L.embbag_mx4_matmul_grad_workspace_bytes.argtypes = [i32, i64, i32]
         L.embbag_mx4_matmul_grad.argtypes = [p, i32, i64, i32, p, p, i64, i32, p, i32, i64, p, sz,
                                              p]
@@ -110,10 +113,10 @@ def _lib():
         L.embbag_rmsnorm.argtypes = [p, p]
         L.embbag_rmsnorm_grad_workspace_bytes.argtypes = [i64, i32]
         L.embbag_rmsnorm_grad.argtypes = [p, p, sz, p]
-        for n in ("mx8_dequantize", "rmsnorm", "rmsnorm_grad", "mx4_quantize", "mx4_dequantize", "mx4_forward", "mx4_matmul",
+        for n in ("mx8_dequantize", "mx4_matmul_x8", "rmsnorm", "rmsnorm_grad", "mx4_quantize", "mx4_dequantize", "mx4_forward", "mx4_matmul",
                   "mx4_matmul_grad", "logits_process", "distill"):
             getattr(L, "embbag_" + n).restype = C.c_int
-        for n in ("rmsnorm_grad", "mx4_matmul", "mx4_matmul_grad", "distill"):
+        for n in ("rmsnorm_grad", "mx4_matmul_x8", "mx4_matmul", "mx4_matmul_grad", "distill"):
             getattr(L, f"embbag_{n}_workspace_bytes").restype = sz
         _ready = L
     return _ready
@@ -349,6 +352,22 @@ def embbag_mx4_matmul(x, table, out, workspace, stream=None) -> int:
     w, n = _ws(workspace)
     return _lib().embbag_mx4_matmul(p, ty, ld, _i32(m), table.codes_ptr, table.scales_ptr, table.rows,
                                     table.dim, q, tq, lq, w, n, _stream(stream))
+
+
+def embbag_mx4_matmul_x8_workspace_bytes(m, n, k) -> int:
+    return int(_lib().embbag_mx4_matmul_x8_workspace_bytes(_i32(int(m)), int(n), _i32(int(k))))
+
+
+def embbag_mx4_matmul_x8(x, table, out, workspace, stream=None) -> int:
+    """Scores of every row of ``table`` from 8-bit rows ``x`` (``Mx8Rows``): ``out`` [m, M] = x W^T."""
+    if x.dim != table.dim:
+        raise ValueError(f"x: rows of {x.dim}, expected {table.dim} like the table's")
+    q, tq, lq = _matrix(out, table.rows, "out")
+    _check_rows(out, x.rows, "out")
+    w, n = _ws(workspace)
+    return _lib().embbag_mx4_matmul_x8(x.codes_ptr, x.scales_ptr, _i32(x.rows), table.codes_ptr,
+                                       table.scales_ptr, table.rows, table.dim, q, tq, lq, w, n,
+                                       _stream(stream))
 
 
 def embbag_mx4_matmul_grad_workspace_bytes(m, n, k) -> int:

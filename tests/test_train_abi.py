@@ -123,3 +123,35 @@ def test_binding_refuses_wrong_shapes_and_types():
         pk.Mx8Rows(fake(4, 64, dtype=torch.uint8), fake(4, 4, dtype=torch.uint8), 64)
     with pytest.raises(TypeError):
         pk.Mx8Rows(torch.zeros(4, 128, dtype=torch.uint8), torch.zeros(4, 4, dtype=torch.uint8), 64)
+
+
+M_NAMES = "x xs m codes scales n k out otype ostride ws bytes stream".split()
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(x=None), BAD), (dict(x=FAKE + 8), BAD), (dict(xs=None), BAD), (dict(xs=FAKE + 2), BAD), (dict(m=-1), BAD),
+    (dict(m=2 ** 23), BAD), (dict(codes=FAKE + 8), BAD), (dict(scales=None), BAD), (dict(n=0), BAD),
+    (dict(n=2 ** 31), BAD), (dict(k=250), BAD), (dict(k=16388), BAD), (dict(out=None), BAD), (dict(out=FAKE + 2), BAD),
+    (dict(ostride=999), BAD), (dict(otype=2), BAD), (dict(m=2 ** 22, n=2 ** 20, ostride=2 ** 20), BAD),
+    (dict(ws=None), WS), (dict(ws=FAKE + 64), WS), (dict(bytes=0), WS)])
+def test_scores_from_eight_bits_refusals(L, change, code):
+    good = dict(x=FAKE, xs=FAKE, m=100, codes=FAKE, scales=FAKE, n=1000, k=256, out=FAKE, otype=F32, ostride=1000,
+                ws=FAKE, bytes=1 << 30, stream=None)
+    args = dict(good, **change)
+    assert L.embbag_mx4_matmul_x8(*[args[n] for n in M_NAMES]) == code
+
+
+def test_scores_from_eight_bits_sizes():
+    f = pk.embbag_mx4_matmul_x8_workspace_bytes
+    assert f(16, 1000, 256) == 0 and f(17, 1000, 256) > 0
+    for m, n, k in [(-1, 10, 64), (2 ** 23, 10, 64), (10, 0, 64), (10, 2 ** 31, 64), (10, 10, 66), (10, 10, 16388),
+                    (2 ** 32 + 17, 10, 64), (17, 10, 2 ** 32 + 64)]:
+        assert f(m, n, k) == 0
+    x = SimpleNamespace(rows=4, dim=64, codes_ptr=FAKE, scales_ptr=FAKE)
+    t = SimpleNamespace(rows=10, dim=68, codes_ptr=FAKE, scales_ptr=FAKE)
+    with pytest.raises(ValueError):
+        pk.embbag_mx4_matmul_x8(x, t, fake(4, 10), None, stream=0)
+    t.dim = 64
+    for shape in [(3, 10), (4, 11)]:
+        with pytest.raises(ValueError):
+            pk.embbag_mx4_matmul_x8(x, t, fake(*shape), None, stream=0)
