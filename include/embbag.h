@@ -568,6 +568,52 @@ typedef struct {
 
 int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStream_t stream);
 
+/* Softmax cross entropy of the scores over a table, without keeping the scores, with
+ * the gradients of both of their sides.  With z[r][v] = scale * sum over e of
+ * x[r][e] * table[v][e] and q = softmax(z[r]) over the vocabulary, for every row r:
+ *   loss[r] = w * (log(sum over v of exp z[r][v]) - z[r][labels[r]]),
+ *   grad_x[r] = scale * w * sum over v of (q[v] - [v == labels[r]]) * table[v],
+ *   grad_table[v] = scale * sum over r of w * (q[v] - [v == labels[r]]) * x[r],
+ * w = row_weights[r] (null: 1), the gradients of the sum of the losses.  A row with a
+ * negative label or the weight 0 is left out: its loss and grad_x are 0, whatever x
+ * holds there, and it costs no products.
+ * x [rows][dim] of x_type, table [vocab][dim] of table_type (for split tables the high
+ * halves, as BF16), grad_x and grad_table (each nullable) of their sides' types: row
+ * strides in elements and alignments as embbag_mx4_quantize's src, table_stride at most
+ * 2^19.  labels: device int32 [rows], loss: FP32 [rows].  scale: finite.  rows <= 2^20,
+ * vocab <= 2^31 - 1, rows * vocab <= 2^40.  Outputs must not overlap inputs, but
+ * grad_x may be x itself with the same stride.  A label >= vocab is a data error; its row
+ * is left out then.  Scores and sums are FP32.  BF16 sides: q - [v == label], times w
+ * over the largest weight, is rounded to BF16 (two terms of it up to 256 rows) for the
+ * gradients' products.  If either side is FP32 both enter with 24 bits.
+ * `workspace`: 256-byte aligned; `type` is EMBBAG_F32 if either side is FP32, `backward`
+ * whether a gradient is wanted.  It holds a piece of the vocabulary's q at a time (at most
+ * about 512 MB of it, or 256 columns). */
+typedef struct {
+  int32_t rows;
+  int32_t dim;
+  int64_t vocab;
+  int32_t x_type;
+  const void* x;
+  int64_t x_stride;
+  int32_t table_type;
+  const void* table;
+  int64_t table_stride;
+  const int32_t* labels;
+  const float* row_weights;
+  float scale;
+  float* loss;
+  void* grad_x;
+  int64_t grad_x_stride;
+  void* grad_table;
+  int64_t grad_table_stride;
+} embbag_xent_t;
+
+size_t embbag_xent_workspace_bytes(int32_t rows, int64_t vocab, int32_t dim, int32_t type,
+                                   int32_t backward);
+int embbag_xent(const embbag_xent_t* args, void* workspace, size_t workspace_bytes, int32_t* d_status,
+                hipStream_t stream);
+
 /* Distillation from a teacher's top logits.  For every row r, with z =
  * logits[r]/temperature, q = softmax(z) over the vocabulary and p the softmax of
  * teacher[r]/temperature over the row's entries (k with ids[r][k] >= 0):

@@ -656,7 +656,8 @@ from .head import (EMBBAG_BF16, EMBBAG_F32, Mx4Table, Mx4Tables, Mx8Rows,  # noq
                    embbag_mx4_matmul_workspace_bytes, embbag_mx4_matmul_x8,
                    embbag_mx4_matmul_x8_workspace_bytes, embbag_mx4_quantize,
                    embbag_mx8_dequantize, embbag_rmsnorm, embbag_rmsnorm_grad,
-                   embbag_rmsnorm_grad_workspace_bytes, mx4_code_bytes, mx4_scale_bytes,
+                   embbag_rmsnorm_grad_workspace_bytes, embbag_xent,
+                   embbag_xent_workspace_bytes, mx4_code_bytes, mx4_scale_bytes,
                    mx8_code_bytes)
 
 __all__ = [n for n in dir() if n.startswith("embbag_") or n.startswith("EMBBAG_")] + [

@@ -231,6 +231,11 @@ hipError_t launch_rmsnorm_grad(NormGradArgs a, bool y_bf16, bool h_bf16, void* d
 hipError_t launch_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
                                  int32_t dim, void* dst, bool bf16, int64_t dst_stride, hipStream_t st);
 
+constexpr int32_t kMaxXentRows = 1 << 20;
+constexpr int64_t kMaxXentStride = int64_t(1) << 19;  // of the table: a tile's rows within 2^30 bytes
+size_t xent_workspace(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward);
+hipError_t launch_xent(const embbag_xent_t& a, char* ws, int32_t* status, hipStream_t st);
+
 size_t distill_workspace(int32_t rows, int32_t vocab, int32_t top);
 hipError_t launch_distill(const embbag_distill_t& a, char* ws, int32_t* status, hipStream_t st);
 

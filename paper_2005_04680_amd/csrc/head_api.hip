@@ -46,6 +46,11 @@ bool mx8_ok(const uint8_t* codes, const uint8_t* scales) {
 // The vector of a norm's weights or of their gradient (null: none).
 bool weight_ok(const void* p, int32_t type) { return aligned(p, 4 * type_size(type)); }
 
+bool xent_sizes_ok(int32_t rows, int64_t vocab, int32_t dim) {
+  return rows >= 0 && rows <= kMaxXentRows && vocab >= 1 && vocab <= kInt32Max && dim_ok(dim) &&
+         rows * vocab <= kMaxMatrix;
+}
+
 bool eps_ok(float eps) { return eps > 0.f && eps <= 3.4028234663852886e38f; }
 
 // A list per row (offsets, entries) of n entries, fewer than 2^30: occurrences are counted in
@@ -324,6 +329,34 @@ int embbag_distill(const embbag_distill_t* args, void* workspace, size_t workspa
   if (workspace_bytes < need || !aligned(workspace, kWsAlign) || (workspace == nullptr && need > 0))
     return EMBBAG_ERR_WORKSPACE;
   return hip_status(launch_distill(a, static_cast<char*>(workspace), d_status, stream));
+}
+
+size_t embbag_xent_workspace_bytes(int32_t rows, int64_t vocab, int32_t dim, int32_t type,
+                                   int32_t backward) {
+  return xent_sizes_ok(rows, vocab, dim) && type_ok(type)
+             ? xent_workspace(rows, vocab, dim, type == EMBBAG_F32, backward != 0)
+             : 0;
+}
+
+int embbag_xent(const embbag_xent_t* args, void* workspace, size_t workspace_bytes, int32_t* d_status,
+                hipStream_t stream) {
+  if (args == nullptr) return EMBBAG_ERR_INVALID_ARG;
+  const embbag_xent_t& a = *args;
+  if (!xent_sizes_ok(a.rows, a.vocab, a.dim) || !type_ok(a.x_type) || !type_ok(a.table_type) ||
+      !(a.scale >= -3.4028234663852886e38f && a.scale <= 3.4028234663852886e38f))
+    return EMBBAG_ERR_INVALID_ARG;
+  if (!rows_ok(a.table, a.table_type, a.table_stride, a.dim) || a.table_stride > kMaxXentStride ||
+      (a.grad_table != nullptr && !rows_ok(a.grad_table, a.table_type, a.grad_table_stride, a.dim)))
+    return EMBBAG_ERR_INVALID_ARG;
+  if (a.rows > 0 && (!rows_ok(a.x, a.x_type, a.x_stride, a.dim) || a.labels == nullptr || a.loss == nullptr ||
+                     (a.grad_x != nullptr && !rows_ok(a.grad_x, a.x_type, a.grad_x_stride, a.dim))))
+    return EMBBAG_ERR_INVALID_ARG;
+  const bool f32 = a.x_type == EMBBAG_F32 || a.table_type == EMBBAG_F32;
+  const size_t need = xent_workspace(a.rows, a.vocab, a.dim, f32,
+                                     a.grad_x != nullptr || a.grad_table != nullptr);
+  if (workspace_bytes < need || !aligned(workspace, kWsAlign) || workspace == nullptr)
+    return EMBBAG_ERR_WORKSPACE;
+  return hip_status(launch_xent(a, static_cast<char*>(workspace), d_status, stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,673 @@
+// Softmax cross entropy of the scores over a table, with the gradients of the scores' inputs and
+// of the table; the scores are never kept.
+//
+// z = scale x W^T, loss = w (log sum exp z - z[label]), D = softmax(z) - onehot(label):
+//   dx = scale w D W,   dW = scale (w D)^T x.
+// 1. The rows that count (a label, a weight) are packed: x as BF16, rows that are left out are not
+//    computed with.
+// 2. The scores' tiles leave, for every row and 128 columns, their largest score and the sum of the
+//    exponentials; the parts are joined in order.
+// 3. Piece by piece of the vocabulary the tiles are computed again, now as D times w / (largest w),
+//    rounded to BF16 in the workspace, and that piece's two products follow: dx is added up in FP32, dW
+//    of the piece is final.
+// All sums are in orders that the sizes determine; there are no atomics on them.
+//
+// BF16 operands are taken as they are.  D is rounded to BF16 (2^-8 of each element at most, as the
+// gradients' own rounding; two terms of it where rows are few and the products do not bound the call).
+// With the weights' ratio in D, equal weights leave the label's element, next to -1, almost exact.  FP32
+// operands, and D with them, are the sum of three BF16 terms, of whose nine products six are taken: what
+// is left out is below 2^-22 of each product.
+#include "gemm.hpp"
+
+namespace embbag {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of D, of W's terms: a piece's
+constexpr int64_t kMaxPitch = int64_t(1) << 19;       // elements of a row of D
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// x as the sum of three BF16 terms, each the nearest to what is left (the first by truncation where
+// rounding would pass the range).  A NaN is its own first term.  An infinity is its own last one: that term
+// meets the other side's first alone, so that the product is an infinity of the right sign.
+__device__ __forceinline__ void nearest_terms(float x, float (&t)[3]) {
+  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+  t[0] = float(__bf16(x));
+  if (u > 0x7F7F7FFFu && u < 0x7F800000u) t[0] = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+  if (u == 0x7F800000u) t[0] = 0.f;
+  const float rest = u > 0x7F800000u ? 0.f : x - t[0];
+  t[1] = u == 0x7F800000u ? 0.f : float(__bf16(rest));
+  t[2] = rest - t[1];
+}
+
+// What the backward needs of a row that counts.
+struct Token {
+  float top;    // its largest score
+  float inv;    // 1 / the sum of exp(score - top)
+  float ratio;  // its weight over the largest
+  int label;
+};
+
+// In the workspace.
+struct Head {
+  int32_t live;   // rows that count
+  float largest;  // of their weights' magnitudes
+  float factor;   // scale * largest
+};
+
+struct Rows {
+  Head* head;
+  int32_t* place;  // [rows]: among the rows that count, or -1
+  int32_t* row;    // [live]: the row at a place
+  Token* tokens;   // [live]
+  float* target;   // [live]: the label's score
+};
+
+// Which rows count, their places in order, and the largest weight.  One block; the losses of the others
+// are 0.
+__global__ __launch_bounds__(1024) void xent_rows(const int32_t* __restrict__ labels,
+                                                  const float* __restrict__ weights, int32_t rows,
+                                                  int32_t vocab, float scale, Rows out,
+                                                  float* __restrict__ loss, int32_t* __restrict__ status) {
+  __shared__ int counts[16];
+  __shared__ float tops[16];
+  const int lane = lane_id(), wave = wave_id();
+  int base = 0;
+  float top = 0.f;
+  bool bad = false;
+  for (int r0 = 0; r0 < rows; r0 += 4096) {
+    int label[4], n = 0;
+    float w[4];
+    bool in[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + threadIdx.x * 4 + i;
+      label[i] = r < rows ? labels[r] : -1;
+      w[i] = r < rows && weights != nullptr ? weights[r] : 1.f;
+      bad = bad || label[i] >= vocab;
+      in[i] = label[i] >= 0 && label[i] < vocab && w[i] != 0.f;
+      n += in[i];
+      if (in[i]) top = fmaxf(top, fabsf(w[i]));
+    }
+    int before = n;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int v = __shfl_up(before, d, kWave);
+      if (lane >= d) before += v;
+    }
+    __syncthreads();  // (the counts of the round before have been read)
+    if (lane == kWave - 1) counts[wave] = before;
+    __syncthreads();
+    int at = base + before - n, all = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i < wave) at += counts[i];
+      all += counts[i];
+    }
+    base += all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + threadIdx.x * 4 + i;
+      if (r >= rows) continue;
+      out.place[r] = in[i] ? at : -1;
+      if (in[i]) {
+        out.row[at] = r;
+        Token t = {0.f, 0.f, w[i], label[i]};
+        out.tokens[at] = t;
+        ++at;
+      } else {
+        loss[r] = 0.f;
+      }
+    }
+  }
+  if (bad && status != nullptr) atomicMin(status, EMBBAG_ERR_INDEX_RANGE);
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, tops[i]);
+    out.head->live = base;
+    out.head->largest = top;
+    out.head->factor = scale * top;
+  }
+}
+
+// 8 elements of a row from e on (zeros past dim; dim % 4 == 0) as BF16 terms to `dst`.
+template <int TERMS, class T>
+__device__ __forceinline__ void pack8(const T* row, int e, int dim, __bf16* dst, int64_t plane) {
+  const f4 zero = {0.f, 0.f, 0.f, 0.f};
+  const f4 p = e < dim ? load4(row + e) : zero;
+  const f4 q = e + 4 < dim ? load4(row + e + 4) : zero;
+  const float v[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+  if constexpr (TERMS == 1) {
+    store16(dst, pack16(v));
+  } else {
+    float t[3][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float s[3];
+      nearest_terms(v[i], s);
+      t[0][i] = s[0], t[1][i] = s[1], t[2][i] = s[2];
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) store16(dst + k * plane, pack16(t[k]));
+  }
+}
+
+// x's rows that count as TERMS planes [live][padded]; dx's others as zeros.  A wavefront per row.
+template <int TERMS, class T>
+__global__ __launch_bounds__(kBlock) void xent_pack_x(const T* __restrict__ x, int64_t stride,
+                                                      int32_t rows, int32_t dim, int32_t padded,
+                                                      const int32_t* __restrict__ place,
+                                                      __bf16* __restrict__ out, int64_t plane,
+                                                      T* __restrict__ dx, int64_t dx_stride) {
+  const int r = blockIdx.x * kWavesPerBlock + wave_id();
+  if (r >= rows) return;
+  const int at = __builtin_amdgcn_readfirstlane(place[r]);
+  if (at < 0) {
+    if (dx == nullptr) return;
+    for (int e = lane_id() * 4; e < dim; e += kWave * 4)
+      store4(dx + r * dx_stride + e, f4{0.f, 0.f, 0.f, 0.f});
+    return;
+  }
+  for (int e = lane_id() * 8; e < padded; e += kWave * 8)
+    pack8<TERMS>(x + r * stride, e, dim, out + int64_t(at) * padded + e, plane);
+}
+
+// Rows of W as TERMS planes [rows][padded].
+template <int TERMS, class T>
+__global__ __launch_bounds__(kBlock) void xent_pack_w(const T* __restrict__ w, int64_t stride,
+                                                      int64_t rows, int32_t dim, FastDiv chunks,
+                                                      __bf16* __restrict__ out, int64_t plane) {
+  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+  if (i >= rows * chunks.div) return;
+  const uint32_t r = quotient(uint32_t(i), chunks);
+  const int e = int(uint32_t(i) - r * chunks.div) * 8;
+  pack8<TERMS>(w + int64_t(r) * stride, e, dim, out + i * 8, plane);
+}
+
+// A tile's parts: of each row and 128 columns (a wavefront's: 32 TN) the largest score and the sum of the
+// exponentials of the others' distances to it.
+struct StatsEpi {
+  float2* parts;         // [columns / (32 TN)][pitch]
+  int64_t pitch;
+  const Token* tokens;
+  float* target;
+  float scale;
+  int64_t first;         // the piece's first column
+  int64_t columns;       // of the piece
+  template <int TN, int TM>
+  static constexpr int kScratch = 0;
+
+  template <int TN, int TM>
+  __device__ __forceinline__ void operator()(f16v (&acc)[TN][TM], int64_t n, int64_t m, int64_t m_end, int,
+                                             uint8_t*) const {
+    const int row = lane_id() % 32, half = lane_id() / 32;
+    const bool whole = n + 32 * TN <= columns;
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int64_t at = m + j * 32 + row;
+      const bool in = at < m_end;
+      float top = low();
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int c = i * 32 + r / 4 * 8 + half * 4 + r % 4;
+          acc[i][j][r] = whole || n + c < columns ? acc[i][j][r] * scale : low();
+          top = fmaxf(top, acc[i][j][r]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const float ref = top == low() ? 0.f : top;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += exp2_of((acc[i][j][r] - ref) * kLog2e);
+      sum += __shfl_xor(sum, 32, kWave);
+      const int label = in ? tokens[at].label : -1;
+      const int64_t place = label - first - n;  // of the label among the wavefront's columns
+      if (place >= 0 && place < 32 * TN && (place / 4 % 2) == half) {
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (place == i * 32 + r / 4 * 8 + half * 4 + r % 4) z = acc[i][j][r];
+        target[at] = z;
+      }
+      if (in && half == 0 && n < columns) parts[((first + n) / (32 * TN)) * pitch + at] = float2{top, sum};
+    }
+  }
+};
+
+// Joins the parts of TOKENS rows per block; losses, and what the backward needs.
+template <int TOKENS>
+__global__ __launch_bounds__(1024) void xent_join(const float2* __restrict__ parts, int64_t pitch,
+                                                  int32_t count, Rows rows, float* __restrict__ loss) {
+  constexpr int SLICES = 1024 / TOKENS;
+  __shared__ float2 shared[SLICES][TOKENS + 1];
+  const int live = rows.head->live;
+  const int t = threadIdx.x % TOKENS, slice = threadIdx.x / TOKENS;
+  const int at = blockIdx.x * TOKENS + t;
+  if (int(blockIdx.x) * TOKENS >= live) return;
+  float top = low(), sum = 0.f;
+  auto add = [&](float2 p) {
+    const float m = fmaxf(top, p.x), ref = m == low() ? 0.f : m;
+    sum = sum * exp2_of((top - ref) * kLog2e) + p.y * exp2_of((p.x - ref) * kLog2e);
+    top = m;
+  };
+  if (at < live) {
+#pragma unroll 4
+    for (int i = slice; i < count; i += SLICES) add(parts[int64_t(i) * pitch + at]);
+  }
+  shared[slice][t] = float2{top, sum};
+  __syncthreads();
+  for (int d = SLICES / 2; d > 0; d /= 2) {
+    if (slice < d) {
+      add(shared[slice + d][t]);
+      shared[slice][t] = float2{top, sum};
+    }
+    __syncthreads();
+  }
+  if (slice != 0 || at >= live) return;
+  Token k = rows.tokens[at];
+  const float w = k.ratio;
+  const int r = rows.row[at];
+  loss[r] = w * ((top - rows.target[at]) + __builtin_logf(sum));
+  k.top = top, k.inv = 1.f / sum, k.ratio = w / rows.head->largest;
+  rows.tokens[at] = k;
+}
+
+// Rows of a tile turned around in a wavefront's own LDS: 32 rows of m, 128 bytes of each.
+template <class T>
+constexpr int kTurnTiles = 128 / 32 / int(sizeof(T)) < 1 ? 1 : 128 / 32 / int(sizeof(T));
+template <class T, int TN>
+constexpr int kTiles = kTurnTiles<T> < TN ? kTurnTiles<T> : TN;
+template <class T, int TN>
+constexpr int kTurnPitch = 32 * kTiles<T, TN> + kVec<T>;
+
+// Stores 32 rows of m and kTiles * 32 columns from `turn`: `put(row of the 32, column, 16 bytes)`.
+template <class T, int TN, class Put>
+__device__ __forceinline__ void stored_rows(const T* turn, Put put) {
+  constexpr int V = kVec<T>, PITCH = kTurnPitch<T, TN>, PER_ROW = 32 * kTiles<T, TN> / V;
+  constexpr int ROWS = kWave / PER_ROW;
+  const int r = lane_id() / PER_ROW, c = lane_id() % PER_ROW * V;
+#pragma unroll
+  for (int q = 0; q < 32 / ROWS; ++q)
+    put(r + q * ROWS, c, *reinterpret_cast<const u4*>(turn + (r + q * ROWS) * PITCH + c));
+}
+template <class T, int TN, int TM>
+__device__ __forceinline__ void turn_rows(T* turn, const f16v (&acc)[TN][TM], int h, int j) {
+  const int row = lane_id() % 32, half = lane_id() / 32;
+#pragma unroll
+  for (int i = 0; i < kTiles<T, TN>; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      store4(turn + row * kTurnPitch<T, TN> + i * 32 + q * 8 + half * 4,
+             f4{acc[h + i][j][q * 4], acc[h + i][j][q * 4 + 1], acc[h + i][j][q * 4 + 2],
+                acc[h + i][j][q * 4 + 3]});
+}
+
+// A tile of D (times the weights' ratio): TERMS planes [live][pitch], zeros in the columns past the
+// vocabulary.
+template <int TERMS>
+struct GradEpi {
+  __bf16* d;
+  int64_t pitch, plane;
+  const Token* tokens;
+  float scale;
+  int64_t first, columns;
+  template <int TN, int TM>
+  static constexpr int kScratch = 32 * kTurnPitch<__bf16, TN> * 2;
+
+  template <int TN, int TM>
+  __device__ __forceinline__ void operator()(f16v (&acc)[TN][TM], int64_t n, int64_t m, int64_t m_end, int,
+                                             uint8_t* scratch) const {
+    const int row = lane_id() % 32, half = lane_id() / 32;
+    __bf16* turn = reinterpret_cast<__bf16*>(scratch);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int64_t at = m + j * 32 + row;
+      const Token t = at < m_end ? tokens[at] : Token{0.f, 0.f, 0.f, -1};
+      const int64_t place = t.label - first - n;
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int c = i * 32 + r / 4 * 8 + half * 4 + r % 4;
+          const float p = exp2_of((acc[i][j][r] * scale - t.top) * kLog2e) * t.inv;
+          acc[i][j][r] = n + c < columns ? (place == c ? p - 1.f : p) * t.ratio : 0.f;
+        }
+#pragma unroll
+      for (int h = 0; h < TN; h += kTiles<__bf16, TN>) {
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) {
+          turn_rows<__bf16, TN, TM>(turn, acc, h, j);
+          stored_rows<__bf16, TN>(turn, [&](int r, int c, const u4& v) {
+            const int64_t to = m + j * 32 + r;
+            if (to < m_end && n + h * 32 + c < pitch)
+              *reinterpret_cast<u4*>(d + k * plane + to * pitch + n + h * 32 + c) = v;
+          });
+          if (k + 1 < TERMS) {
+#pragma unroll
+            for (int i = 0; i < kTiles<__bf16, TN>; ++i)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const float x = acc[h + i][j][r], rest = x - float(__bf16(x));
+                acc[h + i][j][r] = x - x == 0.f ? rest : 0.f;  // (an infinity or a NaN leaves nothing)
+              }
+          }
+        }
+      }
+    }
+  }
+};
+
+// Sums times `factor` into rows of `out` (the row that `map` names at a place, or the place itself), or into
+// part z, where `add` adds to what it holds.
+template <class T>
+struct StoreEpi {
+  T* out;
+  int64_t pitch;
+  int64_t columns;
+  const int32_t* map;
+  const float* factor;
+  int64_t part;
+  bool add;
+  template <int TN, int TM>
+  static constexpr int kScratch = 32 * kTurnPitch<T, TN> * int(sizeof(T));
+
+  template <int TN, int TM>
+  __device__ __forceinline__ void operator()(f16v (&acc)[TN][TM], int64_t n, int64_t m, int64_t m_end, int z,
+                                             uint8_t* scratch) const {
+    constexpr int V = kVec<T>;
+    T* turn = reinterpret_cast<T*>(scratch);
+    const float f = factor != nullptr ? *factor : 1.f;
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      if (factor != nullptr) {
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] *= f;
+      }
+#pragma unroll
+      for (int h = 0; h < TN; h += kTiles<T, TN>) {
+        turn_rows<T, TN, TM>(turn, acc, h, j);
+        stored_rows<T, TN>(turn, [&](int r, int c, const u4& v) {
+          const int64_t at = m + j * 32 + r, col = n + h * 32 + c;
+          if (at >= m_end || col >= columns) return;
+          T* p = out + z * part + (map != nullptr ? int64_t(map[at]) : at) * pitch + col;
+          if (col + V <= columns) {
+            if (sizeof(T) == 4 && add) {
+              float x[kVec<T>], y[kVec<T>];
+              unpack16(v, x);
+              unpack16(load16(p), y);
+#pragma unroll
+              for (int e = 0; e < V; ++e) x[e] += y[e];
+              store16(p, pack16(x));
+            } else {
+              store16(p, v);
+            }
+          } else {  // 4 BF16 elements: columns % 4 == 0
+            *reinterpret_cast<u2*>(p) = u2{v.x, v.y};
+          }
+        });
+      }
+    }
+  }
+};
+
+// The parts [splits][rows of m][dim] added in order, times the factor, into the rows that `map` names.
+template <class T>
+__global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restrict__ parts, int32_t splits,
+                                                          int64_t part, const int32_t* __restrict__ live,
+                                                          int64_t rows, FastDiv d4,
+                                                          const int32_t* __restrict__ map,
+                                                          const float* __restrict__ factor,
+                                                          T* __restrict__ out, int64_t pitch,
+                                                          int64_t row0) {
+  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+  const uint32_t q = quotient(uint32_t(i), d4);
+  const int64_t at = row0 + q;
+  const int c = int(uint32_t(i) - q * d4.div) * 4;
+  const int64_t end = live != nullptr ? int64_t(*live) : rows;
+  if (i >= (rows - row0) * int64_t(d4.div) || at >= end) return;
+  const float* p = parts + at * (int64_t(d4.div) * 4) + c;
+  f4 s = load4(p);
+#pragma unroll 4
+  for (int z = 1; z < splits; ++z) s += load4(p + z * part);
+  const float f = *factor;
+  store4(out + (map != nullptr ? int64_t(map[at]) : at) * pitch + c, s * f);
+}
+
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Tile shapes: columns and rows.
+struct Shape {
+  int bn, bm;
+  // Columns of a wavefront, which a part of a row's sum covers.
+  int part() const { return bn == 256 ? 128 : bm == 128 ? 64 : 32; }
+};
+
+// Everything that the sizes decide.
+struct Plan {
+  bool f32;            // three terms of everything
+  int terms;           // of D
+  int pairs;           // of planes, in the gradients' products
+  bool pack;           // whether W is packed
+  int32_t padded;      // elements of a packed row
+  int64_t piece;       // columns of the vocabulary at a time (a multiple of 256)
+  Shape scores, dx, dw;
+  int32_t dx_splits, dx_per, dw_splits, dw_per;
+  // Workspace.
+  size_t place, row, tokens, target, x, parts, w, d, dxp, dwp, total;
+};
+
+// Of m rows (an upper bound) and n columns, in `rest` further blocks of work (splits that may be had).
+Shape shape_of(int64_t m, int64_t n, int64_t rest) {
+  if (m <= 32) return {128, 32};
+  if (m <= 64) return {128, 64};
+  if (up(m, 256) * up(n, 256) * rest >= kNumCu * 3 / 4 && n > 128 && m > 128) return {256, 256};
+  return {128, 128};
+}
+// Splits of `steps` steps that fill the chip with tiles.
+void split_steps(int64_t tiles, int64_t steps, int resident, int32_t* splits, int32_t* per) {
+  int64_t s = int64_t(kNumCu) * resident / (tiles > 0 ? tiles : 1);
+  if (s > steps / 8) s = steps / 8;
+  if (s < 1) s = 1;
+  if (steps < 1) steps = 1;
+  *per = int32_t(up(steps, s));
+  *splits = int32_t(up(steps, *per));
+}
+
+Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) {
+  Plan p = {};
+  p.f32 = f32;
+  const int planes = f32 ? 3 : 1;
+  // Few rows: the products' time is W's way from memory, and a second term of D costs little.
+  p.terms = f32 ? 3 : rows <= 256 ? 2 : 1;
+  p.pairs = f32 ? 6 : p.terms;
+  p.pack = f32 || dim % 8 != 0;
+  p.padded = (dim + kStepK - 1) / kStepK * kStepK;
+  int64_t piece = up(vocab, 256) * 256;
+  auto at_most = [&](int64_t v) {
+    v = v / 256 * 256;
+    if (v < 256) v = 256;
+    if (piece > v) piece = v;
+  };
+  at_most(kMaxPitch);
+  if (backward) at_most(kPieceBytes * 2 / (int64_t(rows > 0 ? rows : 1) * 2 * p.terms));
+  if (p.pack) at_most(kPieceBytes * 2 / (int64_t(p.padded) * 2 * planes));
+  const int64_t pieces = up(vocab, piece);
+  p.piece = up(up(vocab, pieces), 256) * 256;  // pieces of one size
+  size_t at = 256;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += align256(bytes);
+    return was;
+  };
+  p.place = take(size_t(rows) * 4);
+  p.row = take(size_t(rows) * 4);
+  p.tokens = take(size_t(rows) * sizeof(Token));
+  p.target = take(size_t(rows) * 4);
+  p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
+  p.scores = shape_of(rows, p.piece, 1);
+  p.parts = take(size_t(up(vocab, p.scores.part())) * size_t(rows) * sizeof(float2));
+  p.w = p.pack ? take(size_t(p.piece) * size_t(p.padded) * 2 * planes) : 0;
+  if (backward) {
+    p.d = take(size_t(rows) * size_t(p.piece) * 2 * p.terms);
+    p.dx = shape_of(rows, dim, 16);
+    split_steps(up(rows, p.dx.bm) * up(dim, p.dx.bn), up(p.piece, kStepK), p.dx.bn == 256 ? 1 : 2,
+                &p.dx_splits, &p.dx_per);
+    p.dxp = take(size_t(p.dx_splits) * size_t(rows) * size_t(dim) * 4);
+    p.dw = shape_of(p.piece, dim, 1);
+    split_steps(up(p.piece, p.dw.bm) * up(dim, p.dw.bn), up(rows, kStepK), p.dw.bn == 256 ? 1 : 2,
+                &p.dw_splits, &p.dw_per);
+    if (p.dw_splits > 1) p.dwp = take(size_t(p.dw_splits) * size_t(p.piece) * size_t(dim) * 4);
+  }
+  p.total = at;
+  return p;
+}
+
+template <bool AT, bool BT, bool LIVE_K, class Epi>
+void run_gemm(const Gemm& g, const Epi& epi, Shape s, hipStream_t st) {
+  if (s.bn == 256)
+    launch_gemm<4, 4, 2, 2, 4, 1, AT, BT, LIVE_K>(g, epi, 2, st);
+  else if (s.bm == 128)
+    launch_gemm<2, 2, 2, 2, 3, 2, AT, BT, LIVE_K>(g, epi, 8, st);
+  else if constexpr (!BT) {
+    if (s.bm == 64)
+      launch_gemm<1, 2, 4, 1, 4, 2, AT, BT, LIVE_K>(g, epi, 8, st);
+    else
+      launch_gemm<1, 1, 4, 1, 4, 2, AT, BT, LIVE_K>(g, epi, 8, st);
+  }
+}
+
+template <int TERMS, class TX, class TW>
+hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t* status, hipStream_t st) {
+  const int32_t N = a.rows, E = a.dim;
+  const int64_t V = a.vocab;
+  Head* head = reinterpret_cast<Head*>(ws);
+  Rows rows = {head, reinterpret_cast<int32_t*>(ws + p.place), reinterpret_cast<int32_t*>(ws + p.row),
+               reinterpret_cast<Token*>(ws + p.tokens), reinterpret_cast<float*>(ws + p.target)};
+  __bf16* xp = reinterpret_cast<__bf16*>(ws + p.x);
+  float2* parts = reinterpret_cast<float2*>(ws + p.parts);
+  __bf16* wp = reinterpret_cast<__bf16*>(ws + p.w);
+  __bf16* d = reinterpret_cast<__bf16*>(ws + p.d);
+  float* dxp = reinterpret_cast<float*>(ws + p.dxp);
+  const TX* x = static_cast<const TX*>(a.x);
+  const TW* w = static_cast<const TW*>(a.table);
+  TX* dx = static_cast<TX*>(a.grad_x);
+  TW* dw = static_cast<TW*>(a.grad_table);
+  const int64_t xplane = int64_t(N) * p.padded, wplane = p.piece * p.padded;
+
+  hipLaunchKernelGGL(xent_rows, dim3(1), dim3(1024), 0, st, a.labels, a.row_weights, N, int32_t(V), a.scale,
+                     rows, a.loss, status);
+  if (N > 0)
+    hipLaunchKernelGGL((xent_pack_x<TERMS, TX>), dim3(unsigned(up(N, kWavesPerBlock))), dim3(kBlock), 0, st, x,
+                     a.x_stride, N, E, p.padded, rows.place, xp, xplane, dx, a.grad_x_stride);
+
+  const int64_t xpitch = int64_t(p.padded) * 2;
+  const Side xs = {xp, xpitch, xplane * 2};
+  int64_t packed = -1;  // the piece that wp holds
+  auto side_w = [&](int64_t v0, int64_t n) {
+    if (!p.pack) return Side{w + v0 * a.table_stride, a.table_stride * 2, 0};
+    if (packed != v0) {
+      const FastDiv chunks = fast_div(uint32_t(p.padded / 8));
+      hipLaunchKernelGGL((xent_pack_w<TERMS, TW>), dim3(unsigned(up(n * (p.padded / 8), kBlock))),
+                         dim3(kBlock), 0, st, w + v0 * a.table_stride, a.table_stride, n, E, chunks, wp,
+                         wplane);
+      packed = v0;
+    }
+    return Side{wp, xpitch, wplane * 2};
+  };
+  const int32_t pairs = TERMS == 3 ? 6 : 1;
+  const Shape ss = p.scores;
+  for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
+    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
+    const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, 1, int32_t(up(E, kStepK))};
+    run_gemm<false, false, false>(
+        g, StatsEpi{parts, N, rows.tokens, rows.target, a.scale, v0, n}, ss, st);
+  }
+  const int32_t count = int32_t(up(V, ss.part()));
+  if (N > 0 && N <= 16)
+    hipLaunchKernelGGL(xent_join<4>, dim3(unsigned(up(N, 4))), dim3(1024), 0, st, parts, int64_t(N),
+                       count, rows, a.loss);
+  else if (N > 0)
+    hipLaunchKernelGGL(xent_join<64>, dim3(unsigned(up(N, 64))), dim3(1024), 0, st, parts, int64_t(N),
+                       count, rows, a.loss);
+  if (dx == nullptr && dw == nullptr) return hipGetLastError();
+
+  const int64_t dplane = int64_t(N) * p.piece;
+  const Side ds = {d, p.piece * 2, dplane * 2};
+  const int64_t dpart = int64_t(N) * E;
+  for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
+    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
+    const Side wsd = side_w(v0, n);
+    const Gemm g = {wsd, xs, n, N, E, &head->live, pairs, 1, int32_t(up(E, kStepK))};
+    auto grad = [&](auto terms) {
+      run_gemm<false, false, false>(
+          g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, a.scale, v0, n}, ss, st);
+    };
+    if constexpr (TERMS == 3)
+      grad(std::integral_constant<int, 3>());
+    else if (p.terms == 2)
+      grad(std::integral_constant<int, 2>());
+    else
+      grad(std::integral_constant<int, 1>());
+    if (dx != nullptr) {
+      const Gemm gx = {wsd, ds, E, N, n, &head->live, p.pairs, p.dx_splits, p.dx_per};
+      run_gemm<true, false, false>(gx, StoreEpi<float>{dxp, E, E, nullptr, nullptr, dpart, v0 > 0},
+                                   p.dx, st);
+    }
+    if (dw != nullptr) {
+      const Gemm gw = {xs, ds, E, n, N, &head->live, p.pairs, p.dw_splits, p.dw_per};
+      const Shape sw = p.dw;
+      TW* to = dw + v0 * a.grad_table_stride;
+      if (p.dw_splits == 1) {
+        run_gemm<true, true, true>(gw, StoreEpi<TW>{to, a.grad_table_stride, E, nullptr, &head->factor, 0,
+                                                    false}, sw, st);
+      } else {
+        float* dwp = reinterpret_cast<float*>(ws + p.dwp);
+        run_gemm<true, true, true>(gw, StoreEpi<float>{dwp, E, E, nullptr, nullptr, p.piece * E, false}, sw,
+                                   st);
+        hipLaunchKernelGGL(xent_join_parts<TW>, dim3(unsigned(up(n * (E / 4), kBlock))), dim3(kBlock), 0, st,
+                           dwp, p.dw_splits, p.piece * E, nullptr, n, fast_div(uint32_t(E / 4)), nullptr,
+                           &head->factor, to, a.grad_table_stride, int64_t(0));
+      }
+    }
+  }
+  if (dx != nullptr) {
+    const int64_t most = (int64_t(1) << 30) / (E / 4);
+    for (int64_t r0 = 0; r0 < N; r0 += most) {
+      const int64_t n = N - r0 < most ? N - r0 : most;
+      hipLaunchKernelGGL(xent_join_parts<TX>, dim3(unsigned(up(n * (E / 4), kBlock))), dim3(kBlock), 0, st,
+                         dxp, p.dx_splits, dpart, &head->live, r0 + n, fast_div(uint32_t(E / 4)), rows.row,
+                         &head->factor, dx, a.grad_x_stride, r0);
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t xent_workspace(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) {
+  return plan_of(rows, vocab, dim, f32, backward).total;
+}
+
+hipError_t launch_xent(const embbag_xent_t& a, char* ws, int32_t* status, hipStream_t st) {
+  if (a.rows == 0 && a.grad_table == nullptr) return hipSuccess;
+  const bool xb = a.x_type == EMBBAG_BF16, wb = a.table_type == EMBBAG_BF16;
+  const Plan p = plan_of(a.rows, a.vocab, a.dim, !(xb && wb), a.grad_x != nullptr || a.grad_table != nullptr);
+  if (xb && wb) return launch_types<1, __bf16, __bf16>(a, p, ws, status, st);
+  if (xb) return launch_types<3, __bf16, float>(a, p, ws, status, st);
+  if (wb) return launch_types<3, float, __bf16>(a, p, ws, status, st);
+  return launch_types<3, float, float>(a, p, ws, status, st);
+}
+
+}  // namespace embbag

@@ -9,7 +9,8 @@ other entry points (device pointers and the current HIP stream to the C ABI of
 ``embbag_rmsnorm`` (into FP32, BF16 or 8-bit rows, ``Mx8Rows``), ``embbag_rmsnorm_grad``,
 ``embbag_mx8_dequantize``.  Logits:
 ``embbag_logits_process`` (penalties, biases, masks) and ``embbag_distill`` (loss
-and gradient against a teacher's top logits).
+and gradient against a teacher's top logits).  ``embbag_xent``: loss on labels over an
+FP32 or BF16 table, with the gradients of both sides, no logits kept.
 """
 from __future__ import annotations
 
@@ -68,6 +69,15 @@ class _RmsNormGrad(C.Structure):
                 ("dweight", C.c_void_p)]
 
 
+class _Xent(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("dim", C.c_int32), ("vocab", C.c_int64),
+                ("x_type", C.c_int32), ("x", C.c_void_p), ("x_stride", C.c_int64),
+                ("table_type", C.c_int32), ("table", C.c_void_p), ("table_stride", C.c_int64),
+                ("labels", C.c_void_p), ("row_weights", C.c_void_p), ("scale", C.c_float),
+                ("loss", C.c_void_p), ("grad_x", C.c_void_p), ("grad_x_stride", C.c_int64),
+                ("grad_table", C.c_void_p), ("grad_table_stride", C.c_int64)]
+
+
 # A call's arguments as the bytes of its structure (0.2 us; a ctypes object of 22 fields 1.0).
 _CODES = {C.c_int32: "i", C.c_int64: "q", C.c_void_p: "P", C.c_float: "f"}
 
@@ -85,6 +95,7 @@ def _packer(cls):
 
 
 _pack_logits, _pack_distill = _packer(_Logits), _packer(_Distill)
+_pack_xent = _packer(_Xent)
 _pack_norm, _pack_norm_grad = _packer(_RmsNorm), _packer(_RmsNormGrad)
 
 _ready = None
@@ -113,10 +124,12 @@ def _lib():
         L.embbag_rmsnorm.argtypes = [p, p]
         L.embbag_rmsnorm_grad_workspace_bytes.argtypes = [i64, i32]
         L.embbag_rmsnorm_grad.argtypes = [p, p, sz, p]
-        for n in ("mx8_dequantize", "mx4_matmul_x8", "rmsnorm", "rmsnorm_grad", "mx4_quantize", "mx4_dequantize", "mx4_forward", "mx4_matmul",
+        L.embbag_xent_workspace_bytes.argtypes = [i32, i64, i32, i32, i32]
+        L.embbag_xent.argtypes = [p, p, sz, p, p]
+        for n in ("xent", "mx8_dequantize", "mx4_matmul_x8", "rmsnorm", "rmsnorm_grad", "mx4_quantize", "mx4_dequantize", "mx4_forward", "mx4_matmul",
                   "mx4_matmul_grad", "logits_process", "distill"):
             getattr(L, "embbag_" + n).restype = C.c_int
-        for n in ("rmsnorm_grad", "mx4_matmul_x8", "mx4_matmul", "mx4_matmul_grad", "distill"):
+        for n in ("xent", "rmsnorm_grad", "mx4_matmul_x8", "mx4_matmul", "mx4_matmul_grad", "distill"):
             getattr(L, f"embbag_{n}_workspace_bytes").restype = sz
         _ready = L
     return _ready
@@ -527,3 +540,29 @@ def embbag_distill(logits, teacher_ids, teacher_logits, temperature, loss, works
         _vector(loss, rows, "loss", _F32_T), q, lq)
     w, n = _ws(workspace)
     return _lib().embbag_distill(a, w, n, _status(d_status), _stream(stream))
+
+
+def embbag_xent_workspace_bytes(rows, vocab, dim, type, backward) -> int:
+    """``type``: EMBBAG_F32 if x or the table is FP32, else EMBBAG_BF16; ``backward``: whether a
+    gradient is wanted."""
+    return int(_lib().embbag_xent_workspace_bytes(_i32(int(rows)), int(vocab), _i32(int(dim)),
+                                                  int(type), 1 if backward else 0))
+
+
+def embbag_xent(x, table, labels, loss, workspace, grad_x=None, grad_table=None, row_weights=None,
+                scale=1.0, d_status=None, stream=None) -> int:
+    """Loss of every row of ``x`` [rows, dim] on its label among the rows of ``table`` [vocab, dim]
+    (scores ``scale`` x table^T; a negative label is no row to learn) and, into ``grad_x`` and
+    ``grad_table``, the gradients of the losses' sum."""
+    dim = x.shape[1] if len(x.shape) == 2 else -1
+    p, ty, ld = _matrix(x, dim, "x")
+    rows = x.shape[0]
+    w, tw, lw = _matrix(table, dim, "table")
+    vocab = table.shape[0]
+    g, _, lg = _same_rows(grad_x, rows, dim, "grad_x", ty, "x")
+    h, _, lh = _same_rows(grad_table, vocab, dim, "grad_table", tw, "table")
+    a = _pack_xent(_i32(rows), dim, vocab, ty, p, ld, tw, w, lw, _vector(labels, rows, "labels", _I32_T),
+                   _vector(row_weights, rows, "row_weights", _F32_T), scale,
+                   _vector(loss, rows, "loss", _F32_T), g, lg, h, lh)
+    ws, n = _ws(workspace)
+    return _lib().embbag_xent(a, ws, n, _status(d_status), _stream(stream))

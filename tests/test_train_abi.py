@@ -155,3 +155,53 @@ def test_scores_from_eight_bits_sizes():
     for shape in [(3, 10), (4, 11)]:
         with pytest.raises(ValueError):
             pk.embbag_mx4_matmul_x8(x, t, fake(*shape), None, stream=0)
+
+
+XENT = dict(rows=4, dim=64, vocab=1000, x_type=F32, x=FAKE, x_stride=64, table_type=F32, table=FAKE, table_stride=64,
+            labels=FAKE, scale=1.0, loss=FAKE, grad_x=FAKE, grad_x_stride=64, grad_table=FAKE, grad_table_stride=64)
+
+
+@pytest.mark.parametrize("change", [
+    dict(rows=-1), dict(rows=2 ** 20 + 1), dict(vocab=0), dict(vocab=2 ** 31), dict(rows=2 ** 20, vocab=2 ** 20 + 1),
+    dict(dim=0), dict(dim=6), dict(dim=16388), dict(x_type=2), dict(table_type=-1), dict(scale=float("nan")),
+    dict(scale=float("inf")), dict(scale=-float("inf")), dict(x=None), dict(x=FAKE + 4), dict(x_stride=62),
+    dict(x_stride=66), dict(table=None), dict(table=FAKE + 8), dict(table_stride=60), dict(table_stride=2 ** 19 + 4),
+    dict(labels=None), dict(loss=None), dict(grad_x=FAKE + 4), dict(grad_x_stride=60), dict(grad_table=FAKE + 8),
+    dict(grad_table_stride=65), dict(x_type=BF16, x=FAKE + 4), dict(rows=0, table=None),
+    dict(rows=0, grad_table=FAKE + 4)])
+def test_xent_refusals(L, change):
+    assert L.embbag_xent(packed(head._Xent, XENT, change), FAKE, 1 << 40, None, None) == BAD
+
+
+def test_xent_workspace(L):
+    need = pk.embbag_xent_workspace_bytes(4, 1000, 64, F32, True)
+    assert need > pk.embbag_xent_workspace_bytes(4, 1000, 64, F32, False) > 0 and need % 256 == 0
+    a = packed(head._Xent, XENT, {})
+    assert L.embbag_xent(a, FAKE, need - 1, None, None) == WS
+    assert L.embbag_xent(a, FAKE + 16, need, None, None) == WS
+    assert L.embbag_xent(a, None, need, None, None) == WS
+    assert L.embbag_xent(None, FAKE, need, None, None) == BAD
+    for r, v, e, t in [(-1, 10, 64, F32), (2 ** 20 + 1, 10, 64, F32), (4, 0, 64, F32), (4, 2 ** 31, 64, F32),
+                       (4, 10, 66, F32), (4, 10, 16388, F32), (4, 10, 64, 2), (2 ** 32 + 4, 10, 64, F32),
+                       (4, 10, 2 ** 32 + 64, F32), (2 ** 20, 2 ** 20 + 1, 64, F32)]:
+        assert pk.embbag_xent_workspace_bytes(r, v, e, t, True) == 0
+    # A piece of the vocabulary at a time: of D 512 MB at most.
+    assert pk.embbag_xent_workspace_bytes(4096, 2 ** 27, 256, BF16, True) < 2 ** 36
+    for r, v, e in [(0, 1, 4), (1, 1, 4), (2 ** 20, 2 ** 20, 16384), (1, 2 ** 31 - 1, 16384)]:
+        for t in (F32, BF16):
+            assert pk.embbag_xent_workspace_bytes(r, v, e, t, True) > 0
+
+
+def test_binding_refuses_wrong_labels_and_gradients():
+    x, w = fake(4, 64), fake(10, 64)
+    labels, loss = fake(4, dtype=torch.int32), fake(4)
+    ok = dict(x=x, table=w, labels=labels, loss=loss, workspace=None, stream=0)
+    for bad in (dict(labels=fake(3, dtype=torch.int32)), dict(loss=fake(5)), dict(table=fake(10, 60)),
+                dict(grad_x=fake(3, 64)), dict(grad_table=fake(10, 60)), dict(row_weights=fake(3))):
+        with pytest.raises(ValueError):
+            pk.embbag_xent(**dict(ok, **bad))
+    for bad in (dict(labels=fake(4, dtype=torch.int64)), dict(grad_x=fake(4, 64, dtype=torch.bfloat16)),
+                dict(grad_table=fake(10, 64, dtype=torch.bfloat16)), dict(x=fake(4, 64, dtype=torch.float16))):
+        with pytest.raises(TypeError):
+            pk.embbag_xent(**dict(ok, **bad))
+    assert pk.embbag_xent(**ok) == WS
