@@ -53,10 +53,12 @@ __device__ __forceinline__ void planes_of(int pairs, int i, int* pa, int* pb) {
 }
 
 typedef __attribute__((address_space(3))) void* LdsAny;
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int64_t bytes) {
-  const int64_t most = kFar - 1;
-  const int n = int(bytes < 0 ? 0 : bytes < most ? bytes : most);
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, n, 0x00020000);
+// (Addresses and sizes are the wavefront's; said so, they stay in scalar registers.)
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  const uint64_t u = uint64_t(uint32_t(scalar(int(a >> 32)))) << 32 | uint32_t(scalar(int(a)));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(u), 0, scalar(bytes), 0x00020000);
 }
 __device__ __forceinline__ void buffer_to_lds16(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff,
                                                 void* dst) {
@@ -85,45 +87,64 @@ struct Stream {
   static_assert(!TURNED || ROWS >= 64, "swizzle of turned rows");
   const uint8_t* base;
   int64_t left;      // bytes from base to the side's end
-  int64_t pitch;
-  uint32_t voff;     // of this lane in its wavefront's loads
+  int records;       // of them in the loads' buffer
+  uint32_t at;       // bytes from base to the step
+  uint32_t step;     // bytes of a step
+  uint32_t rows;     // bytes from a load's first row to the next load's
+  uint32_t voff;     // of this lane in a load
   int limit;         // rows of k: elements of k from this lane's chunk to the end
 
   __device__ __forceinline__ int number(int i, int wave) const { return (i * W + wave) % ALL; }
+  __device__ __forceinline__ void clamp() {
+    const int64_t most = kFar - 1;
+    records = int(left < 0 ? 0 : left < most ? left : most);
+  }
 
-  // The tile from row r0 of `rows`, the steps from k0 of `k` elements on.
-  __device__ __forceinline__ void open(const Side& s, int plane, int64_t r0, int64_t rows, int64_t k0,
+  // The tile from row r0 of `total`, the steps from k0 of `k` elements on.
+  __device__ __forceinline__ void open(const Side& s, int plane, int64_t r0, int64_t total, int64_t k0,
                                        int64_t k, int lane, int wave) {
-    pitch = s.pitch;
+    const int64_t pitch = s.pitch;
     const uint8_t* p = static_cast<const uint8_t*>(s.data) + plane * s.plane;
     if constexpr (TURNED) {
       base = p + k0 * pitch + r0 * 2;
-      left = (k - k0 - 1) * pitch + (rows - r0 + 7) / 8 * 16;
+      left = (k - k0 - 1) * pitch + (total - r0 + 7) / 8 * 16;
       constexpr int PER = 64 / KROWS;  // lanes per row
       const int kk = lane / PER;
       const int sw = KROWS == 8 ? (kk >> 1 & 1) : KROWS == 4 ? kk : (wave & 1) * 2 + kk;
       voff = uint32_t(kk * pitch) + uint32_t((lane % PER) ^ (sw * 4)) * 16;
       static_assert(KROWS > 2 || W % 2 == 0, "a load's parity is its wavefront's");
+      step = uint32_t(kStepK * pitch);
+      rows = uint32_t(KROWS * pitch);
     } else {
       base = p + r0 * pitch + k0 * 2;
-      left = (rows - r0 - 1) * pitch + (k - k0 + 7) / 8 * 16;
+      left = (total - r0 - 1) * pitch + (k - k0 + 7) / 8 * 16;
       const int c = (lane % 4) ^ (lane / 16);
       voff = uint32_t(lane / 4 * pitch) + uint32_t(c) * 16;
       limit = int(k - k0) - c * 8;
+      step = kStepBytes;
+      rows = uint32_t(16 * pitch);
     }
     if (k <= k0) left = 0;
+    at = 0;
+    clamp();
   }
   __device__ __forceinline__ void advance() {
-    const int64_t step = TURNED ? kStepK * pitch : kStepBytes;
-    base += step;
-    left -= step;
-    if constexpr (!TURNED) limit -= kStepK;
+    at += step;
+    if constexpr (TURNED) {
+      if (at >= kFar / 4) {  // (the buffer's offsets and a step's rows stay below kFar)
+        base += at;
+        left -= at;
+        at = 0;
+        clamp();
+      }
+    } else {
+      limit -= kStepK;
+    }
   }
   __device__ __forceinline__ void load(int i, int wave, uint8_t* dst) const {
     const int l = number(i, wave);
-    const uint32_t soff = uint32_t(l) * uint32_t((TURNED ? KROWS : 16) * pitch);
     const uint32_t v = !TURNED && limit <= 0 ? kFar : voff;
-    buffer_to_lds16(buffer_of(base, left), v, soff, dst + l * 1024);
+    buffer_to_lds16(buffer_of(base, records), v, at + uint32_t(l) * rows, dst + l * 1024);
   }
 };
 
@@ -245,38 +266,27 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
       a[p][i - TM] = fragment(cur, std::integral_constant<bool, AT>(), std::integral_constant<int, BN>(), 0,
                               wn * TN + i - TM, p);
   };
-  auto products = [&](int p, int i) {
+  // The products of part p, and after every one of them what a wavefront alone on its SIMD can issue while
+  // it runs (an instruction per 4 cycles, a product takes 32): in the first half the reads of the next part's
+  // fragments (part `next` of `cur`), in the second half that half step's loads of a later step, which go to
+  // `nxt`.
+  auto part = [&](const uint8_t* __restrict__ cur, uint8_t* __restrict__ nxt, int p, int next) {
+    constexpr int N = TN + TM, SLOTS = TN * TM, EARLY = SLOTS > 1 ? SLOTS / 2 : 1, LATE = SLOTS - SLOTS / 2;
+    constexpr int HALF = (PER + 1) / 2;
 #pragma unroll
-    for (int j = 0; j < TM; ++j)
+    for (int s = 0; s < SLOTS; ++s) {
+      const int i = s / TM, j = s % TM;
       acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a[p][i]),
                                                           __builtin_bit_cast(bf8, b[p][j]), acc[i][j], 0,
                                                           0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  // The products of the part before, and between their rows the reads of the next part's fragments and the
-  // loads of a later step, which go to `nxt`.
-  auto step_of = [&](const uint8_t* __restrict__ cur, uint8_t* __restrict__ nxt) {
-    constexpr int N = TN + TM, READS = TN > 1 ? TN - 1 : 1;
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      products(1, i);
-#pragma unroll
-      for (int r = 0; r < N; ++r)
-        if (r * READS / N == i) fetch(cur, 0, r);
-#pragma unroll
-      for (int l = 0; l < PER; ++l)
-        if (l * 2 * TN / PER == i) load(nxt, l);
+      if (next < 0) continue;
       __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      products(0, i);
 #pragma unroll
       for (int r = 0; r < N; ++r)
-        if (r * READS / N == i) fetch(cur, 1, r);
+        if (r * EARLY / N == s) fetch(cur, next, r);
 #pragma unroll
       for (int l = 0; l < PER; ++l)
-        if (l * 2 * TN / PER == TN + i) load(nxt, l);
+        if (l / HALF == next && SLOTS / 2 + l % HALF * LATE / HALF == s) load(nxt, l);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -301,11 +311,11 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
       wait_loads<(STAGES - 2) * PER>();
       block_barrier();
       const int free = cur == 0 ? STAGES - 1 : cur - 1;
-      step_of(lds + cur * STAGE, lds + free * STAGE);
+      part(lds + cur * STAGE, lds + free * STAGE, 1, 0);
+      part(lds + cur * STAGE, lds + free * STAGE, 0, 1);
       cur = cur == STAGES - 1 ? 0 : cur + 1;
     }
-#pragma unroll
-    for (int i = 0; i < TN; ++i) products(1, i);
+    part(lds, lds, 1, -1);
     // (The next tile's first products take no fragments.)
 #pragma unroll
     for (int i = 0; i < TN; ++i) a[1][i] = u4{0u, 0u, 0u, 0u};

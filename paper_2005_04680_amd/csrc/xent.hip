@@ -22,7 +22,7 @@
 namespace embbag {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of D, of W's terms: a piece's
 constexpr int64_t kMaxPitch = int64_t(1) << 19;       // elements of a row of D
 
@@ -41,10 +41,20 @@ __device__ __forceinline__ void nearest_terms(float x, float (&t)[3]) {
   t[2] = rest - t[1];
 }
 
+// Scores enter the exponentials as 2^(score * log2(e)), in one FMA: their sums are taken with x times the
+// scale's sign, of which `unit` = |scale| log2(e) makes the exponent.  (A scale of 0 makes x 0, and its
+// unit is any.)
+__host__ __device__ __forceinline__ float sign_of(float scale) {
+  return scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
+}
+__host__ __device__ __forceinline__ float unit_of(float scale) {
+  return scale == 0.f ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
+}
+
 // What the backward needs of a row that counts.
 struct Token {
-  float top;    // its largest score
-  float inv;    // 1 / the sum of exp(score - top)
+  float top;    // about its largest score's exponent
+  float inv;    // 1 / the sum of 2^(exponent - top)
   float ratio;  // its weight over the largest
   int label;
 };
@@ -53,7 +63,8 @@ struct Token {
 struct Head {
   int32_t live;   // rows that count
   float largest;  // of their weights' magnitudes
-  float factor;   // scale * largest
+  float factor;   // scale * largest, of dx
+  float factor_w; // |scale| * largest, of dW (x has the scale's sign)
 };
 
 struct Rows {
@@ -61,7 +72,7 @@ struct Rows {
   int32_t* place;  // [rows]: among the rows that count, or -1
   int32_t* row;    // [live]: the row at a place
   Token* tokens;   // [live]
-  float* target;   // [live]: the label's score
+  float* target;   // [live]: the label's sum
 };
 
 // Which rows count, their places in order, and the largest weight.  One block; the losses of the others
@@ -131,16 +142,18 @@ __global__ __launch_bounds__(1024) void xent_rows(const int32_t* __restrict__ la
     out.head->live = base;
     out.head->largest = top;
     out.head->factor = scale * top;
+    out.head->factor_w = fabsf(scale) * top;
   }
 }
 
-// 8 elements of a row from e on (zeros past dim; dim % 4 == 0) as BF16 terms to `dst`.
+// 8 elements of a row from e on (zeros past dim; dim % 4 == 0) times the sign as BF16 terms to `dst`.
 template <int TERMS, class T>
-__device__ __forceinline__ void pack8(const T* row, int e, int dim, __bf16* dst, int64_t plane) {
+__device__ __forceinline__ void pack8(const T* row, int e, int dim, float sign, __bf16* dst, int64_t plane) {
   const f4 zero = {0.f, 0.f, 0.f, 0.f};
   const f4 p = e < dim ? load4(row + e) : zero;
   const f4 q = e + 4 < dim ? load4(row + e + 4) : zero;
-  const float v[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+  const float v[8] = {p.x * sign, p.y * sign, p.z * sign, p.w * sign,
+                      q.x * sign, q.y * sign, q.z * sign, q.w * sign};
   if constexpr (TERMS == 1) {
     store16(dst, pack16(v));
   } else {
@@ -156,10 +169,10 @@ __device__ __forceinline__ void pack8(const T* row, int e, int dim, __bf16* dst,
   }
 }
 
-// x's rows that count as TERMS planes [live][padded]; dx's others as zeros.  A wavefront per row.
+// x's rows that count, times the sign, as TERMS planes [live][padded]; dx's others as zeros.  A wavefront per row.
 template <int TERMS, class T>
 __global__ __launch_bounds__(kBlock) void xent_pack_x(const T* __restrict__ x, int64_t stride,
-                                                      int32_t rows, int32_t dim, int32_t padded,
+                                                      int32_t rows, int32_t dim, int32_t padded, float sign,
                                                       const int32_t* __restrict__ place,
                                                       __bf16* __restrict__ out, int64_t plane,
                                                       T* __restrict__ dx, int64_t dx_stride) {
@@ -173,7 +186,7 @@ __global__ __launch_bounds__(kBlock) void xent_pack_x(const T* __restrict__ x, i
     return;
   }
   for (int e = lane_id() * 8; e < padded; e += kWave * 8)
-    pack8<TERMS>(x + r * stride, e, dim, out + int64_t(at) * padded + e, plane);
+    pack8<TERMS>(x + r * stride, e, dim, sign, out + int64_t(at) * padded + e, plane);
 }
 
 // Rows of W as TERMS planes [rows][padded].
@@ -185,17 +198,17 @@ __global__ __launch_bounds__(kBlock) void xent_pack_w(const T* __restrict__ w, i
   if (i >= rows * chunks.div) return;
   const uint32_t r = quotient(uint32_t(i), chunks);
   const int e = int(uint32_t(i) - r * chunks.div) * 8;
-  pack8<TERMS>(w + int64_t(r) * stride, e, dim, out + i * 8, plane);
+  pack8<TERMS>(w + int64_t(r) * stride, e, dim, 1.f, out + i * 8, plane);
 }
 
-// A tile's parts: of each row and 128 columns (a wavefront's: 32 TN) the largest score and the sum of the
-// exponentials of the others' distances to it.
+// A tile's parts: of each row and the wavefront's 32 TN columns the exponent of the largest score, rounded,
+// and the sum of the exponentials beside exactly that.
 struct StatsEpi {
   float2* parts;         // [columns / (32 TN)][pitch]
   int64_t pitch;
   const Token* tokens;
   float* target;
-  float scale;
+  float unit;
   int64_t first;         // the piece's first column
   int64_t columns;       // of the piece
   template <int TN, int TM>
@@ -205,40 +218,43 @@ struct StatsEpi {
   __device__ __forceinline__ void operator()(f16v (&acc)[TN][TM], int64_t n, int64_t m, int64_t m_end, int,
                                              uint8_t*) const {
     const int row = lane_id() % 32, half = lane_id() / 32;
-    const bool whole = n + 32 * TN <= columns;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const int64_t at = m + j * 32 + row;
       const bool in = at < m_end;
+      if (n + 32 * TN > columns) {
+        const int64_t left = columns - n - half * 4;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            acc[i][j][r] = i * 32 + r / 4 * 8 + r % 4 < left ? acc[i][j][r] : low();
+      }
       float top = low();
 #pragma unroll
       for (int i = 0; i < TN; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int c = i * 32 + r / 4 * 8 + half * 4 + r % 4;
-          acc[i][j][r] = whole || n + c < columns ? acc[i][j][r] * scale : low();
-          top = fmaxf(top, acc[i][j][r]);
-        }
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float ref = top == low() ? 0.f : top;
+      const float ref = top == low() ? 0.f : -(top * unit);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < TN; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += exp2_of((acc[i][j][r] - ref) * kLog2e);
+        for (int r = 0; r < 16; ++r) sum += exp2_of(__builtin_fmaf(acc[i][j][r], unit, ref));
       sum += __shfl_xor(sum, 32, kWave);
       const int label = in ? tokens[at].label : -1;
-      const int64_t place = label - first - n;  // of the label among the wavefront's columns
-      if (place >= 0 && place < 32 * TN && (place / 4 % 2) == half) {
+      const int64_t place = label - first - n - half * 4;  // of the label among the lane's columns
+      if (place >= 0 && place < 32 * TN && place / 4 % 2 == 0) {
         float z = 0.f;
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (place == i * 32 + r / 4 * 8 + half * 4 + r % 4) z = acc[i][j][r];
+            if (int(place) == i * 32 + r / 4 * 8 + r % 4) z = acc[i][j][r];
         target[at] = z;
       }
-      if (in && half == 0 && n < columns) parts[((first + n) / (32 * TN)) * pitch + at] = float2{top, sum};
+      if (in && half == 0 && n < columns) parts[((first + n) / (32 * TN)) * pitch + at] = float2{top * unit, sum};
     }
   }
 };
@@ -246,7 +262,8 @@ struct StatsEpi {
 // Joins the parts of TOKENS rows per block; losses, and what the backward needs.
 template <int TOKENS>
 __global__ __launch_bounds__(1024) void xent_join(const float2* __restrict__ parts, int64_t pitch,
-                                                  int32_t count, Rows rows, float* __restrict__ loss) {
+                                                  int32_t count, float unit, Rows rows,
+                                                  float* __restrict__ loss) {
   constexpr int SLICES = 1024 / TOKENS;
   __shared__ float2 shared[SLICES][TOKENS + 1];
   const int live = rows.head->live;
@@ -256,7 +273,7 @@ __global__ __launch_bounds__(1024) void xent_join(const float2* __restrict__ par
   float top = low(), sum = 0.f;
   auto add = [&](float2 p) {
     const float m = fmaxf(top, p.x), ref = m == low() ? 0.f : m;
-    sum = sum * exp2_of((top - ref) * kLog2e) + p.y * exp2_of((p.x - ref) * kLog2e);
+    sum = sum * exp2_of(top - ref) + p.y * exp2_of(p.x - ref);
     top = m;
   };
   if (at < live) {
@@ -276,7 +293,7 @@ __global__ __launch_bounds__(1024) void xent_join(const float2* __restrict__ par
   Token k = rows.tokens[at];
   const float w = k.ratio;
   const int r = rows.row[at];
-  loss[r] = w * ((top - rows.target[at]) + __builtin_logf(sum));
+  loss[r] = w * (__builtin_fmaf(-rows.target[at], unit, top) * kLn2 + __builtin_logf(sum));
   k.top = top, k.inv = 1.f / sum, k.ratio = w / rows.head->largest;
   rows.tokens[at] = k;
 }
@@ -318,7 +335,7 @@ struct GradEpi {
   __bf16* d;
   int64_t pitch, plane;
   const Token* tokens;
-  float scale;
+  float unit;
   int64_t first, columns;
   template <int TN, int TM>
   static constexpr int kScratch = 32 * kTurnPitch<__bf16, TN> * 2;
@@ -332,15 +349,33 @@ struct GradEpi {
     for (int j = 0; j < TM; ++j) {
       const int64_t at = m + j * 32 + row;
       const Token t = at < m_end ? tokens[at] : Token{0.f, 0.f, 0.f, -1};
-      const int64_t place = t.label - first - n;
+      const float c = t.inv * t.ratio;
+      const int64_t place = t.label - first - n - half * 4;  // of the label among the lane's columns
+      const bool mine = place >= 0 && place < 32 * TN && place / 4 % 2 == 0;
+      if (__builtin_amdgcn_ballot_w64(mine) != 0ull) {
 #pragma unroll
-      for (int i = 0; i < TN; ++i)
+        for (int i = 0; i < TN; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int c = i * 32 + r / 4 * 8 + half * 4 + r % 4;
-          const float p = exp2_of((acc[i][j][r] * scale - t.top) * kLog2e) * t.inv;
-          acc[i][j][r] = n + c < columns ? (place == c ? p - 1.f : p) * t.ratio : 0.f;
-        }
+          for (int r = 0; r < 16; ++r) {
+            const float e = exp2_of(__builtin_fmaf(acc[i][j][r], unit, -t.top));
+            const bool label = mine && int(place) == i * 32 + r / 4 * 8 + r % 4;
+            acc[i][j][r] = label ? (e * t.inv - 1.f) * t.ratio : e * c;
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            acc[i][j][r] = exp2_of(__builtin_fmaf(acc[i][j][r], unit, -t.top)) * c;
+      }
+      if (n + 32 * TN > columns) {
+        const int64_t left = columns - n - half * 4;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            acc[i][j][r] = i * 32 + r / 4 * 8 + r % 4 < left ? acc[i][j][r] : 0.f;
+      }
 #pragma unroll
       for (int h = 0; h < TN; h += kTiles<__bf16, TN>) {
 #pragma unroll
@@ -564,13 +599,14 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   const TW* w = static_cast<const TW*>(a.table);
   TX* dx = static_cast<TX*>(a.grad_x);
   TW* dw = static_cast<TW*>(a.grad_table);
+  const float unit = unit_of(a.scale);
   const int64_t xplane = int64_t(N) * p.padded, wplane = p.piece * p.padded;
 
   hipLaunchKernelGGL(xent_rows, dim3(1), dim3(1024), 0, st, a.labels, a.row_weights, N, int32_t(V), a.scale,
                      rows, a.loss, status);
   if (N > 0)
     hipLaunchKernelGGL((xent_pack_x<TERMS, TX>), dim3(unsigned(up(N, kWavesPerBlock))), dim3(kBlock), 0, st, x,
-                     a.x_stride, N, E, p.padded, rows.place, xp, xplane, dx, a.grad_x_stride);
+                     a.x_stride, N, E, p.padded, sign_of(a.scale), rows.place, xp, xplane, dx, a.grad_x_stride);
 
   const int64_t xpitch = int64_t(p.padded) * 2;
   const Side xs = {xp, xpitch, xplane * 2};
@@ -592,15 +628,15 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
     const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, 1, int32_t(up(E, kStepK))};
     run_gemm<false, false, false>(
-        g, StatsEpi{parts, N, rows.tokens, rows.target, a.scale, v0, n}, ss, st);
+        g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n}, ss, st);
   }
   const int32_t count = int32_t(up(V, ss.part()));
   if (N > 0 && N <= 16)
     hipLaunchKernelGGL(xent_join<4>, dim3(unsigned(up(N, 4))), dim3(1024), 0, st, parts, int64_t(N),
-                       count, rows, a.loss);
+                       count, unit, rows, a.loss);
   else if (N > 0)
     hipLaunchKernelGGL(xent_join<64>, dim3(unsigned(up(N, 64))), dim3(1024), 0, st, parts, int64_t(N),
-                       count, rows, a.loss);
+                       count, unit, rows, a.loss);
   if (dx == nullptr && dw == nullptr) return hipGetLastError();
 
   const int64_t dplane = int64_t(N) * p.piece;
@@ -612,7 +648,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     const Gemm g = {wsd, xs, n, N, E, &head->live, pairs, 1, int32_t(up(E, kStepK))};
     auto grad = [&](auto terms) {
       run_gemm<false, false, false>(
-          g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, a.scale, v0, n}, ss, st);
+          g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, unit, v0, n}, ss, st);
     };
     if constexpr (TERMS == 3)
       grad(std::integral_constant<int, 3>());
@@ -630,7 +666,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       const Shape sw = p.dw;
       TW* to = dw + v0 * a.grad_table_stride;
       if (p.dw_splits == 1) {
-        run_gemm<true, true, true>(gw, StoreEpi<TW>{to, a.grad_table_stride, E, nullptr, &head->factor, 0,
+        run_gemm<true, true, true>(gw, StoreEpi<TW>{to, a.grad_table_stride, E, nullptr, &head->factor_w, 0,
                                                     false}, sw, st);
       } else {
         float* dwp = reinterpret_cast<float*>(ws + p.dwp);
@@ -638,7 +674,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
                                    st);
         hipLaunchKernelGGL(xent_join_parts<TW>, dim3(unsigned(up(n * (E / 4), kBlock))), dim3(kBlock), 0, st,
                            dwp, p.dw_splits, p.piece * E, nullptr, n, fast_div(uint32_t(E / 4)), nullptr,
-                           &head->factor, to, a.grad_table_stride, int64_t(0));
+                           &head->factor_w, to, a.grad_table_stride, int64_t(0));
       }
     }
   }
