@@ -18,62 +18,13 @@
 // operands, and D with them, are the sum of three BF16 terms, of whose nine products six are taken: what
 // is left out is below 2^-22 of each product.
 #include "gemm.hpp"
+#include "xent.hpp"
 
 namespace embbag {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of D, of W's terms: a piece's
 constexpr int64_t kMaxPitch = int64_t(1) << 19;       // elements of a row of D
-
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// x as the sum of three BF16 terms, each the nearest to what is left (the first by truncation where
-// rounding would pass the range).  A NaN is its own first term.  An infinity is its own last one: that term
-// meets the other side's first alone, so that the product is an infinity of the right sign.
-__device__ __forceinline__ void nearest_terms(float x, float (&t)[3]) {
-  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
-  t[0] = float(__bf16(x));
-  if (u > 0x7F7F7FFFu && u < 0x7F800000u) t[0] = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-  if (u == 0x7F800000u) t[0] = 0.f;
-  const float rest = u > 0x7F800000u ? 0.f : x - t[0];
-  t[1] = u == 0x7F800000u ? 0.f : float(__bf16(rest));
-  t[2] = rest - t[1];
-}
-
-// Scores enter the exponentials as 2^(score * log2(e)), in one FMA: their sums are taken with x times the
-// scale's sign, of which `unit` = |scale| log2(e) makes the exponent.  (A scale of 0 makes x 0, and its
-// unit is any.)
-__host__ __device__ __forceinline__ float sign_of(float scale) {
-  return scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
-}
-__host__ __device__ __forceinline__ float unit_of(float scale) {
-  return scale == 0.f ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
-}
-
-// What the backward needs of a row that counts.
-struct Token {
-  float top;    // about its largest score's exponent
-  float inv;    // 1 / the sum of 2^(exponent - top)
-  float ratio;  // its weight over the largest
-  int label;
-};
-
-// In the workspace.
-struct Head {
-  int32_t live;   // rows that count
-  float largest;  // of their weights' magnitudes
-  float factor;   // scale * largest, of dx
-  float factor_w; // |scale| * largest, of dW (x has the scale's sign)
-};
-
-struct Rows {
-  Head* head;
-  int32_t* place;  // [rows]: among the rows that count, or -1
-  int32_t* row;    // [live]: the row at a place
-  Token* tokens;   // [live]
-  float* target;   // [live]: the label's sum
-};
 
 // Which rows count, their places in order, and the largest weight.  One block; the losses of the others
 // are 0.
@@ -491,6 +442,8 @@ struct Shape {
 
 // Everything that the sizes decide.
 struct Plan {
+  bool narrow;         // the products of xent_narrow.hip
+  Narrow nar;
   bool f32;            // three terms of everything
   int terms;           // of D
   int pairs;           // of planes, in the gradients' products
@@ -529,6 +482,30 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   p.pairs = f32 ? 6 : p.terms;
   p.pack = f32 || dim % 8 != 0;
   p.padded = (dim + kStepK - 1) / kStepK * kStepK;
+  size_t at = 256;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += align256(bytes);
+    return was;
+  };
+  p.place = take(size_t(rows) * 4);
+  p.row = take(size_t(rows) * 4);
+  p.tokens = take(size_t(rows) * sizeof(Token));
+  p.target = take(size_t(rows) * 4);
+  p.narrow = dim <= kNarrow;
+  if (p.narrow) {
+    p.padded = dim <= 64 ? 64 : 128;
+    p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
+    p.nar = narrow_plan(rows, vocab, dim, f32);
+    const size_t parts = size_t(p.nar.splits) * p.nar.parts;
+    p.parts = take(parts * size_t(rows) * sizeof(float2));
+    if (backward) {
+      p.dxp = take(parts * size_t(rows) * size_t(dim) * 4);
+      if (p.nar.dw_splits > 1) p.dwp = take(size_t(p.nar.dw_splits) * size_t(vocab) * size_t(dim) * 4);
+    }
+    p.total = at;
+    return p;
+  }
   int64_t piece = up(vocab, 256) * 256;
   auto at_most = [&](int64_t v) {
     v = v / 256 * 256;
@@ -540,16 +517,6 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   if (p.pack) at_most(kPieceBytes * 2 / (int64_t(p.padded) * 2 * planes));
   const int64_t pieces = up(vocab, piece);
   p.piece = up(up(vocab, pieces), 256) * 256;  // pieces of one size
-  size_t at = 256;
-  auto take = [&](size_t bytes) {
-    const size_t was = at;
-    at += align256(bytes);
-    return was;
-  };
-  p.place = take(size_t(rows) * 4);
-  p.row = take(size_t(rows) * 4);
-  p.tokens = take(size_t(rows) * sizeof(Token));
-  p.target = take(size_t(rows) * 4);
   p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
   p.scores = shape_of(rows, p.piece, 1);
   p.parts = take(size_t(up(vocab, p.scores.part())) * size_t(rows) * sizeof(float2));
@@ -608,6 +575,53 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     hipLaunchKernelGGL((xent_pack_x<TERMS, TX>), dim3(unsigned(up(N, kWavesPerBlock))), dim3(kBlock), 0, st, x,
                      a.x_stride, N, E, p.padded, sign_of(a.scale), rows.place, xp, xplane, dx, a.grad_x_stride);
 
+  auto join_sums = [&](int32_t count) {
+    if (N > 0 && N <= 256)
+      hipLaunchKernelGGL(xent_join<4>, dim3(unsigned(up(N, 4))), dim3(1024), 0, st, parts, int64_t(N), count,
+                         unit, rows, a.loss);
+    else if (N > 0)
+      hipLaunchKernelGGL(xent_join<64>, dim3(unsigned(up(N, 64))), dim3(1024), 0, st, parts, int64_t(N), count,
+                         unit, rows, a.loss);
+  };
+  auto join_dx = [&](int32_t count) {
+    const int64_t most = (int64_t(1) << 30) / (E / 4);
+    for (int64_t r0 = 0; r0 < N; r0 += most) {
+      const int64_t n = N - r0 < most ? N - r0 : most;
+      hipLaunchKernelGGL(xent_join_parts<TX>, dim3(unsigned(up(n * (E / 4), kBlock))), dim3(kBlock), 0, st, dxp,
+                         count, int64_t(N) * E, &head->live, r0 + n, fast_div(uint32_t(E / 4)), rows.row,
+                         &head->factor, dx, a.grad_x_stride, r0);
+    }
+  };
+  auto join_dw = [&](const float* from, int32_t count, int64_t part, int64_t n, TW* to) {
+    const int64_t most = (int64_t(1) << 30) / (E / 4);
+    for (int64_t r0 = 0; r0 < n; r0 += most) {
+      const int64_t q = n - r0 < most ? n - r0 : most;
+      hipLaunchKernelGGL(xent_join_parts<TW>, dim3(unsigned(up(q * (E / 4), kBlock))), dim3(kBlock), 0, st, from,
+                         count, part, nullptr, r0 + q, fast_div(uint32_t(E / 4)), nullptr, &head->factor_w, to,
+                         a.grad_table_stride, r0);
+    }
+  };
+  if (p.narrow) {
+    NarrowArgs q = {p.nar, p.terms, w, sizeof(TW) == 2, a.table_stride, xp, xplane, head, rows.tokens, rows.target,
+                    unit, parts, dxp, dw, sizeof(TW) == 2, a.grad_table_stride, &head->factor_w};
+    hipError_t e = launch_narrow_scores(q, st);
+    if (e != hipSuccess) return e;
+    join_sums(p.nar.splits * p.nar.parts);
+    if (dx != nullptr) {
+      e = launch_narrow_dx(q, st);
+      if (e != hipSuccess) return e;
+      join_dx(p.nar.splits * p.nar.parts);
+    }
+    if (dw != nullptr) {
+      if (p.nar.dw_splits > 1)
+        q.dw = ws + p.dwp, q.dw_bf16 = false, q.dw_stride = E, q.dw_factor = nullptr;
+      e = launch_narrow_dw(q, st);
+      if (e != hipSuccess) return e;
+      if (p.nar.dw_splits > 1)
+        join_dw(reinterpret_cast<float*>(ws + p.dwp), p.nar.dw_splits, V * E, V, dw);
+    }
+    return hipGetLastError();
+  }
   const int64_t xpitch = int64_t(p.padded) * 2;
   const Side xs = {xp, xpitch, xplane * 2};
   int64_t packed = -1;  // the piece that wp holds
@@ -630,13 +644,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     run_gemm<false, false, false>(
         g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n}, ss, st);
   }
-  const int32_t count = int32_t(up(V, ss.part()));
-  if (N > 0 && N <= 16)
-    hipLaunchKernelGGL(xent_join<4>, dim3(unsigned(up(N, 4))), dim3(1024), 0, st, parts, int64_t(N),
-                       count, unit, rows, a.loss);
-  else if (N > 0)
-    hipLaunchKernelGGL(xent_join<64>, dim3(unsigned(up(N, 64))), dim3(1024), 0, st, parts, int64_t(N),
-                       count, unit, rows, a.loss);
+  join_sums(int32_t(up(V, ss.part())));
   if (dx == nullptr && dw == nullptr) return hipGetLastError();
 
   const int64_t dplane = int64_t(N) * p.piece;
@@ -672,21 +680,11 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
         float* dwp = reinterpret_cast<float*>(ws + p.dwp);
         run_gemm<true, true, true>(gw, StoreEpi<float>{dwp, E, E, nullptr, nullptr, p.piece * E, false}, sw,
                                    st);
-        hipLaunchKernelGGL(xent_join_parts<TW>, dim3(unsigned(up(n * (E / 4), kBlock))), dim3(kBlock), 0, st,
-                           dwp, p.dw_splits, p.piece * E, nullptr, n, fast_div(uint32_t(E / 4)), nullptr,
-                           &head->factor_w, to, a.grad_table_stride, int64_t(0));
+        join_dw(dwp, p.dw_splits, p.piece * E, n, to);
       }
     }
   }
-  if (dx != nullptr) {
-    const int64_t most = (int64_t(1) << 30) / (E / 4);
-    for (int64_t r0 = 0; r0 < N; r0 += most) {
-      const int64_t n = N - r0 < most ? N - r0 : most;
-      hipLaunchKernelGGL(xent_join_parts<TX>, dim3(unsigned(up(n * (E / 4), kBlock))), dim3(kBlock), 0, st,
-                         dxp, p.dx_splits, dpart, &head->live, r0 + n, fast_div(uint32_t(E / 4)), rows.row,
-                         &head->factor, dx, a.grad_x_stride, r0);
-    }
-  }
+  if (dx != nullptr) join_dx(p.dx_splits);
   return hipGetLastError();
 }
 

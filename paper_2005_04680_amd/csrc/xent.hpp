@@ -1,0 +1,96 @@
+// What the kernels of the cross entropy share: exponents, BF16 terms, the rows that count.
+#pragma once
+
+#include "head.hpp"
+
+namespace embbag {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// x as the sum of three BF16 terms, each the nearest to what is left (the first by truncation where
+// rounding would pass the range).  A NaN is its own first term.  An infinity is its own last one: that term
+// meets the other side's first alone, so that the product is an infinity of the right sign.
+__device__ __forceinline__ void nearest_terms(float x, float (&t)[3]) {
+  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+  t[0] = float(__bf16(x));
+  if (u > 0x7F7F7FFFu && u < 0x7F800000u) t[0] = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+  if (u == 0x7F800000u) t[0] = 0.f;
+  const float rest = u > 0x7F800000u ? 0.f : x - t[0];
+  t[1] = u == 0x7F800000u ? 0.f : float(__bf16(rest));
+  t[2] = rest - t[1];
+}
+
+// Scores enter the exponentials as 2^(score * log2(e)), in one FMA: their sums are taken with x times the
+// scale's sign, of which `unit` = |scale| log2(e) makes the exponent.  (A scale of 0 makes x 0, and its
+// unit is any.)
+__host__ __device__ __forceinline__ float sign_of(float scale) {
+  return scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
+}
+__host__ __device__ __forceinline__ float unit_of(float scale) {
+  return scale == 0.f ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
+}
+
+// What the backward needs of a row that counts.
+struct Token {
+  float top;    // about its largest score's exponent
+  float inv;    // 1 / the sum of 2^(exponent - top)
+  float ratio;  // its weight over the largest
+  int label;
+};
+
+// In the workspace.
+struct Head {
+  int32_t live;   // rows that count
+  float largest;  // of their weights' magnitudes
+  float factor;   // scale * largest, of dx
+  float factor_w; // |scale| * largest, of dW (x has the scale's sign)
+};
+
+struct Rows {
+  Head* head;
+  int32_t* place;  // [rows]: among the rows that count, or -1
+  int32_t* row;    // [live]: the row at a place
+  Token* tokens;   // [live]
+  float* target;   // [live]: the label's sum
+};
+
+}  // namespace
+
+// The products of narrow tables (dim <= kNarrow), whose D stays in registers.  Sizes as xent.hip's plan has
+// them.
+constexpr int kNarrow = 128;
+struct Narrow {
+  int32_t rows, dim;
+  int64_t vocab;
+  int bm;               // rows of x per block: 64, 128 or 256
+  int32_t splits, per;  // ranges of the vocabulary: blocks of it, and rows of W in each
+  int parts;            // parts per range (wavefronts that share a block's rows of x)
+  int32_t dw_splits, dw_per;  // ranges of the rows that count, rows in each
+};
+Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32);
+struct NarrowArgs {
+  Narrow n;
+  int terms;  // of D; of the sides 3 if that is 3, else 1
+  const void* table;
+  bool table_bf16;
+  int64_t table_stride;
+  const void* x;       // planes [rows][padded]
+  int64_t x_plane;     // elements
+  const void* head;    // Head, Token[rows], the labels' sums
+  const void* tokens;
+  float* target;
+  float unit;
+  void* sums;          // float2 [splits * parts][rows]: exponents and sums
+  float* dx_parts;     // [splits * parts][rows][dim]
+  void* dw;            // table's type, or FP32 parts [dw_splits][vocab][dim]
+  bool dw_bf16;
+  int64_t dw_stride;
+  const float* dw_factor;  // null for parts
+};
+hipError_t launch_narrow_scores(const NarrowArgs& a, hipStream_t st);
+hipError_t launch_narrow_dx(const NarrowArgs& a, hipStream_t st);
+hipError_t launch_narrow_dw(const NarrowArgs& a, hipStream_t st);
+
+}  // namespace embbag

@@ -134,7 +134,10 @@ def test_weights_and_scale(N, V, E, t, scale):
 @pytest.mark.parametrize("N,V,E,t", [(300, 25601, 1500, "bf16"), (300, 25001, 1500, "f32"), (600, 20000, 516, "bf16"),
                                      (20000, 14001, 8, "bf16"), (7000, 14000, 36, "f32"), (3, 600001, 8, "bf16"),
                                      (2, 530000, 4, "f32"), (40, 60001, 2052, "f32"), (5000, 300, 260, "bf16"),
-                                     (3000, 1, 64, "f32"), (4500, 257, 100, "f32")])
+                                     (3000, 1, 64, "f32"), (4500, 257, 100, "f32"), (20000, 14001, 132, "bf16"),
+                                     (7000, 14000, 132, "f32"), (3, 600001, 136, "bf16"), (2, 530000, 132, "f32"),
+                                     (3000, 1, 132, "f32"), (4500, 257, 164, "f32"), (9000, 1000, 128, "bf16"),
+                                     (2000, 30001, 128, "f32"), (100, 70001, 64, "bf16")])
 def test_large(N, V, E, t):
     check(N, V, E, N, t, t, sure=4.0)
 
