@@ -24,78 +24,8 @@ namespace embbag {
 namespace {
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of D, of W's terms: a piece's
+constexpr int kRowsAtOnce = 4096;                     // rows whose places 1024 threads find in a round
 constexpr int64_t kMaxPitch = int64_t(1) << 19;       // elements of a row of D
-
-// Which rows count, their places in order, and the largest weight.  One block; the losses of the others
-// are 0.
-__global__ __launch_bounds__(1024) void xent_rows(const int32_t* __restrict__ labels,
-                                                  const float* __restrict__ weights, int32_t rows,
-                                                  int32_t vocab, float scale, Rows out,
-                                                  float* __restrict__ loss, int32_t* __restrict__ status) {
-  __shared__ int counts[16];
-  __shared__ float tops[16];
-  const int lane = lane_id(), wave = wave_id();
-  int base = 0;
-  float top = 0.f;
-  bool bad = false;
-  for (int r0 = 0; r0 < rows; r0 += 4096) {
-    int label[4], n = 0;
-    float w[4];
-    bool in[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + threadIdx.x * 4 + i;
-      label[i] = r < rows ? labels[r] : -1;
-      w[i] = r < rows && weights != nullptr ? weights[r] : 1.f;
-      bad = bad || label[i] >= vocab;
-      in[i] = label[i] >= 0 && label[i] < vocab && w[i] != 0.f;
-      n += in[i];
-      if (in[i]) top = fmaxf(top, fabsf(w[i]));
-    }
-    int before = n;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int v = __shfl_up(before, d, kWave);
-      if (lane >= d) before += v;
-    }
-    __syncthreads();  // (the counts of the round before have been read)
-    if (lane == kWave - 1) counts[wave] = before;
-    __syncthreads();
-    int at = base + before - n, all = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (i < wave) at += counts[i];
-      all += counts[i];
-    }
-    base += all;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + threadIdx.x * 4 + i;
-      if (r >= rows) continue;
-      out.place[r] = in[i] ? at : -1;
-      if (in[i]) {
-        out.row[at] = r;
-        Token t = {0.f, 0.f, w[i], label[i]};
-        out.tokens[at] = t;
-        ++at;
-      } else {
-        loss[r] = 0.f;
-      }
-    }
-  }
-  if (bad && status != nullptr) atomicMin(status, EMBBAG_ERR_INDEX_RANGE);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
-  if (lane == 0) tops[wave] = top;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, tops[i]);
-    out.head->live = base;
-    out.head->largest = top;
-    out.head->factor = scale * top;
-    out.head->factor_w = fabsf(scale) * top;
-  }
-}
 
 // 8 elements of a row from e on (zeros past dim; dim % 4 == 0) times the sign as BF16 terms to `dst`.
 template <int TERMS, class T>
@@ -120,16 +50,101 @@ __device__ __forceinline__ void pack8(const T* row, int e, int dim, float sign, 
   }
 }
 
-// x's rows that count, times the sign, as TERMS planes [live][padded]; dx's others as zeros.  A wavefront per row.
+// Which rows count, their places in order, and the largest weight, by the threads of one block of 1024.
+// `writes`: whether the block stores them; `place` is stored for rows from `low` to `high` alone
+// and may be in LDS (its entry 0 is row `low`).  The losses of the rows that do not count are 0.
+struct RowSums {
+  int counts[16];
+  float tops[16];
+};
+__device__ __forceinline__ void find_rows(const int32_t* __restrict__ labels, const float* __restrict__ weights,
+                                          int32_t rows, int32_t vocab, float scale, const Rows& out,
+                                          int32_t* place, int32_t low_row, int32_t high_row, bool writes,
+                                          float* __restrict__ loss, int32_t* __restrict__ status,
+                                          RowSums& shared) {
+  const int lane = lane_id(), wave = wave_id();
+  int base = 0;
+  float top = 0.f;
+  bool bad = false;
+  for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
+    int label[4], n = 0;
+    float w[4];
+    bool in[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + threadIdx.x * 4 + i;
+      label[i] = r < rows ? labels[r] : -1;
+      w[i] = r < rows && weights != nullptr ? weights[r] : 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bad = bad || label[i] >= vocab;
+      in[i] = label[i] >= 0 && label[i] < vocab && w[i] != 0.f;
+      n += in[i];
+      if (in[i]) top = fmaxf(top, fabsf(w[i]));
+    }
+    int before = n;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int v = __shfl_up(before, d, kWave);
+      if (lane >= d) before += v;
+    }
+    __syncthreads();  // (the counts of the round before have been read)
+    if (lane == kWave - 1) shared.counts[wave] = before;
+    __syncthreads();
+    int at = base + before - n, all = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i < wave) at += shared.counts[i];
+      all += shared.counts[i];
+    }
+    base += all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + threadIdx.x * 4 + i;
+      if (r >= rows) continue;
+      if (r >= low_row && r < high_row) place[r - low_row] = in[i] ? at : -1;
+      if (in[i]) {
+        if (writes) {
+          out.row[at] = r;
+          Token t = {0.f, 0.f, w[i], label[i]};
+          out.tokens[at] = t;
+        }
+        ++at;
+      } else if (writes) {
+        loss[r] = 0.f;
+      }
+    }
+  }
+  if (!writes) return;
+  if (bad && status != nullptr) atomicMin(status, EMBBAG_ERR_INDEX_RANGE);
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
+  if (lane == 0) shared.tops[wave] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, shared.tops[i]);
+    out.head->live = base;
+    out.head->largest = top;
+    out.head->factor = scale * top;
+    out.head->factor_w = fabsf(scale) * top;
+  }
+}
+
+__global__ __launch_bounds__(1024) void xent_rows(const int32_t* __restrict__ labels,
+                                                  const float* __restrict__ weights, int32_t rows,
+                                                  int32_t vocab, float scale, Rows out,
+                                                  float* __restrict__ loss, int32_t* __restrict__ status) {
+  __shared__ RowSums shared;
+  find_rows(labels, weights, rows, vocab, scale, out, out.place, 0, rows, true, loss, status, shared);
+}
+
+// Row r of x, times the sign, as TERMS planes at its place among the rows that count; dx's row as zeros if
+// it does not.  By a wavefront.
 template <int TERMS, class T>
-__global__ __launch_bounds__(kBlock) void xent_pack_x(const T* __restrict__ x, int64_t stride,
-                                                      int32_t rows, int32_t dim, int32_t padded, float sign,
-                                                      const int32_t* __restrict__ place,
-                                                      __bf16* __restrict__ out, int64_t plane,
-                                                      T* __restrict__ dx, int64_t dx_stride) {
-  const int r = blockIdx.x * kWavesPerBlock + wave_id();
-  if (r >= rows) return;
-  const int at = __builtin_amdgcn_readfirstlane(place[r]);
+__device__ __forceinline__ void pack_row(const T* __restrict__ x, int64_t stride, int r, int at, int32_t dim,
+                                         int32_t padded, float sign, __bf16* __restrict__ out, int64_t plane,
+                                         T* __restrict__ dx, int64_t dx_stride) {
   if (at < 0) {
     if (dx == nullptr) return;
     for (int e = lane_id() * 4; e < dim; e += kWave * 4)
@@ -138,6 +153,36 @@ __global__ __launch_bounds__(kBlock) void xent_pack_x(const T* __restrict__ x, i
   }
   for (int e = lane_id() * 8; e < padded; e += kWave * 8)
     pack8<TERMS>(x + r * stride, e, dim, sign, out + int64_t(at) * padded + e, plane);
+}
+
+template <int TERMS, class T>
+__global__ __launch_bounds__(kBlock) void xent_pack_x(const T* __restrict__ x, int64_t stride,
+                                                      int32_t rows, int32_t dim, int32_t padded, float sign,
+                                                      const int32_t* __restrict__ place,
+                                                      __bf16* __restrict__ out, int64_t plane,
+                                                      T* __restrict__ dx, int64_t dx_stride) {
+  const int r = blockIdx.x * kWavesPerBlock + wave_id();
+  if (r >= rows) return;
+  pack_row<TERMS>(x, stride, r, scalar(place[r]), dim, padded, sign, out, plane, dx, dx_stride);
+}
+
+// Both for up to kRowsAtOnce rows: every block finds the places for itself and packs 16 rows (a launch
+// less: 33 x 32001 x 128 4 us).
+template <int TERMS, class T>
+__global__ __launch_bounds__(1024) void xent_rows_pack(const int32_t* __restrict__ labels,
+                                                       const float* __restrict__ weights, int32_t rows,
+                                                       int32_t vocab, float scale, Rows found,
+                                                       float* __restrict__ loss, int32_t* __restrict__ status,
+                                                       const T* __restrict__ x, int64_t stride, int32_t dim,
+                                                       int32_t padded, float sign, __bf16* __restrict__ out,
+                                                       int64_t plane, T* __restrict__ dx, int64_t dx_stride) {
+  __shared__ RowSums shared;
+  __shared__ int32_t place[16];
+  const int r0 = blockIdx.x * 16, r = r0 + wave_id();
+  find_rows(labels, weights, rows, vocab, scale, found, place, r0, r0 + 16, blockIdx.x == 0, loss, status, shared);
+  __syncthreads();
+  if (r >= rows) return;
+  pack_row<TERMS>(x, stride, r, scalar(place[wave_id()]), dim, padded, sign, out, plane, dx, dx_stride);
 }
 
 // Rows of W as TERMS planes [rows][padded].
@@ -343,7 +388,7 @@ struct GradEpi {
 #pragma unroll
               for (int r = 0; r < 16; ++r) {
                 const float x = acc[h + i][j][r], rest = x - float(__bf16(x));
-                acc[h + i][j][r] = x - x == 0.f ? rest : 0.f;  // (an infinity or a NaN leaves nothing)
+                acc[h + i][j][r] = rest;
               }
           }
         }
@@ -407,8 +452,9 @@ struct StoreEpi {
   }
 };
 
-// The parts [splits][rows of m][dim] added in order, times the factor, into the rows that `map` names.
-template <class T>
+// The parts [splits][rows of m][dim] added up, times the factor, into the rows that `map` names: SLICES
+// threads for 4 elements add every SLICES-th part each, then their sums are added in order.
+template <int SLICES, class T>
 __global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restrict__ parts, int32_t splits,
                                                           int64_t part, const int32_t* __restrict__ live,
                                                           int64_t rows, FastDiv d4,
@@ -416,18 +462,51 @@ __global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restric
                                                           const float* __restrict__ factor,
                                                           T* __restrict__ out, int64_t pitch,
                                                           int64_t row0) {
-  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+  constexpr int EACH = kBlock / SLICES;
+  __shared__ f4 sums[SLICES > 1 ? SLICES : 1][EACH];
+  const int t = threadIdx.x % EACH, slice = threadIdx.x / EACH;
+  const int64_t i = int64_t(blockIdx.x) * EACH + t;
   const uint32_t q = quotient(uint32_t(i), d4);
   const int64_t at = row0 + q;
   const int c = int(uint32_t(i) - q * d4.div) * 4;
   const int64_t end = live != nullptr ? int64_t(*live) : rows;
-  if (i >= (rows - row0) * int64_t(d4.div) || at >= end) return;
-  const float* p = parts + at * (int64_t(d4.div) * 4) + c;
-  f4 s = load4(p);
-#pragma unroll 4
-  for (int z = 1; z < splits; ++z) s += load4(p + z * part);
+  const bool in = i < (rows - row0) * int64_t(d4.div) && at < end;
+  f4 s = {0.f, 0.f, 0.f, 0.f};
+  if (in) {
+    const float* p = parts + at * (int64_t(d4.div) * 4) + c;
+#pragma unroll 8
+    for (int z = slice; z < splits; z += SLICES) s += load4(p + z * part);
+  }
+  if constexpr (SLICES > 1) {
+    sums[slice][t] = s;
+    __syncthreads();
+    if (slice != 0) return;
+#pragma unroll
+    for (int k = 1; k < SLICES; ++k) s += sums[k][t];
+  }
+  if (!in) return;
   const float f = *factor;
   store4(out + (map != nullptr ? int64_t(map[at]) : at) * pitch + c, s * f);
+}
+// Slices where the parts are many: their loads are a chain otherwise (33 rows of 128 from 250 parts: 18 us
+// with one).
+template <class T>
+void launch_join_parts(const float* parts, int32_t splits, int64_t part, const int32_t* live, int64_t rows,
+                       int32_t dim, const int32_t* map, const float* factor, T* out, int64_t pitch,
+                       int64_t row0, hipStream_t st) {
+  const int64_t n = (rows - row0) * (dim / 4);
+  const FastDiv d = fast_div(uint32_t(dim / 4));
+  auto run = [&](auto slices) {
+    constexpr int S = decltype(slices)::value;
+    hipLaunchKernelGGL((xent_join_parts<S, T>), dim3(unsigned((n + kBlock / S - 1) / (kBlock / S))),
+                       dim3(kBlock), 0, st, parts, splits, part, live, rows, d, map, factor, out, pitch, row0);
+  };
+  if (splits > 32)
+    run(std::integral_constant<int, 32>());
+  else if (splits > 4)
+    run(std::integral_constant<int, 4>());
+  else
+    run(std::integral_constant<int, 1>());
 }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -569,11 +648,18 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   const float unit = unit_of(a.scale);
   const int64_t xplane = int64_t(N) * p.padded, wplane = p.piece * p.padded;
 
-  hipLaunchKernelGGL(xent_rows, dim3(1), dim3(1024), 0, st, a.labels, a.row_weights, N, int32_t(V), a.scale,
-                     rows, a.loss, status);
-  if (N > 0)
-    hipLaunchKernelGGL((xent_pack_x<TERMS, TX>), dim3(unsigned(up(N, kWavesPerBlock))), dim3(kBlock), 0, st, x,
-                     a.x_stride, N, E, p.padded, sign_of(a.scale), rows.place, xp, xplane, dx, a.grad_x_stride);
+  if (N > 0 && N <= kRowsAtOnce) {
+    hipLaunchKernelGGL((xent_rows_pack<TERMS, TX>), dim3(unsigned(up(N, 16))), dim3(1024), 0, st, a.labels,
+                       a.row_weights, N, int32_t(V), a.scale, rows, a.loss, status, x, a.x_stride, E, p.padded,
+                       sign_of(a.scale), xp, xplane, dx, a.grad_x_stride);
+  } else {
+    hipLaunchKernelGGL(xent_rows, dim3(1), dim3(1024), 0, st, a.labels, a.row_weights, N, int32_t(V), a.scale,
+                       rows, a.loss, status);
+    if (N > 0)
+      hipLaunchKernelGGL((xent_pack_x<TERMS, TX>), dim3(unsigned(up(N, kWavesPerBlock))), dim3(kBlock), 0, st,
+                         x, a.x_stride, N, E, p.padded, sign_of(a.scale), rows.place, xp, xplane, dx,
+                         a.grad_x_stride);
+  }
 
   auto join_sums = [&](int32_t count) {
     if (N > 0 && N <= 256)
@@ -584,21 +670,19 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
                          unit, rows, a.loss);
   };
   auto join_dx = [&](int32_t count) {
-    const int64_t most = (int64_t(1) << 30) / (E / 4);
+    const int64_t most = (int64_t(1) << 25) / (E / 4);  // 32 threads for each
     for (int64_t r0 = 0; r0 < N; r0 += most) {
       const int64_t n = N - r0 < most ? N - r0 : most;
-      hipLaunchKernelGGL(xent_join_parts<TX>, dim3(unsigned(up(n * (E / 4), kBlock))), dim3(kBlock), 0, st, dxp,
-                         count, int64_t(N) * E, &head->live, r0 + n, fast_div(uint32_t(E / 4)), rows.row,
-                         &head->factor, dx, a.grad_x_stride, r0);
+      launch_join_parts<TX>(dxp, count, int64_t(N) * E, &head->live, r0 + n, E, rows.row, &head->factor, dx,
+                            a.grad_x_stride, r0, st);
     }
   };
   auto join_dw = [&](const float* from, int32_t count, int64_t part, int64_t n, TW* to) {
-    const int64_t most = (int64_t(1) << 30) / (E / 4);
+    const int64_t most = (int64_t(1) << 25) / (E / 4);  // 32 threads for each
     for (int64_t r0 = 0; r0 < n; r0 += most) {
       const int64_t q = n - r0 < most ? n - r0 : most;
-      hipLaunchKernelGGL(xent_join_parts<TW>, dim3(unsigned(up(q * (E / 4), kBlock))), dim3(kBlock), 0, st, from,
-                         count, part, nullptr, r0 + q, fast_div(uint32_t(E / 4)), nullptr, &head->factor_w, to,
-                         a.grad_table_stride, r0);
+      launch_join_parts<TW>(from, count, part, nullptr, r0 + q, E, nullptr, &head->factor_w, to,
+                            a.grad_table_stride, r0, st);
     }
   };
   if (p.narrow) {

@@ -113,10 +113,7 @@ __device__ __forceinline__ void d_terms(const f16v& d, int t, u4 (&out)[PD]) {
     out[k] = pack16(v);
     if (k + 1 == PD) break;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = v[i], rest = x - float(__bf16(x));
-      v[i] = x - x == 0.f ? rest : 0.f;  // (an infinity or a NaN leaves nothing)
-    }
+    for (int i = 0; i < 8; ++i) v[i] -= (i % 2 ? bf16_hi : bf16_lo)(out[k][i / 2]);
   }
 }
 
@@ -237,10 +234,12 @@ __global__ __launch_bounds__(kBlock, P == 1 && EP == 128 ? 1 : 2) void narrow_to
         if constexpr (GRAD) {
           const float c = inv[i] * ratio[i];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float e = exp2_of(__builtin_fmaf(z2[i][r], a.unit, -top[i]));
-            z2[i][r] = e * c;
-            if (some && mine && int(place) == r / 4 * 8 + r % 4) z2[i][r] = (e * inv[i] - 1.f) * ratio[i];
+          for (int r = 0; r < 16; ++r)
+            z2[i][r] = exp2_of(__builtin_fmaf(z2[i][r], a.unit, -top[i])) * c;
+          if (some) {
+            const float less = mine ? ratio[i] : 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z2[i][r] -= int(place) == r / 4 * 8 + r % 4 ? less : 0.f;
           }
           if (!whole) {
 #pragma unroll
@@ -575,10 +574,10 @@ Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32) {
   const int wm = n.bm / (f32 ? 32 : 64), wv = 4 / wm;
   const int vb = 32 * wv * (wv == 1 && !f32 ? 2 : 1);
   n.parts = wv;
-  // Two blocks per compute unit, of at least 4 tiles of the table.
+  // Two blocks per compute unit, of at least 2 tiles of the table.
   const int64_t blocks = up(rows > 0 ? rows : 1, n.bm), tiles = up(vocab, vb);
   int64_t splits = 2 * kNumCu / blocks;
-  if (splits > tiles / 4) splits = tiles / 4;
+  if (splits > tiles / 2) splits = tiles / 2;
   if (splits < 1) splits = 1;
   while (up(tiles, splits) > (int64_t(1) << 24)) ++splits;  // (ranges fit 31 bits)
   n.per = int32_t(up(tiles, splits) * vb);
