@@ -64,7 +64,7 @@ constexpr int kNarrow = 128;
 struct Narrow {
   int32_t rows, dim;
   int64_t vocab;
-  int bm;               // rows of x per block: 64, 128 or 256
+  int bm;               // rows of x per block
   int32_t splits, per;  // ranges of the vocabulary: blocks of it, and rows of W in each
   int parts;            // parts per range (wavefronts that share a block's rows of x)
   int32_t dw_splits, dw_per;  // ranges of the rows that count, rows in each

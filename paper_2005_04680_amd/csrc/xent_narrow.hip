@@ -52,33 +52,52 @@ __device__ __forceinline__ f16v mfma(const u4& a, const u4& b, const f16v& c) {
                                                  0, 0);
 }
 
-// 8 elements of a row on their way (zeros past `n` of them, n % 4 == 0).
+// 8 elements of a row on their way (zeros past `n` of them, n % 4 == 0), untouched until terms() wants them.
 template <class T>
-struct Eight {
+struct Eight;
+template <>
+struct Eight<float> {
   f4 a, b;
-  __device__ __forceinline__ void load(const T* p, int n) {
+  __device__ __forceinline__ void load(const float* p, int n) {
     a = n > 0 ? load4(p) : f4{0.f, 0.f, 0.f, 0.f};
     b = n > 4 ? load4(p + 4) : f4{0.f, 0.f, 0.f, 0.f};
   }
-  // As P planes of BF16 terms.
-  template <int P>
-  __device__ __forceinline__ void terms(u4 (&t)[P]) const {
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    if constexpr (P == 1) {
-      t[0] = pack16(v);
-    } else {
-      float s[3][8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float q[3];
-        nearest_terms(v[i], q);
-        s[0][i] = q[0], s[1][i] = q[1], s[2][i] = q[2];
-      }
-#pragma unroll
-      for (int k = 0; k < 3; ++k) t[k] = pack16(s[k]);
-    }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
   }
 };
+template <>
+struct Eight<__bf16> {
+  u4 w;
+  __device__ __forceinline__ void load(const __bf16* p, int n) {
+    w = u4{0u, 0u, 0u, 0u};
+    if (n > 4) {
+      w = load16(p);
+    } else if (n > 0) {
+      const u2 h = *reinterpret_cast<const u2*>(p);
+      w.x = h.x, w.y = h.y;
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const { unpack16(w, v); }
+};
+// As P planes of BF16 terms.
+template <int P, class T>
+__device__ __forceinline__ void terms_of(const Eight<T>& x, u4 (&t)[P]) {
+  if constexpr (P == 1) {
+    t[0] = x.w;
+  } else {
+    float v[8], s[3][8];
+    x.values(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float q[3];
+      nearest_terms(v[i], q);
+      s[0][i] = q[0], s[1][i] = q[1], s[2][i] = q[2];
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) t[k] = pack16(s[k]);
+  }
+}
 
 // Fragments of a tile in LDS: rows of EP elements, plane after plane.
 template <int EP>
@@ -134,11 +153,21 @@ struct TokenArgs {
   int32_t splits, per;
 };
 
+// Groups of 32 standing rows per wavefront: two meet every fragment of the streaming tile where their
+// registers leave room for a second wavefront on the SIMD, whose products run while the first one makes D.
+template <int EP, int P>
+constexpr int kStanding = P == 1 && EP == 64 ? 2 : 1;
+constexpr int standing(int dim, bool f32) { return !f32 && dim <= 64 ? 2 : 1; }
+// Groups of 32 rows that a wavefront takes from a streaming tile of the table, and of x.
+template <int P, int WV>
+constexpr int kGroups = WV == 1 && P == 1 ? 2 : 1;
+constexpr int groups(int wv, bool f32) { return wv == 1 && !f32 ? 2 : 1; }
+
 // WM wavefronts side by side over rows of x (32 TM each), the others over the rows of the table's tile,
 // SUB groups of 32 of them each.  GRAD: dx, else the sums.
 template <int EP, int P, int PD, int WM, bool GRAD, class TW>
-__global__ __launch_bounds__(kBlock, P == 1 && EP == 128 ? 1 : 2) void narrow_tokens(TokenArgs a) {
-  constexpr int TM = P == 1 ? 2 : 1, WV = 4 / WM, SUB = WV == 1 && P == 1 ? 2 : 1;
+__global__ __launch_bounds__(kBlock, 2) void narrow_tokens(TokenArgs a) {
+  constexpr int TM = kStanding<EP, P>, WV = 4 / WM, SUB = kGroups<P, WV>;
   constexpr int BM = 32 * TM * WM, VB = 32 * WV * SUB, S = EP / 16;
   constexpr int TILE = VB * EP * 2, STAGE = TILE * P;
   constexpr int CHUNKS = VB * EP / 8 / kBlock;
@@ -184,7 +213,7 @@ __global__ __launch_bounds__(kBlock, P == 1 && EP == 128 ? 1 : 2) void narrow_to
     for (int i = 0; i < CHUNKS; ++i) {
       const int c = i * kBlock + threadIdx.x, r = c / (EP / 8), k = c % (EP / 8);
       u4 t[P];
-      next[i].template terms<P>(t);
+      terms_of<P>(next[i], t);
 #pragma unroll
       for (int p = 0; p < P; ++p)
         *reinterpret_cast<u4*>(st + p * TILE + r * (EP * 2) + chunk_at<EP>(r, k) * 16) = t[p];
@@ -237,24 +266,28 @@ __global__ __launch_bounds__(kBlock, P == 1 && EP == 128 ? 1 : 2) void narrow_to
           for (int r = 0; r < 16; ++r)
             z2[i][r] = exp2_of(__builtin_fmaf(z2[i][r], a.unit, -top[i])) * c;
           if (some) {
+            asm volatile("");  // (a branch: few tiles hold a label)
             const float less = mine ? ratio[i] : 0.f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) z2[i][r] -= int(place) == r / 4 * 8 + r % 4 ? less : 0.f;
           }
           if (!whole) {
+            asm volatile("");
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if (first + r / 4 * 8 + r % 4 >= v1) z2[i][r] = 0.f;
           }
         } else {
-          if (some && mine) {
+          if (some) {
+            asm volatile("");
             float t = 0.f;
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if (int(place) == r / 4 * 8 + r % 4) t = z2[i][r];
-            if (at[i] < live) a.target[at[i]] = t;
+            if (mine && at[i] < live) a.target[at[i]] = t;
           }
           if (!whole) {
+            asm volatile("");
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if (first + r / 4 * 8 + r % 4 >= v1) z2[i][r] = low();
@@ -339,8 +372,8 @@ struct VocabArgs {
 
 // A wavefront's 32 TV rows of the table stand, rows that count stream.
 template <int EP, int P, int PD, class TW, class TO>
-__global__ __launch_bounds__(kBlock, P == 1 && EP == 128 ? 1 : 2) void narrow_vocab(VocabArgs a) {
-  constexpr int TV = P == 1 ? 2 : 1, SUB = P == 1 ? 2 : 1, MB = 32 * SUB, S = EP / 16;
+__global__ __launch_bounds__(kBlock, 2) void narrow_vocab(VocabArgs a) {
+  constexpr int TV = kStanding<EP, P>, SUB = kGroups<P, 1>, MB = 32 * SUB, S = EP / 16;
   constexpr int BV = 32 * TV * 4;
   constexpr int TILE = MB * EP * 2, STAGE = TILE * P;
   constexpr int ALL = MB * EP / 8 * P, CHUNKS = (ALL + kBlock - 1) / kBlock;
@@ -366,7 +399,7 @@ __global__ __launch_bounds__(kBlock, P == 1 && EP == 128 ? 1 : 2) void narrow_vo
       Eight<TW> q;
       q.load(p + e, a.dim - e);
       u4 t[P];
-      q.template terms<P>(t);
+      terms_of<P>(q, t);
 #pragma unroll
       for (int k = 0; k < P; ++k) w[i][k][s] = t[k];
     }
@@ -500,7 +533,7 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 template <int EP, int P, int PD, int WM, bool GRAD, class TW>
 void launch_tokens(const NarrowArgs& n, hipStream_t st) {
-  constexpr int WV = 4 / WM, SUB = WV == 1 && P == 1 ? 2 : 1, VB = 32 * WV * SUB;
+  constexpr int WV = 4 / WM, VB = 32 * WV * kGroups<P, WV>;
   constexpr int lds = 2 * VB * EP * 2 * P;
   static_assert(lds <= 160 * 1024, "LDS");
   auto kernel = narrow_tokens<EP, P, PD, WM, GRAD, TW>;
@@ -515,7 +548,7 @@ void launch_tokens(const NarrowArgs& n, hipStream_t st) {
 
 template <int EP, int P, int PD, bool GRAD, class TW>
 void launch_tokens_shape(const NarrowArgs& n, hipStream_t st) {
-  constexpr int TM = P == 1 ? 2 : 1;
+  constexpr int TM = kStanding<EP, P>;
   if constexpr (P == 1) {
     if (n.n.bm == 32 * TM) return launch_tokens<EP, P, PD, 1, GRAD, TW>(n, st);
   }
@@ -527,7 +560,7 @@ void launch_tokens_shape(const NarrowArgs& n, hipStream_t st) {
 
 template <int EP, int P, int PD, class TW, class TO>
 void launch_vocab(const NarrowArgs& n, hipStream_t st) {
-  constexpr int TV = P == 1 ? 2 : 1, BV = 32 * TV * 4, MB = P == 1 ? 64 : 32;
+  constexpr int BV = 32 * kStanding<EP, P> * 4, MB = 32 * kGroups<P, 1>;
   constexpr int lds = 2 * MB * EP * 2 * P;
   static_assert(lds <= 65536, "LDS");
   const NarrowArgs& q = n;
@@ -570,9 +603,11 @@ Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32) {
   Narrow n = {};
   n.rows = rows, n.dim = dim, n.vocab = vocab;
   // Few rows: wavefronts share them and take different rows of the table.
-  n.bm = f32 ? (rows <= 64 ? 64 : 128) : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-  const int wm = n.bm / (f32 ? 32 : 64), wv = 4 / wm;
-  const int vb = 32 * wv * (wv == 1 && !f32 ? 2 : 1);
+  const int each = 32 * standing(dim, f32);
+  int wm = f32 ? 2 : 1;
+  while (wm < 4 && wm * each < rows) wm *= 2;
+  n.bm = wm * each;
+  const int wv = 4 / wm, vb = 32 * wv * groups(wv, f32);
   n.parts = wv;
   // Two blocks per compute unit, of at least 2 tiles of the table.
   const int64_t blocks = up(rows > 0 ? rows : 1, n.bm), tiles = up(vocab, vb);
@@ -582,7 +617,7 @@ Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32) {
   while (up(tiles, splits) > (int64_t(1) << 24)) ++splits;  // (ranges fit 31 bits)
   n.per = int32_t(up(tiles, splits) * vb);
   n.splits = int32_t(up(vocab, n.per));
-  const int mb = f32 ? 32 : 64, bv = f32 ? 128 : 256;
+  const int mb = 32 * groups(1, f32), bv = 4 * each;
   const int64_t vblocks = up(vocab, bv), steps = up(rows > 0 ? rows : 1, mb);
   int64_t ds = 2 * kNumCu / vblocks;
   if (ds > steps / 4) ds = steps / 4;
@@ -611,10 +646,11 @@ hipError_t launch_narrow_dx(const NarrowArgs& a, hipStream_t st) {
 
 hipError_t launch_narrow_dw(const NarrowArgs& a, hipStream_t st) {
   for_kind(a, [&](auto EP, auto P, auto PD, auto w) {
-    if (a.dw_bf16)
-      launch_vocab<EP.value, P.value, PD.value, decltype(w), __bf16>(a, st);
-    else
-      launch_vocab<EP.value, P.value, PD.value, decltype(w), float>(a, st);
+    using TW = decltype(w);
+    if constexpr (sizeof(TW) == 2) {
+      if (a.dw_bf16) return launch_vocab<EP.value, P.value, PD.value, TW, __bf16>(a, st);
+    }
+    launch_vocab<EP.value, P.value, PD.value, TW, float>(a, st);
   });
   return hipGetLastError();
 }
