@@ -38,15 +38,10 @@ __device__ __forceinline__ void pack8(const T* row, int e, int dim, float sign, 
   if constexpr (TERMS == 1) {
     store16(dst, pack16(v));
   } else {
-    float t[3][8];
+    u4 t[3];
+    nearest_terms(v, t);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float s[3];
-      nearest_terms(v[i], s);
-      t[0][i] = s[0], t[1][i] = s[1], t[2][i] = s[2];
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) store16(dst + k * plane, pack16(t[k]));
+    for (int k = 0; k < 3; ++k) store16(dst + k * plane, t[k]);
   }
 }
 

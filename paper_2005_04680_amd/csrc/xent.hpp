@@ -9,17 +9,25 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// x as the sum of three BF16 terms, each the nearest to what is left (the first by truncation where
-// rounding would pass the range).  A NaN is its own first term.  An infinity is its own last one: that term
-// meets the other side's first alone, so that the product is an infinity of the right sign.
-__device__ __forceinline__ void nearest_terms(float x, float (&t)[3]) {
-  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
-  t[0] = float(__bf16(x));
-  if (u > 0x7F7F7FFFu && u < 0x7F800000u) t[0] = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-  if (u == 0x7F800000u) t[0] = 0.f;
-  const float rest = u > 0x7F800000u ? 0.f : x - t[0];
-  t[1] = u == 0x7F800000u ? 0.f : float(__bf16(rest));
-  t[2] = rest - t[1];
+// Numbers as sums of three BF16 terms, each the nearest to what is left.  What BF16 cannot hold, beyond its
+// largest number (infinities and NaN too), comes in the last term, which meets the other side's first alone.
+__device__ __forceinline__ void nearest_terms(const float (&x)[8], u4 (&t)[3]) {
+  constexpr float kLargest = 3.3895313892515355e38f;
+  float v[8], over[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = __builtin_amdgcn_fmed3f(x[i], -kLargest, kLargest);
+    over[i] = x[i] - v[i];
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    t[k] = pack16(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] -= (i % 2 ? bf16_hi : bf16_lo)(t[k][i / 2]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] += over[i];
+  t[2] = pack16(v);
 }
 
 // Scores enter the exponentials as 2^(score * log2(e)), in one FMA: their sums are taken with x times the

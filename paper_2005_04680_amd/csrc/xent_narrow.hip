@@ -86,16 +86,9 @@ __device__ __forceinline__ void terms_of(const Eight<T>& x, u4 (&t)[P]) {
   if constexpr (P == 1) {
     t[0] = x.w;
   } else {
-    float v[8], s[3][8];
+    float v[8];
     x.values(v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float q[3];
-      nearest_terms(v[i], q);
-      s[0][i] = q[0], s[1][i] = q[1], s[2][i] = q[2];
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) t[k] = pack16(s[k]);
+    nearest_terms(v, t);
   }
 }
 
