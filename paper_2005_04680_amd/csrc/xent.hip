@@ -686,19 +686,14 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     hipError_t e = launch_narrow_scores(q, st);
     if (e != hipSuccess) return e;
     join_sums(p.nar.splits * p.nar.parts);
-    if (dx != nullptr) {
-      e = launch_narrow_dx(q, st);
-      if (e != hipSuccess) return e;
-      join_dx(p.nar.splits * p.nar.parts);
-    }
-    if (dw != nullptr) {
-      if (p.nar.dw_splits > 1)
-        q.dw = ws + p.dwp, q.dw_bf16 = false, q.dw_stride = E, q.dw_factor = nullptr;
-      e = launch_narrow_dw(q, st);
-      if (e != hipSuccess) return e;
-      if (p.nar.dw_splits > 1)
-        join_dw(reinterpret_cast<float*>(ws + p.dwp), p.nar.dw_splits, V * E, V, dw);
-    }
+    if (dx == nullptr && dw == nullptr) return hipGetLastError();
+    const bool dw_parts = dw != nullptr && p.nar.dw_splits > 1;
+    if (dx == nullptr) q.dx_parts = nullptr;
+    if (dw_parts) q.dw = ws + p.dwp, q.dw_bf16 = false, q.dw_stride = E, q.dw_factor = nullptr;
+    e = launch_narrow_gradients(q, st);
+    if (e != hipSuccess) return e;
+    if (dx != nullptr) join_dx(p.nar.splits * p.nar.parts);
+    if (dw_parts) join_dw(reinterpret_cast<float*>(ws + p.dwp), p.nar.dw_splits, V * E, V, dw);
     return hipGetLastError();
   }
   const int64_t xpitch = int64_t(p.padded) * 2;

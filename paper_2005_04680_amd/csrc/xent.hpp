@@ -91,14 +91,13 @@ struct NarrowArgs {
   float* target;
   float unit;
   void* sums;          // float2 [splits * parts][rows]: exponents and sums
-  float* dx_parts;     // [splits * parts][rows][dim]
-  void* dw;            // table's type, or FP32 parts [dw_splits][vocab][dim]
+  float* dx_parts;     // [splits * parts][rows][dim], null if not wanted
+  void* dw;            // table's type, or FP32 parts [dw_splits][vocab][dim]; null if not wanted
   bool dw_bf16;
   int64_t dw_stride;
   const float* dw_factor;  // null for parts
 };
 hipError_t launch_narrow_scores(const NarrowArgs& a, hipStream_t st);
-hipError_t launch_narrow_dx(const NarrowArgs& a, hipStream_t st);
-hipError_t launch_narrow_dw(const NarrowArgs& a, hipStream_t st);
+hipError_t launch_narrow_gradients(const NarrowArgs& a, hipStream_t st);
 
 }  // namespace embbag

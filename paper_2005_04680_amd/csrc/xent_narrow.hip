@@ -159,18 +159,17 @@ constexpr int groups(int wv, bool f32) { return wv == 1 && !f32 ? 2 : 1; }
 // WM wavefronts side by side over rows of x (32 TM each), the others over the rows of the table's tile,
 // SUB groups of 32 of them each.  GRAD: dx, else the sums.
 template <int EP, int P, int PD, int WM, bool GRAD, class TW>
-__global__ __launch_bounds__(kBlock, 2) void narrow_tokens(TokenArgs a) {
+__device__ __forceinline__ void narrow_tokens(const TokenArgs& a, uint32_t block, uint8_t* lds) {
   constexpr int TM = kStanding<EP, P>, WV = 4 / WM, SUB = kGroups<P, WV>;
   constexpr int BM = 32 * TM * WM, VB = 32 * WV * SUB, S = EP / 16;
   constexpr int TILE = VB * EP * 2, STAGE = TILE * P;
   constexpr int CHUNKS = VB * EP / 8 / kBlock;
   static_assert(CHUNKS >= 1, "a chunk per thread");
   typedef Tile<EP> L;
-  extern __shared__ __align__(16) uint8_t lds[];
   const int lane = lane_id(), wave = wave_id(), half = lane / 32, row = lane % 32;
   const int wm = wave % WM, wv = wave / WM;
   const int live = __builtin_amdgcn_readfirstlane(a.head->live);
-  const uint32_t z = blockIdx.x % uint32_t(a.splits), tb = blockIdx.x / uint32_t(a.splits);
+  const uint32_t z = block % uint32_t(a.splits), tb = block / uint32_t(a.splits);
   if (int64_t(tb) * BM >= live) return;
   const int64_t v0 = int64_t(z) * a.per, v1 = min(v0 + a.per, a.vocab);
 
@@ -360,23 +359,24 @@ struct VocabArgs {
   int64_t dw_part;
   const float* factor;
   int32_t splits, per;
-  uint32_t first;
 };
 
 // A wavefront's 32 TV rows of the table stand, rows that count stream.
+template <int MB>
+struct Streamed {
+  float tops[2][MB], scales[2][MB], ratios[2][MB];
+  int labels[2][MB];
+};
 template <int EP, int P, int PD, class TW, class TO>
-__global__ __launch_bounds__(kBlock, 2) void narrow_vocab(VocabArgs a) {
+__device__ __forceinline__ void narrow_vocab(const VocabArgs& a, uint32_t block, uint8_t* lds) {
   constexpr int TV = kStanding<EP, P>, SUB = kGroups<P, 1>, MB = 32 * SUB, S = EP / 16;
   constexpr int BV = 32 * TV * 4;
   constexpr int TILE = MB * EP * 2, STAGE = TILE * P;
   constexpr int ALL = MB * EP / 8 * P, CHUNKS = (ALL + kBlock - 1) / kBlock;
   static_assert(ALL % kBlock == 0, "whole chunks");
   typedef Tile<EP> L;
-  extern __shared__ __align__(16) uint8_t lds[];
-  __shared__ __align__(16) float tops[2][MB], scales[2][MB], ratios[2][MB];
-  __shared__ int labels[2][MB];
+  Streamed<MB>& rows = *reinterpret_cast<Streamed<MB>*>(lds + 2 * STAGE);
   const int lane = lane_id(), wave = wave_id(), half = lane / 32, row = lane % 32;
-  const uint32_t block = a.first + blockIdx.x;
   const uint32_t z = block % uint32_t(a.splits);
   const int64_t v0 = int64_t(block / uint32_t(a.splits)) * BV + wave * 32 * TV;
   const int live = __builtin_amdgcn_readfirstlane(a.head->live);
@@ -424,10 +424,10 @@ __global__ __launch_bounds__(kBlock, 2) void narrow_vocab(VocabArgs a) {
       *reinterpret_cast<u4*>(lds + stage * STAGE + p * TILE + r * (EP * 2) + chunk_at<EP>(r, k) * 16) = next[i];
     }
     if (threadIdx.x < MB) {
-      tops[stage][threadIdx.x] = -token.top;
-      scales[stage][threadIdx.x] = token.inv * token.ratio;
-      ratios[stage][threadIdx.x] = token.ratio;
-      labels[stage][threadIdx.x] = token.label;
+      rows.tops[stage][threadIdx.x] = -token.top;
+      rows.scales[stage][threadIdx.x] = token.inv * token.ratio;
+      rows.ratios[stage][threadIdx.x] = token.ratio;
+      rows.labels[stage][threadIdx.x] = token.label;
     }
   };
   if (m0 < m1) {
@@ -459,8 +459,8 @@ __global__ __launch_bounds__(kBlock, 2) void narrow_vocab(VocabArgs a) {
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const f4 t = *reinterpret_cast<const f4*>(&tops[cur][r0 + q * 8 + half * 4]);
-        const f4 c = *reinterpret_cast<const f4*>(&scales[cur][r0 + q * 8 + half * 4]);
+        const f4 t = *reinterpret_cast<const f4*>(&rows.tops[cur][r0 + q * 8 + half * 4]);
+        const f4 c = *reinterpret_cast<const f4*>(&rows.scales[cur][r0 + q * 8 + half * 4]);
 #pragma unroll
         for (int i = 0; i < TV; ++i)
 #pragma unroll
@@ -468,13 +468,13 @@ __global__ __launch_bounds__(kBlock, 2) void narrow_vocab(VocabArgs a) {
             d[i][q * 4 + e] = exp2_of(__builtin_fmaf(d[i][q * 4 + e], a.unit, t[e])) * c[e];
       }
       // The labels among the wavefront's rows of the table, one after the other.
-      const int64_t off = labels[cur][r0 + row] - v0;
+      const int64_t off = rows.labels[cur][r0 + row] - v0;
       uint64_t some = __builtin_amdgcn_ballot_w64(half == 0 && off >= 0 && off < 32 * TV);
       while (some != 0ull) {
         const int k = __builtin_ctzll(some);
         some &= some - 1;
         const int at = __builtin_amdgcn_readlane(int(off), k);  // of the table's rows
-        const float ratio = ratios[cur][r0 + k];
+        const float ratio = rows.ratios[cur][r0 + k];
         const bool mine = row == at % 32 && half == k / 4 % 2;
         const int reg = k / 8 * 4 + k % 4;
 #pragma unroll
@@ -522,48 +522,90 @@ __global__ __launch_bounds__(kBlock, 2) void narrow_vocab(VocabArgs a) {
   }
 }
 
+template <int EP, int P, int WM>
+constexpr int kTokenLds = 2 * 32 * (4 / WM) * kGroups<P, 4 / WM> * EP * 2 * P;
+template <int EP, int P>
+constexpr int kVocabLds = 2 * 32 * kGroups<P, 1> * EP * 2 * P + int(sizeof(Streamed<32 * kGroups<P, 1>>));
+
+template <int EP, int P, int WM, class TW>
+__global__ __launch_bounds__(kBlock, 2) void narrow_scores(TokenArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  narrow_tokens<EP, P, 1, WM, false, TW>(a, blockIdx.x, lds);
+}
+
+// Both gradients, of which either may have no blocks: neither needs the other, and one launch leaves no
+// compute unit idle between them.  Blocks from `turn` on are of the second kind; dx is the first kind if
+// `dx_first`.
+template <int EP, int P, int PD, int WM, class TW, class TO>
+__global__ __launch_bounds__(kBlock, 2) void narrow_gradients(TokenArgs t, VocabArgs v, uint32_t first,
+                                                              uint64_t turn, bool dx_first) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  const uint64_t block = uint64_t(first) + blockIdx.x;
+  const bool second = block >= turn;
+  const uint32_t at = uint32_t(second ? block - turn : block);
+  if (second != dx_first)
+    narrow_tokens<EP, P, PD, WM, true, TW>(t, at, lds);
+  else
+    narrow_vocab<EP, P, PD, TW, TO>(v, at, lds);
+}
+
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <int EP, int P, int PD, int WM, bool GRAD, class TW>
-void launch_tokens(const NarrowArgs& n, hipStream_t st) {
-  constexpr int WV = 4 / WM, VB = 32 * WV * kGroups<P, WV>;
-  constexpr int lds = 2 * VB * EP * 2 * P;
-  static_assert(lds <= 160 * 1024, "LDS");
-  auto kernel = narrow_tokens<EP, P, PD, WM, GRAD, TW>;
+TokenArgs token_args(const NarrowArgs& n) {
+  return {n.table, n.table_stride, n.n.vocab, n.n.dim, static_cast<const __bf16*>(n.x), n.x_plane,
+          static_cast<const Head*>(n.head), static_cast<const Token*>(n.tokens), n.target, n.unit,
+          static_cast<float2*>(n.sums), n.dx_parts, n.n.rows, n.n.splits, n.n.per};
+}
+VocabArgs vocab_args(const NarrowArgs& n) {
+  return {n.table, n.table_stride, n.n.vocab, n.n.dim, static_cast<const __bf16*>(n.x), n.x_plane,
+          static_cast<const Head*>(n.head), static_cast<const Token*>(n.tokens), n.unit, n.dw, n.dw_stride,
+          n.n.vocab * n.n.dim, n.dw_factor, n.n.dw_splits, n.n.dw_per};
+}
+
+template <class K>
+void allow_lds(K kernel, int lds) {
   if (lds > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  const TokenArgs a = {n.table, n.table_stride, n.n.vocab, n.n.dim, static_cast<const __bf16*>(n.x), n.x_plane,
-                       static_cast<const Head*>(n.head), static_cast<const Token*>(n.tokens), n.target, n.unit,
-                       static_cast<float2*>(n.sums), n.dx_parts, n.n.rows, n.n.splits, n.n.per};
-  hipLaunchKernelGGL(kernel, dim3(unsigned(up(n.n.rows, n.n.bm) * n.n.splits)), dim3(kBlock), lds, st, a);
 }
 
-template <int EP, int P, int PD, bool GRAD, class TW>
-void launch_tokens_shape(const NarrowArgs& n, hipStream_t st) {
+template <int EP, int P, int WM, class TW>
+void launch_sums(const NarrowArgs& n, hipStream_t st) {
+  auto kernel = narrow_scores<EP, P, WM, TW>;
+  constexpr int lds = kTokenLds<EP, P, WM>;
+  allow_lds(kernel, lds);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(up(n.n.rows, n.n.bm) * n.n.splits)), dim3(kBlock), lds, st,
+                     token_args(n));
+}
+
+template <int EP, int P, int PD, int WM, class TW, class TO>
+void launch_both(const NarrowArgs& n, hipStream_t st) {
+  auto kernel = narrow_gradients<EP, P, PD, WM, TW, TO>;
+  constexpr int lds = kTokenLds<EP, P, WM> > kVocabLds<EP, P> ? kTokenLds<EP, P, WM> : kVocabLds<EP, P>;
+  static_assert(lds <= 160 * 1024, "LDS");
+  allow_lds(kernel, lds);
+  constexpr int BV = 32 * kStanding<EP, P> * 4;
+  const int64_t nx = n.dx_parts != nullptr ? up(n.n.rows, n.n.bm) * n.n.splits : 0;
+  const int64_t nw = n.dw != nullptr ? up(n.n.vocab, BV) * n.n.dw_splits : 0;
+  // The longer blocks first.
+  const bool dx_first = int64_t(n.n.per) * n.n.bm > int64_t(n.n.dw_per) * BV;
+  for_launches(nx + nw, kBlock, [&](uint32_t first, dim3 grid) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, st, token_args(n), vocab_args(n), first,
+                       uint64_t(dx_first ? nx : nw), dx_first);
+  });
+}
+
+// Calls fn(WM).
+template <int EP, int P, class Fn>
+void for_rows(const NarrowArgs& n, Fn fn) {
   constexpr int TM = kStanding<EP, P>;
   if constexpr (P == 1) {
-    if (n.n.bm == 32 * TM) return launch_tokens<EP, P, PD, 1, GRAD, TW>(n, st);
+    if (n.n.bm == 32 * TM) return fn(std::integral_constant<int, 1>());
   }
   if (n.n.bm == 64 * TM)
-    launch_tokens<EP, P, PD, 2, GRAD, TW>(n, st);
+    fn(std::integral_constant<int, 2>());
   else
-    launch_tokens<EP, P, PD, 4, GRAD, TW>(n, st);
-}
-
-template <int EP, int P, int PD, class TW, class TO>
-void launch_vocab(const NarrowArgs& n, hipStream_t st) {
-  constexpr int BV = 32 * kStanding<EP, P> * 4, MB = 32 * kGroups<P, 1>;
-  constexpr int lds = 2 * MB * EP * 2 * P;
-  static_assert(lds <= 65536, "LDS");
-  const NarrowArgs& q = n;
-  VocabArgs a = {q.table, q.table_stride, q.n.vocab, q.n.dim, static_cast<const __bf16*>(q.x), q.x_plane,
-                 static_cast<const Head*>(q.head), static_cast<const Token*>(q.tokens), q.unit, q.dw, q.dw_stride,
-                 q.n.vocab * q.n.dim, q.dw_factor, q.n.dw_splits, q.n.dw_per, 0};
-  for_launches(up(q.n.vocab, BV) * q.n.dw_splits, kBlock, [&](uint32_t first, dim3 grid) {
-    a.first = first;
-    hipLaunchKernelGGL((narrow_vocab<EP, P, PD, TW, TO>), grid, dim3(kBlock), lds, st, a);
-  });
+    fn(std::integral_constant<int, 4>());
 }
 
 // Calls fn(EP, P, PD, the table's type).
@@ -613,7 +655,7 @@ Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32) {
   const int mb = 32 * groups(1, f32), bv = 4 * each;
   const int64_t vblocks = up(vocab, bv), steps = up(rows > 0 ? rows : 1, mb);
   int64_t ds = 2 * kNumCu / vblocks;
-  if (ds > steps / 4) ds = steps / 4;
+  if (ds > steps / 2) ds = steps / 2;
   if (ds < 1) ds = 1;
   n.dw_per = int32_t(up(steps, ds) * mb);
   n.dw_splits = int32_t(up(rows > 0 ? rows : 1, n.dw_per));
@@ -621,29 +663,24 @@ Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32) {
 }
 
 hipError_t launch_narrow_scores(const NarrowArgs& n, hipStream_t st) {
-  if (n.n.rows > 0) {
+  if (n.n.rows > 0)
     for_kind(n, [&](auto EP, auto P, auto, auto w) {
-      launch_tokens_shape<EP.value, P.value, P.value, false, decltype(w)>(n, st);  // (no D)
-    });
-  }
-  return hipGetLastError();
-}
-
-hipError_t launch_narrow_dx(const NarrowArgs& a, hipStream_t st) {
-  if (a.n.rows > 0)
-    for_kind(a, [&](auto EP, auto P, auto PD, auto w) {
-      launch_tokens_shape<EP.value, P.value, PD.value, true, decltype(w)>(a, st);
+      for_rows<EP.value, P.value>(n, [&](auto WM) {
+        launch_sums<EP.value, P.value, WM.value, decltype(w)>(n, st);
+      });
     });
   return hipGetLastError();
 }
 
-hipError_t launch_narrow_dw(const NarrowArgs& a, hipStream_t st) {
-  for_kind(a, [&](auto EP, auto P, auto PD, auto w) {
-    using TW = decltype(w);
-    if constexpr (sizeof(TW) == 2) {
-      if (a.dw_bf16) return launch_vocab<EP.value, P.value, PD.value, TW, __bf16>(a, st);
-    }
-    launch_vocab<EP.value, P.value, PD.value, TW, float>(a, st);
+hipError_t launch_narrow_gradients(const NarrowArgs& n, hipStream_t st) {
+  for_kind(n, [&](auto EP, auto P, auto PD, auto w) {
+    for_rows<EP.value, P.value>(n, [&](auto WM) {
+      using TW = decltype(w);
+      if constexpr (sizeof(TW) == 2) {
+        if (n.dw_bf16) return launch_both<EP.value, P.value, PD.value, WM.value, TW, __bf16>(n, st);
+      }
+      launch_both<EP.value, P.value, PD.value, WM.value, TW, float>(n, st);
+    });
   });
   return hipGetLastError();
 }
