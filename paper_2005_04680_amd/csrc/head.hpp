@@ -108,6 +108,35 @@ typedef u4 u4_any __attribute__((aligned(2)));
 __device__ __forceinline__ void store16(void* p, const u4& v) { *static_cast<u4_any*>(p) = v; }
 __device__ __forceinline__ u4 load16(const void* p) { return *static_cast<const u4_any*>(p); }
 
+// 8 elements of a row on their way (zeros past `n` of them, n % 4 == 0): untouched until values(), so that
+// other work can run before they are there.
+template <class T>
+struct Eight;
+template <>
+struct Eight<float> {
+  f4 a, b;
+  __device__ __forceinline__ void load(const float* p, int n) {
+    a = n > 0 ? load4(p) : f4{0.f, 0.f, 0.f, 0.f};
+    b = n > 4 ? load4(p + 4) : f4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+};
+template <>
+struct Eight<__bf16> {
+  u4 w;
+  __device__ __forceinline__ void load(const __bf16* p, int n) {
+    w = u4{0u, 0u, 0u, 0u};
+    if (n > 4) {
+      w = load16(p);
+    } else if (n > 0) {
+      const u2 h = *reinterpret_cast<const u2*>(p);
+      w.x = h.x, w.y = h.y;
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const { unpack16(w, v); }
+};
 __device__ __forceinline__ float low() { return -__builtin_inff(); }
 
 // 16 bytes of a row of which n elements exist: the others become -infinity.

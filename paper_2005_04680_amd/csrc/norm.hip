@@ -32,24 +32,11 @@ __device__ __forceinline__ Inverse inverse_of(double sum, double per, double eps
 __device__ __forceinline__ float times(float x, const Inverse& s) { return ldexpf(x, s.exp) * s.rest; }
 
 // 8 elements of a row from chunk c on (zeros past dim; dim % 4 == 0).
-__device__ __forceinline__ void load_chunk(const float* row, int c, int dim, float (&v)[8]) {
-  const f4 zero = {0.f, 0.f, 0.f, 0.f};
-  const int e = c * kChunk;
-  const f4 a = e < dim ? load4(row + e) : zero;
-  const f4 b = e + 4 < dim ? load4(row + e + 4) : zero;
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-  v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-__device__ __forceinline__ void load_chunk(const __bf16* row, int c, int dim, float (&v)[8]) {
-  const int e = c * kChunk;
-  u4 w = {0u, 0u, 0u, 0u};
-  if (e + 4 < dim) {
-    w = load16(row + e);
-  } else if (e < dim) {
-    const u2 h = *reinterpret_cast<const u2*>(row + e);
-    w.x = h.x, w.y = h.y;
-  }
-  unpack16(w, v);
+template <class T>
+__device__ __forceinline__ void load_chunk(const T* row, int c, int dim, float (&v)[8]) {
+  Eight<T> x;
+  x.load(row + c * kChunk, dim - c * kChunk);
+  x.values(v);
 }
 __device__ __forceinline__ void store_chunk(float* row, int c, int dim, const float (&v)[8]) {
   const int e = c * kChunk;
@@ -147,25 +134,43 @@ __global__ __launch_bounds__(kNormThreads<T>) void norm_rows(NormArgs a) {
   float w[NC][8];
 #pragma unroll
   for (int i = 0; i < NC; ++i) load_weight(a.weight, a.weight_bf16, t + i * T, dim, w[i]);
+  // The next row's inputs are on their way while a row is summed and stored.
+  Eight<TX> nx[NC];
+  Eight<TR> nr[NC];
+  auto fetch = [&](int64_t row) {
+    const int last = row < a.rows ? dim : 0;
+    const int64_t at = row < a.rows ? row : 0;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int e = (t + i * T) * kChunk;
+      nx[i].load(static_cast<const TX*>(a.x) + at * a.x_stride + e, last - e);
+    }
+    if (a.residual == nullptr) return;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int e = (t + i * T) * kChunk;
+      nr[i].load(static_cast<const TR*>(a.residual) + at * a.residual_stride + e, last - e);
+    }
+  };
+  fetch(int64_t(blockIdx.x) * R + threadIdx.x / T);
   int turn = 0;
   for (int64_t row0 = int64_t(blockIdx.x) * R; row0 < a.rows; row0 += int64_t(gridDim.x) * R) {
     const int64_t row = row0 + threadIdx.x / T;
     const bool in = row < a.rows;
     const int last = in ? dim : 0;  // (the others of the wavefront need its lanes)
-    const TX* x = static_cast<const TX*>(a.x) + (in ? row : 0) * a.x_stride;
     float h[NC][8];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) load_chunk(x, t + i * T, last, h[i]);
+    for (int i = 0; i < NC; ++i) nx[i].values(h[i]);
     if (a.residual != nullptr) {
-      const TR* r = static_cast<const TR*>(a.residual) + (in ? row : 0) * a.residual_stride;
-      float q[NC][8];
 #pragma unroll
-      for (int i = 0; i < NC; ++i) load_chunk(r, t + i * T, last, q[i]);
+      for (int i = 0; i < NC; ++i) {
+        float q[8];
+        nr[i].values(q);
 #pragma unroll
-      for (int i = 0; i < NC; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[i][j] += q[i][j];
+        for (int j = 0; j < 8; ++j) h[i][j] += q[j];
+      }
     }
+    if (row0 + int64_t(gridDim.x) * R < a.rows) fetch(row + int64_t(gridDim.x) * R);
     double sum[1] = {0.0};
 #pragma unroll
     for (int i = 0; i < NC; ++i)
@@ -217,31 +222,51 @@ __global__ __launch_bounds__(kNormThreads<T>) void norm_grad_rows(NormGradArgs a
   __shared__ __align__(16) float sums[R > 1 ? kBlock * NC * 8 : 4];
   const int t = threadIdx.x % T;
   const int dim = a.dim;
+  // 1024 threads have 128 registers each: the weights are loaded again for every row then, and no row ahead.
+  constexpr bool ROOM = T < 1024;
   float w[NC][8], dw[NC][8];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    load_weight(a.weight, a.weight_bf16, t + i * T, dim, w[i]);
+    if (ROOM) load_weight(a.weight, a.weight_bf16, t + i * T, dim, w[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
   }
+  // The next row's inputs are on their way while a row is summed and stored.
+  Eight<TH> nh[NC], nd[NC];
+  Eight<TY> ny[NC];
+  auto fetch = [&](int64_t row) {
+    const int last = row < a.rows ? dim : 0;
+    const int64_t at = row < a.rows ? row : 0;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int e = (t + i * T) * kChunk;
+      nh[i].load(static_cast<const TH*>(a.h) + at * a.h_stride + e, last - e);
+      ny[i].load(static_cast<const TY*>(a.dy) + at * a.dy_stride + e, last - e);
+    }
+    if (a.dsum == nullptr) return;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int e = (t + i * T) * kChunk;
+      nd[i].load(static_cast<const TH*>(a.dsum) + at * a.dsum_stride + e, last - e);
+    }
+  };
+  if (ROOM) fetch(int64_t(blockIdx.x) * R + threadIdx.x / T);
   int turn = 0;
   for (int64_t row0 = int64_t(blockIdx.x) * R; row0 < a.rows; row0 += int64_t(gridDim.x) * R) {
     const int64_t row = row0 + threadIdx.x / T;
     const bool in = row < a.rows;
     const int last = in ? dim : 0;
     const int64_t at = in ? row : 0;
-    const TH* hp = static_cast<const TH*>(a.h) + at * a.h_stride;
-    const TY* yp = static_cast<const TY*>(a.dy) + at * a.dy_stride;
-    float h[NC][8], y[NC][8], d[NC][8];
+    if (!ROOM) {
+      fetch(row);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) load_chunk(hp, t + i * T, last, h[i]);
-#pragma unroll
-    for (int i = 0; i < NC; ++i) load_chunk(yp, t + i * T, last, y[i]);
-    if (a.dsum != nullptr) {
-      const TH* p = static_cast<const TH*>(a.dsum) + at * a.dsum_stride;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) load_chunk(p, t + i * T, last, d[i]);
+      for (int i = 0; i < NC; ++i) load_weight(a.weight, a.weight_bf16, t + i * T, dim, w[i]);
     }
+    float h[NC][8], y[NC][8];
+    Eight<TH> d[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) nh[i].values(h[i]), ny[i].values(y[i]), d[i] = nd[i];
+    if (ROOM && row0 + int64_t(gridDim.x) * R < a.rows) fetch(row + int64_t(gridDim.x) * R);
     double sum[2] = {0.0, 0.0};
 #pragma unroll
     for (int i = 0; i < NC; ++i)
@@ -261,8 +286,16 @@ __global__ __launch_bounds__(kNormThreads<T>) void norm_grad_rows(NormGradArgs a
         const float n = times(h[i][j], s);
         dw[i][j] += in ? y[i][j] * n : 0.f;
         h[i][j] = times(w[i][j] * y[i][j] - n * k, s);
-        if (a.dsum != nullptr) h[i][j] += d[i][j];
       }
+    if (a.dsum != nullptr) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        float q[8];
+        d[i].values(q);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[i][j] += q[j];
+      }
+    }
     TH* p = static_cast<TH*>(a.dh) + at * a.dh_stride;
 #pragma unroll
     for (int i = 0; i < NC; ++i) store_chunk(p, t + i * T, last, h[i]);
@@ -350,7 +383,7 @@ void for_shape(int32_t dim, Fn fn) {
   else if (dim <= 4096)
     fn(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
   else if (dim <= 8192)
-    fn(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
+    fn(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
   else
     fn(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
 }

@@ -52,34 +52,6 @@ __device__ __forceinline__ f16v mfma(const u4& a, const u4& b, const f16v& c) {
                                                  0, 0);
 }
 
-// 8 elements of a row on their way (zeros past `n` of them, n % 4 == 0), untouched until terms() wants them.
-template <class T>
-struct Eight;
-template <>
-struct Eight<float> {
-  f4 a, b;
-  __device__ __forceinline__ void load(const float* p, int n) {
-    a = n > 0 ? load4(p) : f4{0.f, 0.f, 0.f, 0.f};
-    b = n > 4 ? load4(p + 4) : f4{0.f, 0.f, 0.f, 0.f};
-  }
-  __device__ __forceinline__ void values(float (&v)[8]) const {
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  }
-};
-template <>
-struct Eight<__bf16> {
-  u4 w;
-  __device__ __forceinline__ void load(const __bf16* p, int n) {
-    w = u4{0u, 0u, 0u, 0u};
-    if (n > 4) {
-      w = load16(p);
-    } else if (n > 0) {
-      const u2 h = *reinterpret_cast<const u2*>(p);
-      w.x = h.x, w.y = h.y;
-    }
-  }
-  __device__ __forceinline__ void values(float (&v)[8]) const { unpack16(w, v); }
-};
 // As P planes of BF16 terms.
 template <int P, class T>
 __device__ __forceinline__ void terms_of(const Eight<T>& x, u4 (&t)[P]) {

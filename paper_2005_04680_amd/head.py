@@ -416,12 +416,17 @@ def _weight(t, dim, name):
     return _vector(t, dim, name, t.dtype), code
 
 
-def _same_rows(t, rows, cols, name, code=None, like=""):
-    """_matrix of a tensor of `rows` rows, of the type `code` (None: any; no tensor: zeros)."""
+def _same_rows(t, shape, name, code=None, like=""):
+    """_matrix of a tensor of the shape `shape` and of the type `code` (None: any; no tensor: zeros)."""
     if t is None:
         return 0, EMBBAG_F32 if code is None else code, 0
-    m = _matrix(t, cols, name)
-    _check_rows(t, rows, name)
+    own = _type_of.get(t.dtype)
+    if t.shape == shape and own is not None and t.is_cuda and (code is None or own == code):
+        s0, s1 = t.stride()
+        if s1 == 1 and s0 >= shape[1]:
+            return t.data_ptr(), own, s0
+    m = _matrix(t, shape[1], name)
+    _check_rows(t, shape[0], name)
     if code is not None and m[1] != code:
         raise TypeError(f"{name}: dtype {t.dtype}, expected that of {like}")
     return m
@@ -431,12 +436,12 @@ def embbag_rmsnorm(x, weight, eps, out=None, mx8=None, residual=None, sum_out=No
     """RMS norm of ``x`` [rows, dim] plus ``residual``, times ``weight`` ([dim], None: ones), into
     ``out`` and/or the 8-bit rows ``mx8`` (``Mx8Rows``); the sum itself into ``sum_out`` (which may
     be ``residual``, and has its type)."""
-    dim = x.shape[1] if len(x.shape) == 2 else -1
-    p, ty, ld = _matrix(x, dim, "x")
-    rows = x.shape[0]
-    r, tr, lr = _same_rows(residual, rows, dim, "residual")
-    s, ts, ls = _same_rows(sum_out, rows, dim, "sum_out", None if residual is None else tr, "residual")
-    q, tq, lq = _same_rows(out, rows, dim, "out")
+    shape = x.shape
+    p, ty, ld = _matrix(x, shape[1] if len(shape) == 2 else -1, "x")
+    rows, dim = shape
+    r, tr, lr = _same_rows(residual, shape, "residual")
+    s, ts, ls = _same_rows(sum_out, shape, "sum_out", None if residual is None else tr, "residual")
+    q, tq, lq = _same_rows(out, shape, "out")
     w, tw = _weight(weight, dim, "weight")
     codes = scales = 0
     if mx8 is not None:
@@ -454,12 +459,12 @@ def embbag_rmsnorm_grad_workspace_bytes(rows, dim) -> int:
 def embbag_rmsnorm_grad(dy, h, weight, eps, dh, workspace, dweight=None, dsum=None, stream=None) -> int:
     """Gradients of ``embbag_rmsnorm``: ``dh`` (that of x and of the residual) and ``dweight`` from the
     output's gradient ``dy``, the sum ``h`` and the sum's own gradient ``dsum``."""
-    dim = h.shape[1] if len(h.shape) == 2 else -1
-    p, th, lh = _matrix(h, dim, "h")
-    rows = h.shape[0]
-    y, ty, ly = _same_rows(dy, rows, dim, "dy")
-    d, _, ld = _same_rows(dh, rows, dim, "dh", th, "h")
-    s, _, ls = _same_rows(dsum, rows, dim, "dsum", th, "h")
+    shape = h.shape
+    p, th, lh = _matrix(h, shape[1] if len(shape) == 2 else -1, "h")
+    rows, dim = shape
+    y, ty, ly = _same_rows(dy, shape, "dy")
+    d, _, ld = _same_rows(dh, shape, "dh", th, "h")
+    s, _, ls = _same_rows(dsum, shape, "dsum", th, "h")
     w, tw = _weight(weight, dim, "weight")
     g, tg = _weight(dweight, dim, "dweight")
     if dweight is not None and tg != (ty if weight is None else tw):
@@ -554,13 +559,13 @@ def embbag_xent(x, table, labels, loss, workspace, grad_x=None, grad_table=None,
     """Loss of every row of ``x`` [rows, dim] on its label among the rows of ``table`` [vocab, dim]
     (scores ``scale`` x table^T; a negative label is no row to learn) and, into ``grad_x`` and
     ``grad_table``, the gradients of the losses' sum."""
-    dim = x.shape[1] if len(x.shape) == 2 else -1
-    p, ty, ld = _matrix(x, dim, "x")
-    rows = x.shape[0]
+    shape, tshape = x.shape, table.shape
+    p, ty, ld = _matrix(x, shape[1] if len(shape) == 2 else -1, "x")
+    rows, dim = shape
     w, tw, lw = _matrix(table, dim, "table")
-    vocab = table.shape[0]
-    g, _, lg = _same_rows(grad_x, rows, dim, "grad_x", ty, "x")
-    h, _, lh = _same_rows(grad_table, vocab, dim, "grad_table", tw, "table")
+    vocab = tshape[0]
+    g, _, lg = _same_rows(grad_x, shape, "grad_x", ty, "x")
+    h, _, lh = _same_rows(grad_table, tshape, "grad_table", tw, "table")
     a = _pack_xent(_i32(rows), dim, vocab, ty, p, ld, tw, w, lw, _vector(labels, rows, "labels", _I32_T),
                    _vector(row_weights, rows, "row_weights", _F32_T), scale,
                    _vector(loss, rows, "loss", _F32_T), g, lg, h, lh)
