@@ -34,6 +34,20 @@ struct Side {
   int64_t plane;
 };
 
+// Splits of a contraction of `steps` steps over tiles that would leave blocks idle: as many as make `blocks`
+// of them, of 8 steps at least, and the steps of each.
+struct Splits {
+  int32_t count, per;
+};
+__host__ __device__ __forceinline__ Splits split_steps(int64_t tiles, int64_t steps, int32_t blocks) {
+  if (steps < 1) steps = 1;
+  int64_t s = blocks / (tiles > 0 ? tiles : 1);
+  if (s > steps / 8) s = steps / 8;
+  if (s < 1) s = 1;
+  const int64_t per = (steps + s - 1) / s;
+  return {int32_t((steps + per - 1) / per), int32_t(per)};
+}
+
 // The problem.  `live`, where not null, holds the number of rows of m (or of k where LIVE_K) in
 // memory; the counts given are then upper bounds.
 struct Gemm {
@@ -41,8 +55,11 @@ struct Gemm {
   int64_t n, m, k;
   const int32_t* live;
   int32_t pairs;   // of planes: 1, 2 (both of b) or 6 (of three each)
-  int32_t splits;  // of k
-  int32_t per;     // steps per split and pair
+  Splits splits;   // of k: how many, and steps per split and pair
+  // Where not 0, the splits are found from the tiles of the rows that count instead: split_steps of
+  // `steps`.
+  int32_t blocks;
+  int64_t steps;
 };
 
 // Pair number i: the planes of a and b.
@@ -181,7 +198,10 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
       m_end = live;
   }
   const uint32_t mtiles = LIVE_K ? mtiles_most : uint32_t((m_end + BM - 1) / BM);
-  const uint32_t plain = mtiles * ntiles, tiles = plain * uint32_t(g.splits);
+  const uint32_t plain = mtiles * ntiles;
+  Splits sp = g.splits;
+  if (g.blocks != 0) sp = split_steps(plain, g.steps, g.blocks);
+  const uint32_t tiles = plain * uint32_t(sp.count);
   const uint32_t range = (tiles + kNumXcd - 1) / kNumXcd, stride = gridDim.x / kNumXcd;
   const uint32_t end = min((blockIdx.x % kNumXcd + 1) * range, tiles);
   uint32_t tile = blockIdx.x % kNumXcd * range + blockIdx.x / kNumXcd;
@@ -189,9 +209,9 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
 
   // Steps of split z for a pair of planes (one at least, of zeros where there is nothing to add).
   auto steps_of = [&](uint32_t z) {
-    const int64_t k0 = int64_t(z) * g.per * kStepK;
+    const int64_t k0 = int64_t(z) * sp.per * kStepK;
     const int64_t left = (k_end - k0 + kStepK - 1) / kStepK;
-    return int(left < 1 ? 1 : left < g.per ? left : g.per);
+    return int(left < 1 ? 1 : left < sp.per ? left : sp.per);
   };
   uint32_t ltile = tile;
   int lstep = 0, lsteps = 0, lpair = 0;
@@ -203,7 +223,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
     tile_at(ltile - z * plain, mtiles, ntiles, strip, &mt, &nt);
     int pa, pb;
     planes_of(g.pairs, lpair, &pa, &pb);
-    const int64_t k0 = int64_t(z) * g.per * kStepK;
+    const int64_t k0 = int64_t(z) * sp.per * kStepK;
     sa.open(g.a, pa, int64_t(nt) * BN, g.n, k0, k_end, lane, wave);
     sb.open(g.b, pb, int64_t(mt) * BM, m_end, k0, k_end, lane, wave);
     lsteps = steps_of(z);
@@ -343,9 +363,10 @@ void launch_gemm(const Gemm& g, const Epi& epi, uint32_t strip, hipStream_t st) 
   if (lds > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  const uint64_t range = (uint64_t(mtiles) * ntiles * uint32_t(g.splits) + kNumXcd - 1) / kNumXcd;
+  const uint64_t range = (uint64_t(mtiles) * ntiles * uint32_t(g.splits.count) + kNumXcd - 1) / kNumXcd;
   const uint32_t per_xcd = kNumCu / kNumXcd * RESIDENT;
-  hipLaunchKernelGGL(kernel, dim3(kNumXcd * uint32_t(range < per_xcd ? range : per_xcd)), dim3(W * kWave),
+  const uint32_t blocks = g.blocks != 0 ? uint32_t(g.blocks) / kNumXcd : uint32_t(range);
+  hipLaunchKernelGGL(kernel, dim3(kNumXcd * (blocks < per_xcd ? blocks : per_xcd)), dim3(W * kWave),
                      lds, st, g, epi, mtiles, ntiles, strip);
 }
 

@@ -392,14 +392,13 @@ struct GradEpi {
   }
 };
 
-// Sums times `factor` into rows of `out` (the row that `map` names at a place, or the place itself), or into
-// part z, where `add` adds to what it holds.
+// Sums times `factor` into rows of `out`, or into part z of parts [rows of m][pitch] (`part` elements
+// each; of the rows that count where that is negative), where `add` adds to what they hold.
 template <class T>
 struct StoreEpi {
   T* out;
   int64_t pitch;
   int64_t columns;
-  const int32_t* map;
   const float* factor;
   int64_t part;
   bool add;
@@ -426,7 +425,7 @@ struct StoreEpi {
         stored_rows<T, TN>(turn, [&](int r, int c, const u4& v) {
           const int64_t at = m + j * 32 + r, col = n + h * 32 + c;
           if (at >= m_end || col >= columns) return;
-          T* p = out + z * part + (map != nullptr ? int64_t(map[at]) : at) * pitch + col;
+          T* p = out + z * (part < 0 ? m_end * pitch : part) + at * pitch + col;
           if (col + V <= columns) {
             if (sizeof(T) == 4 && add) {
               float x[kVec<T>], y[kVec<T>];
@@ -449,9 +448,16 @@ struct StoreEpi {
 
 // The parts [splits][rows of m][dim] added up, times the factor, into the rows that `map` names: SLICES
 // threads for 4 elements add every SLICES-th part each, then their sums are added in order.
+struct PartCount {
+  int32_t count;
+  int64_t part;  // elements of a part
+  // Where not 0, both are those of a product whose splits are found from the rows that count.
+  int32_t blocks, bm, ntiles;
+  int64_t steps;
+};
 template <int SLICES, class T>
-__global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restrict__ parts, int32_t splits,
-                                                          int64_t part, const int32_t* __restrict__ live,
+__global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restrict__ parts, PartCount pc,
+                                                          const int32_t* __restrict__ live,
                                                           int64_t rows, FastDiv d4,
                                                           const int32_t* __restrict__ map,
                                                           const float* __restrict__ factor,
@@ -465,6 +471,12 @@ __global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restric
   const int64_t at = row0 + q;
   const int c = int(uint32_t(i) - q * d4.div) * 4;
   const int64_t end = live != nullptr ? int64_t(*live) : rows;
+  int32_t splits = pc.count;
+  int64_t part = pc.part;
+  if (pc.blocks != 0) {
+    splits = split_steps((end + pc.bm - 1) / pc.bm * pc.ntiles, pc.steps, pc.blocks).count;
+    part = end * (int64_t(d4.div) * 4);
+  }
   const bool in = i < (rows - row0) * int64_t(d4.div) && at < end;
   f4 s = {0.f, 0.f, 0.f, 0.f};
   if (in) {
@@ -486,19 +498,18 @@ __global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restric
 // Slices where the parts are many: their loads are a chain otherwise (33 rows of 128 from 250 parts: 18 us
 // with one).
 template <class T>
-void launch_join_parts(const float* parts, int32_t splits, int64_t part, const int32_t* live, int64_t rows,
-                       int32_t dim, const int32_t* map, const float* factor, T* out, int64_t pitch,
+void launch_join_parts(const float* parts, const PartCount& pc, const int32_t* live, int64_t rows, int32_t dim, const int32_t* map, const float* factor, T* out, int64_t pitch,
                        int64_t row0, hipStream_t st) {
   const int64_t n = (rows - row0) * (dim / 4);
   const FastDiv d = fast_div(uint32_t(dim / 4));
   auto run = [&](auto slices) {
     constexpr int S = decltype(slices)::value;
     hipLaunchKernelGGL((xent_join_parts<S, T>), dim3(unsigned((n + kBlock / S - 1) / (kBlock / S))),
-                       dim3(kBlock), 0, st, parts, splits, part, live, rows, d, map, factor, out, pitch, row0);
+                       dim3(kBlock), 0, st, parts, pc, live, rows, d, map, factor, out, pitch, row0);
   };
-  if (splits > 32)
+  if (pc.count > 32)
     run(std::integral_constant<int, 32>());
-  else if (splits > 4)
+  else if (pc.count > 4)
     run(std::integral_constant<int, 4>());
   else
     run(std::integral_constant<int, 1>());
@@ -525,27 +536,26 @@ struct Plan {
   int32_t padded;      // elements of a packed row
   int64_t piece;       // columns of the vocabulary at a time (a multiple of 256)
   Shape scores, dx, dw;
-  int32_t dx_splits, dx_per, dw_splits, dw_per;
+  Splits dx_splits, dw_splits;
   // Workspace.
   size_t place, row, tokens, target, x, parts, w, d, dxp, dwp, total;
 };
 
-// Of m rows (an upper bound) and n columns, in `rest` further blocks of work (splits that may be had).
-Shape shape_of(int64_t m, int64_t n, int64_t rest) {
-  if (m <= 32) return {128, 32};
-  if (m <= 64) return {128, 64};
-  if (up(m, 256) * up(n, 256) * rest >= kNumCu * 3 / 4 && n > 128 && m > 128) return {256, 256};
-  return {128, 128};
+// Tiles of 256 x 256 (one block per compute unit) or 128 x 128 (two, of which one's products run while the
+// other stores), by their estimated time in units of 1000 cycles: a round of the chip of `steps` steps takes
+// 1.65 or 1.11 of them each and what an epilogue of the larger tile shows.  Measured, us, the whole call with
+// 256 / 128: scores, 2000 x 50000 x 512 551 / 518, 4096 x 131072 x 2048 7153 / 8545, FP32 500 x
+// 30000 x 256 267 / 281; dW, 1999 x 50001 x 300 340 / 319, 100 x 50000 x 1024 180 / 163, 2000 x 50000 x 512
+// 551 / 562.
+Shape cheaper(int64_t m, int64_t n, int64_t steps, double epilogue) {
+  if (m <= 128 || n <= 128) return {128, 128};
+  const double big = double(up(up(m, 256) * up(n, 256), kNumCu)) * (1.65 * steps + epilogue);
+  const double small = double(up(up(m, 128) * up(n, 128), kNumCu)) / 2 * (1.11 * steps + 0.35 * epilogue);
+  return big <= small ? Shape{256, 256} : Shape{128, 128};
 }
-// Splits of `steps` steps that fill the chip with tiles.
-void split_steps(int64_t tiles, int64_t steps, int resident, int32_t* splits, int32_t* per) {
-  int64_t s = int64_t(kNumCu) * resident / (tiles > 0 ? tiles : 1);
-  if (s > steps / 8) s = steps / 8;
-  if (s < 1) s = 1;
-  if (steps < 1) steps = 1;
-  *per = int32_t(up(steps, s));
-  *splits = int32_t(up(steps, *per));
-}
+Shape few_rows(int64_t m) { return m <= 32 ? Shape{128, 32} : Shape{128, 64}; }
+int blocks_of(Shape s) { return s.bn == 256 ? kNumCu : 2 * kNumCu; }
+int64_t tiles_of(Shape s, int64_t m, int64_t n) { return up(m, s.bm) * up(n, s.bn); }
 
 Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) {
   Plan p = {};
@@ -592,19 +602,26 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   const int64_t pieces = up(vocab, piece);
   p.piece = up(up(vocab, pieces), 256) * 256;  // pieces of one size
   p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
-  p.scores = shape_of(rows, p.piece, 1);
+  const int64_t steps = up(dim, kStepK);
+  p.scores = rows <= 64 ? few_rows(rows) : cheaper(rows, p.piece, steps * (f32 ? 6 : 1), 16);
   p.parts = take(size_t(up(vocab, p.scores.part())) * size_t(rows) * sizeof(float2));
   p.w = p.pack ? take(size_t(p.piece) * size_t(p.padded) * 2 * planes) : 0;
   if (backward) {
     p.d = take(size_t(rows) * size_t(p.piece) * 2 * p.terms);
-    p.dx = shape_of(rows, dim, 16);
-    split_steps(up(rows, p.dx.bm) * up(dim, p.dx.bn), up(p.piece, kStepK), p.dx.bn == 256 ? 1 : 2,
-                &p.dx_splits, &p.dx_per);
-    p.dxp = take(size_t(p.dx_splits) * size_t(rows) * size_t(dim) * 4);
-    p.dw = shape_of(p.piece, dim, 1);
-    split_steps(up(p.piece, p.dw.bm) * up(dim, p.dw.bn), up(rows, kStepK), p.dw.bn == 256 ? 1 : 2,
-                &p.dw_splits, &p.dw_per);
-    if (p.dw_splits > 1) p.dwp = take(size_t(p.dw_splits) * size_t(p.piece) * size_t(dim) * 4);
+    // dx: the larger tiles where they, split, leave few compute units idle.
+    const int64_t psteps = up(p.piece, kStepK);
+    p.dx = {256, 256};
+    if (rows <= 64)
+      p.dx = few_rows(rows);
+    else if (rows <= 128 || dim <= 128 ||
+             tiles_of(p.dx, rows, dim) * split_steps(tiles_of(p.dx, rows, dim), psteps, kNumCu).count < kNumCu * 3 / 4)
+      p.dx = {128, 128};
+    p.dx_splits = split_steps(tiles_of(p.dx, rows, dim), psteps, blocks_of(p.dx));
+    const int64_t area = int64_t(blocks_of(p.dx)) * p.dx.bm * p.dx.bn, whole = int64_t(rows) * dim;
+    p.dxp = take(size_t(area > whole ? area : whole) * 4);
+    p.dw = cheaper(p.piece, dim, up(rows, kStepK) * p.pairs, 8);
+    p.dw_splits = split_steps(tiles_of(p.dw, p.piece, dim), up(rows, kStepK), blocks_of(p.dw));
+    if (p.dw_splits.count > 1) p.dwp = take(size_t(p.dw_splits.count) * size_t(p.piece) * size_t(dim) * 4);
   }
   p.total = at;
   return p;
@@ -664,11 +681,11 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       hipLaunchKernelGGL(xent_join<64>, dim3(unsigned(up(N, 64))), dim3(1024), 0, st, parts, int64_t(N), count,
                          unit, rows, a.loss);
   };
-  auto join_dx = [&](int32_t count) {
+  auto join_dx = [&](const PartCount& pc) {
     const int64_t most = (int64_t(1) << 25) / (E / 4);  // 32 threads for each
     for (int64_t r0 = 0; r0 < N; r0 += most) {
       const int64_t n = N - r0 < most ? N - r0 : most;
-      launch_join_parts<TX>(dxp, count, int64_t(N) * E, &head->live, r0 + n, E, rows.row, &head->factor, dx,
+      launch_join_parts<TX>(dxp, pc, &head->live, r0 + n, E, rows.row, &head->factor, dx,
                             a.grad_x_stride, r0, st);
     }
   };
@@ -676,7 +693,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     const int64_t most = (int64_t(1) << 25) / (E / 4);  // 32 threads for each
     for (int64_t r0 = 0; r0 < n; r0 += most) {
       const int64_t q = n - r0 < most ? n - r0 : most;
-      launch_join_parts<TW>(from, count, part, nullptr, r0 + q, E, nullptr, &head->factor_w, to,
+      launch_join_parts<TW>(from, {count, part, 0, 0, 0, 0}, nullptr, r0 + q, E, nullptr, &head->factor_w, to,
                             a.grad_table_stride, r0, st);
     }
   };
@@ -692,7 +709,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     if (dw_parts) q.dw = ws + p.dwp, q.dw_bf16 = false, q.dw_stride = E, q.dw_factor = nullptr;
     e = launch_narrow_gradients(q, st);
     if (e != hipSuccess) return e;
-    if (dx != nullptr) join_dx(p.nar.splits * p.nar.parts);
+    if (dx != nullptr) join_dx({p.nar.splits * p.nar.parts, int64_t(N) * E, 0, 0, 0, 0});
     if (dw_parts) join_dw(reinterpret_cast<float*>(ws + p.dwp), p.nar.dw_splits, V * E, V, dw);
     return hipGetLastError();
   }
@@ -714,7 +731,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   const Shape ss = p.scores;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
-    const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, 1, int32_t(up(E, kStepK))};
+    const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0};
     run_gemm<false, false, false>(
         g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n}, ss, st);
   }
@@ -723,11 +740,10 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
 
   const int64_t dplane = int64_t(N) * p.piece;
   const Side ds = {d, p.piece * 2, dplane * 2};
-  const int64_t dpart = int64_t(N) * E;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
     const Side wsd = side_w(v0, n);
-    const Gemm g = {wsd, xs, n, N, E, &head->live, pairs, 1, int32_t(up(E, kStepK))};
+    const Gemm g = {wsd, xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0};
     auto grad = [&](auto terms) {
       run_gemm<false, false, false>(
           g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, unit, v0, n}, ss, st);
@@ -739,26 +755,24 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     else
       grad(std::integral_constant<int, 1>());
     if (dx != nullptr) {
-      const Gemm gx = {wsd, ds, E, N, n, &head->live, p.pairs, p.dx_splits, p.dx_per};
-      run_gemm<true, false, false>(gx, StoreEpi<float>{dxp, E, E, nullptr, nullptr, dpart, v0 > 0},
-                                   p.dx, st);
+      const Gemm gx = {wsd, ds, E, N, n, &head->live, p.pairs, p.dx_splits, blocks_of(p.dx), up(p.piece, kStepK)};
+      run_gemm<true, false, false>(gx, StoreEpi<float>{dxp, E, E, nullptr, -1, v0 > 0}, p.dx, st);
     }
     if (dw != nullptr) {
-      const Gemm gw = {xs, ds, E, n, N, &head->live, p.pairs, p.dw_splits, p.dw_per};
+      const Gemm gw = {xs, ds, E, n, N, &head->live, p.pairs, p.dw_splits, 0, 0};
       const Shape sw = p.dw;
       TW* to = dw + v0 * a.grad_table_stride;
-      if (p.dw_splits == 1) {
-        run_gemm<true, true, true>(gw, StoreEpi<TW>{to, a.grad_table_stride, E, nullptr, &head->factor_w, 0,
-                                                    false}, sw, st);
+      if (p.dw_splits.count == 1) {
+        run_gemm<true, true, true>(gw, StoreEpi<TW>{to, a.grad_table_stride, E, &head->factor_w, 0, false}, sw, st);
       } else {
         float* dwp = reinterpret_cast<float*>(ws + p.dwp);
-        run_gemm<true, true, true>(gw, StoreEpi<float>{dwp, E, E, nullptr, nullptr, p.piece * E, false}, sw,
-                                   st);
-        join_dw(dwp, p.dw_splits, p.piece * E, n, to);
+        run_gemm<true, true, true>(gw, StoreEpi<float>{dwp, E, E, nullptr, p.piece * E, false}, sw, st);
+        join_dw(dwp, p.dw_splits.count, p.piece * E, n, to);
       }
     }
   }
-  if (dx != nullptr) join_dx(p.dx_splits);
+  if (dx != nullptr)
+    join_dx({p.dx_splits.count, 0, blocks_of(p.dx), p.dx.bm, int32_t(up(E, p.dx.bn)), up(p.piece, kStepK)});
   return hipGetLastError();
 }
 

@@ -137,7 +137,8 @@ def test_weights_and_scale(N, V, E, t, scale):
                                      (3000, 1, 64, "f32"), (4500, 257, 100, "f32"), (20000, 14001, 132, "bf16"),
                                      (7000, 14000, 132, "f32"), (3, 600001, 136, "bf16"), (2, 530000, 132, "f32"),
                                      (3000, 1, 132, "f32"), (4500, 257, 164, "f32"), (9000, 1000, 128, "bf16"),
-                                     (2000, 30001, 128, "f32"), (100, 70001, 64, "bf16")])
+                                     (2000, 30001, 128, "f32"), (100, 70001, 64, "bf16"), (1000, 32763, 2052, "bf16"),
+                                     (1000, 32763, 512, "f32")])
 def test_large(N, V, E, t):
     check(N, V, E, N, t, t, sure=4.0)
 
