@@ -593,10 +593,13 @@ __global__ __launch_bounds__(kBlock) void scores_direct(const TX* __restrict__ x
   }
 }
 
-// The same from 8-bit rows, read in place.  Into BF16, of product j's four blocks (one of each group) lane
+// The same from 8-bit rows, which every block copies to LDS first where they are few (kStaged bytes; rows
+// 16 bytes further apart, so that 16 of them do not share banks), else read in place.  Into BF16, of product j's four blocks (one of each group) lane
 // group q takes half q % 2 of the first or second (q / 2) and of the third or fourth, and gives the scale
 // of block q; into FP32 it takes block q of x as of W.
-template <class T>
+constexpr int kStaged = 16384;
+
+template <class T, bool STAGED>
 __global__ __launch_bounds__(kBlock) void scores8_direct(const uint8_t* __restrict__ xc,
                                                          const uint32_t* __restrict__ xs, Mx4View w,
                                                          int32_t m, int32_t groups,
@@ -610,31 +613,50 @@ __global__ __launch_bounds__(kBlock) void scores8_direct(const uint8_t* __restri
   const uint8_t* wc = w.codes + wn * nb * 16;
   const uint32_t* wsc = reinterpret_cast<const uint32_t*>(w.scales) + wn * groups;
   constexpr bool EXACT = kExact<true, T>;
-  const uint8_t* xr = xc + int64_t(xm) * groups * 128 + (EXACT ? 0 : q % 2 * 16);
+  __shared__ __align__(16) uint8_t rows[STAGED ? kStaged + 16 * 16 : 16];
+  const int pitch = STAGED ? groups * 128 + 16 : groups * 128;
+  const uint8_t* xr = (STAGED ? rows : xc) + int64_t(xm) * pitch + (EXACT ? 0 : q % 2 * 16);
   const uint32_t* xsc = xs + int64_t(xm) * groups;
 
   const u4 none = {0u, 0u, 0u, 0u};
   u4 b[4];
   Bytes32 a[4];
   uint32_t sw, sx;
-  auto load = [&](int g0) {
-    const int g = g0 + q, ga = EXACT ? g : g0 + q / 2, gb = EXACT ? g : ga + 2;
+  auto load_w = [&](int g0) {
+    const int g = g0 + q;
     sw = g < groups ? wsc[g] : 0u;
     sx = g < groups ? xsc[g] : 0u;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 4; ++j)
       b[j] = g * 4 + j < nb ? *reinterpret_cast<const u4*>(wc + (g * 4 + j) * 16) : none;
+  };
+  auto load_x = [&](int g0) {
+    const int g = g0 + q, ga = EXACT ? g : g0 + q / 2, gb = EXACT ? g : ga + 2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
       a[j].lo = ga < groups ? *reinterpret_cast<const u4*>(xr + ga * 128 + j * 32) : none;
       a[j].hi = gb < groups ? *reinterpret_cast<const u4*>(xr + gb * 128 + j * 32 + (EXACT ? 16 : 0)) : none;
     }
   };
-  load(0);
+  load_w(0);
+  if constexpr (STAGED) {
+    const int per = groups * 8;  // of 16 bytes, of a row
+    for (int i = threadIdx.x; i < m * per; i += kBlock)
+      *reinterpret_cast<u4*>(rows + i / per * pitch + i % per * 16) = reinterpret_cast<const u4*>(xc)[i];
+    __syncthreads();
+  } else {
+    load_x(0);
+  }
   f4 c = {0.f, 0.f, 0.f, 0.f};
   for (int g0 = 0; g0 < groups; g0 += 4) {
+    if (STAGED) load_x(g0);
     const u4 v[4] = {b[0], b[1], b[2], b[3]};
     const Bytes32 u[4] = {a[0], a[1], a[2], a[3]};
     const uint32_t tw = sw, tx = sx;
-    if (g0 + 4 < groups) load(g0 + 4);
+    if (g0 + 4 < groups) {
+      load_w(g0 + 4);
+      if (!STAGED) load_x(g0 + 4);
+    }
     if constexpr (EXACT) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -780,8 +802,12 @@ void launch_scores8(const uint8_t* xc, const uint32_t* xs, int32_t m, int32_t gr
                     T* out, int64_t ldo, char* ws, hipStream_t st) {
   if (m <= 16) {
     for_launches((w.rows + 63) / 64, kBlock, [&](uint32_t first, dim3 grid) {
-      hipLaunchKernelGGL(scores8_direct<T>, grid, dim3(kBlock), 0, st, xc, xs, w, m, groups, out, ldo,
-                         first);
+      if (m * groups * 128 <= kStaged)
+        hipLaunchKernelGGL((scores8_direct<T, true>), grid, dim3(kBlock), 0, st, xc, xs, w, m, groups, out,
+                           ldo, first);
+      else
+        hipLaunchKernelGGL((scores8_direct<T, false>), grid, dim3(kBlock), 0, st, xc, xs, w, m, groups, out,
+                           ldo, first);
     });
     return;
   }
