@@ -351,6 +351,10 @@ int embbag_xent(const embbag_xent_t* args, void* workspace, size_t workspace_byt
   if (a.rows > 0 && (!rows_ok(a.x, a.x_type, a.x_stride, a.dim) || a.labels == nullptr || a.loss == nullptr ||
                      (a.grad_x != nullptr && !rows_ok(a.grad_x, a.x_type, a.grad_x_stride, a.dim))))
     return EMBBAG_ERR_INVALID_ARG;
+  // A gradient in its side's place: x is read before its gradient is written, the table is not.
+  if (a.grad_table != nullptr && a.grad_table == a.table) return EMBBAG_ERR_INVALID_ARG;
+  if (a.rows > 1 && a.grad_x != nullptr && a.grad_x == a.x && a.grad_x_stride != a.x_stride)
+    return EMBBAG_ERR_INVALID_ARG;
   const bool f32 = a.x_type == EMBBAG_F32 || a.table_type == EMBBAG_F32;
   const size_t need = xent_workspace(a.rows, a.vocab, a.dim, f32,
                                      a.grad_x != nullptr || a.grad_table != nullptr);

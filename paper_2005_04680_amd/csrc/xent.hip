@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kBlock) void xent_pack_w(const T* __restrict__ w, i
 // A tile's parts: of each row and the wavefront's 32 TN columns the exponent of the largest score, rounded,
 // and the sum of the exponentials beside exactly that.
 struct StatsEpi {
-  float2* parts;         // [columns / (32 TN)][pitch]
+  float2* parts;         // [the piece's columns / (32 TN)][pitch]
   int64_t pitch;
   const Token* tokens;
   float* target;
@@ -245,16 +245,17 @@ struct StatsEpi {
             if (int(place) == i * 32 + r / 4 * 8 + r % 4) z = acc[i][j][r];
         target[at] = z;
       }
-      if (in && half == 0 && n < columns) parts[((first + n) / (32 * TN)) * pitch + at] = float2{top * unit, sum};
+      if (in && half == 0 && n < columns) parts[n / (32 * TN) * pitch + at] = float2{top * unit, sum};
     }
   }
 };
 
-// Joins the parts of TOKENS rows per block; losses, and what the backward needs.
+// Joins the parts of TOKENS rows per block to what the pieces before have left (none if `first`) in top and
+// inv; after the `last` piece losses, and what the backward needs.
 template <int TOKENS>
 __global__ __launch_bounds__(1024) void xent_join(const float2* __restrict__ parts, int64_t pitch,
-                                                  int32_t count, float unit, Rows rows,
-                                                  float* __restrict__ loss) {
+                                                  int32_t count, bool first, bool last, float unit,
+                                                  Rows rows, float* __restrict__ loss) {
   constexpr int SLICES = 1024 / TOKENS;
   __shared__ float2 shared[SLICES][TOKENS + 1];
   const int live = rows.head->live;
@@ -282,6 +283,12 @@ __global__ __launch_bounds__(1024) void xent_join(const float2* __restrict__ par
   }
   if (slice != 0 || at >= live) return;
   Token k = rows.tokens[at];
+  if (!first) add(float2{k.top, k.inv});
+  if (!last) {
+    k.top = top, k.inv = sum;
+    rows.tokens[at] = k;
+    return;
+  }
   const float w = k.ratio;
   const int r = rows.row[at];
   loss[r] = w * (__builtin_fmaf(-rows.target[at], unit, top) * kLn2 + __builtin_logf(sum));
@@ -604,7 +611,7 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
   const int64_t steps = up(dim, kStepK);
   p.scores = rows <= 64 ? few_rows(rows) : cheaper(rows, p.piece, steps * (f32 ? 6 : 1), 16);
-  p.parts = take(size_t(up(vocab, p.scores.part())) * size_t(rows) * sizeof(float2));
+  p.parts = take(size_t(up(p.piece, p.scores.part())) * size_t(rows) * sizeof(float2));
   p.w = p.pack ? take(size_t(p.piece) * size_t(p.padded) * 2 * planes) : 0;
   if (backward) {
     p.d = take(size_t(rows) * size_t(p.piece) * 2 * p.terms);
@@ -673,13 +680,13 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
                          a.grad_x_stride);
   }
 
-  auto join_sums = [&](int32_t count) {
+  auto join_sums = [&](int32_t count, bool first, bool last) {
     if (N > 0 && N <= 256)
       hipLaunchKernelGGL(xent_join<4>, dim3(unsigned(up(N, 4))), dim3(1024), 0, st, parts, int64_t(N), count,
-                         unit, rows, a.loss);
+                         first, last, unit, rows, a.loss);
     else if (N > 0)
       hipLaunchKernelGGL(xent_join<64>, dim3(unsigned(up(N, 64))), dim3(1024), 0, st, parts, int64_t(N), count,
-                         unit, rows, a.loss);
+                         first, last, unit, rows, a.loss);
   };
   auto join_dx = [&](const PartCount& pc) {
     const int64_t most = (int64_t(1) << 25) / (E / 4);  // 32 threads for each
@@ -702,7 +709,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
                     unit, parts, dxp, dw, sizeof(TW) == 2, a.grad_table_stride, &head->factor_w};
     hipError_t e = launch_narrow_scores(q, st);
     if (e != hipSuccess) return e;
-    join_sums(p.nar.splits * p.nar.parts);
+    join_sums(p.nar.splits * p.nar.parts, true, true);
     if (dx == nullptr && dw == nullptr) return hipGetLastError();
     const bool dw_parts = dw != nullptr && p.nar.dw_splits > 1;
     if (dx == nullptr) q.dx_parts = nullptr;
@@ -734,8 +741,8 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0};
     run_gemm<false, false, false>(
         g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n}, ss, st);
+    join_sums(int32_t(up(n, ss.part())), v0 == 0, v0 + n == V);
   }
-  join_sums(int32_t(up(V, ss.part())));
   if (dx == nullptr && dw == nullptr) return hipGetLastError();
 
   const int64_t dplane = int64_t(N) * p.piece;

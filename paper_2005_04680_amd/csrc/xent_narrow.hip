@@ -621,7 +621,7 @@ Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32) {
   int64_t splits = 2 * kNumCu / blocks;
   if (splits > tiles / 2) splits = tiles / 2;
   if (splits < 1) splits = 1;
-  while (up(tiles, splits) > (int64_t(1) << 24)) ++splits;  // (ranges fit 31 bits)
+  while (up(tiles, splits) * vb > (int64_t(1) << 30)) ++splits;  // (ranges fit 31 bits)
   n.per = int32_t(up(tiles, splits) * vb);
   n.splits = int32_t(up(vocab, n.per));
   const int mb = 32 * groups(1, f32), bv = 4 * each;

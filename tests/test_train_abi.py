@@ -158,7 +158,8 @@ def test_scores_from_eight_bits_sizes():
 
 
 XENT = dict(rows=4, dim=64, vocab=1000, x_type=F32, x=FAKE, x_stride=64, table_type=F32, table=FAKE, table_stride=64,
-            labels=FAKE, scale=1.0, loss=FAKE, grad_x=FAKE, grad_x_stride=64, grad_table=FAKE, grad_table_stride=64)
+            labels=FAKE, scale=1.0, loss=FAKE, grad_x=FAKE + 4096, grad_x_stride=64, grad_table=FAKE + 8192,
+            grad_table_stride=64)
 
 
 @pytest.mark.parametrize("change", [
@@ -168,7 +169,7 @@ XENT = dict(rows=4, dim=64, vocab=1000, x_type=F32, x=FAKE, x_stride=64, table_t
     dict(x_stride=66), dict(table=None), dict(table=FAKE + 8), dict(table_stride=60), dict(table_stride=2 ** 19 + 4),
     dict(labels=None), dict(loss=None), dict(grad_x=FAKE + 4), dict(grad_x_stride=60), dict(grad_table=FAKE + 8),
     dict(grad_table_stride=65), dict(x_type=BF16, x=FAKE + 4), dict(rows=0, table=None),
-    dict(rows=0, grad_table=FAKE + 4)])
+    dict(rows=0, grad_table=FAKE + 4), dict(grad_table=FAKE), dict(grad_x=FAKE, grad_x_stride=68)])
 def test_xent_refusals(L, change):
     assert L.embbag_xent(packed(head._Xent, XENT, change), FAKE, 1 << 40, None, None) == BAD
 
