@@ -122,6 +122,8 @@ struct Eight<float> {
   __device__ __forceinline__ void values(float (&v)[8]) const {
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
   }
+  // What was made of the elements before is to be made again, not kept in registers.
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(a), "+v"(b)); }
 };
 template <>
 struct Eight<__bf16> {
@@ -136,6 +138,7 @@ struct Eight<__bf16> {
     }
   }
   __device__ __forceinline__ void values(float (&v)[8]) const { unpack16(w, v); }
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(w)); }
 };
 __device__ __forceinline__ float low() { return -__builtin_inff(); }
 

@@ -4,8 +4,10 @@
 // A row lives in the registers of T threads, 8 consecutive elements (a chunk) at a
 // time: every input is read once and every output written once.  The sum of
 // squares is FP64, so that it neither overflows nor loses small rows (an FP32 square does beyond
-// 1.8e19 and below 1e-23), and the factor 1/sqrt is a power of two and a rest: its exponent scales
-// the elements first, which is exact.
+// 1.8e19 and below 1e-23).  The forward's outputs are FP64 to their one rounding: an 8-bit code lies next to
+// a border of its rounding often enough that FP32's last bits move codes (16M elements: some tens, 2^-4
+// of the element each).  The gradient works in FP32, its factor 1/sqrt as a power of two and a rest: its
+// exponent scales the elements first, which is exact.
 #include <type_traits>
 
 #include "head.hpp"
@@ -27,6 +29,15 @@ __device__ __forceinline__ Inverse inverse_of(double sum, double per, double eps
   const float f = float(__builtin_amdgcn_frexp_mant(m));  // [0.5, 1)
   const int odd = e & 1;
   return {1.f / sqrtf(odd ? f + f : f), -((e - odd) / 2)};
+}
+// The same in FP64: a Newton step from FP32's 24 bits.
+__device__ __forceinline__ double inverse64_of(double sum, double per, double eps) {
+  const double m = sum * per + eps;
+  const int e = __builtin_amdgcn_frexp_exp(m);
+  const int odd = e & 1;
+  const double f = __builtin_amdgcn_frexp_mant(m) * (odd ? 2.0 : 1.0);
+  const double r = double(1.f / sqrtf(float(f)));
+  return m - m == 0.0 ? ldexp(r * fma(-0.5 * f * r, r, 1.5), -((e - odd) / 2)) : r;  // (0 of an infinity)
 }
 // x / sqrt(mean + eps).
 __device__ __forceinline__ float times(float x, const Inverse& s) { return ldexpf(x, s.exp) * s.rest; }
@@ -158,40 +169,52 @@ __global__ __launch_bounds__(kNormThreads<T>) void norm_rows(NormArgs a) {
     const int64_t row = row0 + threadIdx.x / T;
     const bool in = row < a.rows;
     const int last = in ? dim : 0;  // (the others of the wavefront need its lanes)
-    float h[NC][8];
+    Eight<TX> cx[NC];
+    Eight<TR> cr[NC];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) nx[i].values(h[i]);
-    if (a.residual != nullptr) {
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        float q[8];
-        nr[i].values(q);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[i][j] += q[j];
-      }
-    }
+    for (int i = 0; i < NC; ++i) cx[i] = nx[i], cr[i] = nr[i];
     if (row0 + int64_t(gridDim.x) * R < a.rows) fetch(row + int64_t(gridDim.x) * R);
+    auto sum_of = [&](int i, double (&h)[8]) {
+      float x[8], q[8];
+      cx[i].values(x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = double(x[j]);
+      if (a.residual == nullptr) return;
+      cr[i].values(q);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] += double(q[j]);
+    };
     double sum[1] = {0.0};
 #pragma unroll
-    for (int i = 0; i < NC; ++i)
+    for (int i = 0; i < NC; ++i) {
+      double h[8];
+      sum_of(i, h);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[0] = fma(double(h[i][j]), double(h[i][j]), sum[0]);
+      for (int j = 0; j < 8; ++j) sum[0] = fma(h[j], h[j], sum[0]);
+      if (a.sum_out != nullptr) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = float(h[j]);
+        store_chunk(static_cast<TR*>(a.sum_out) + (in ? row : 0) * a.sum_stride, t + i * T, last, v);
+      }
+    }
     row_sum<T, 1>(sum, slots[turn]);
     turn ^= 1;
-    const Inverse s = inverse_of(sum[0], a.per, a.eps);
-    if (a.sum_out != nullptr) {
-      TR* p = static_cast<TR*>(a.sum_out) + (in ? row : 0) * a.sum_stride;
+    const double s = inverse64_of(sum[0], a.per, a.eps);
+    float y[NC][8];
 #pragma unroll
-      for (int i = 0; i < NC; ++i) store_chunk(p, t + i * T, last, h[i]);
+    for (int i = 0; i < NC; ++i) {
+      double h[8];
+      cx[i].again();
+      if (a.residual != nullptr) cr[i].again();
+      sum_of(i, h);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[i][j] = float(h[j] * s * double(w[i][j]));
     }
-#pragma unroll
-    for (int i = 0; i < NC; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[i][j] = times(h[i][j], s) * w[i][j];
     if (a.out != nullptr) {
       TO* p = static_cast<TO*>(a.out) + (in ? row : 0) * a.out_stride;
 #pragma unroll
-      for (int i = 0; i < NC; ++i) store_chunk(p, t + i * T, last, h[i]);
+      for (int i = 0; i < NC; ++i) store_chunk(p, t + i * T, last, y[i]);
     }
     if (a.codes != nullptr) {
 #pragma unroll
@@ -199,10 +222,10 @@ __global__ __launch_bounds__(kNormThreads<T>) void norm_rows(NormArgs a) {
         const int c = t + i * T;
         if (c >= (dim + kChunk - 1) / kChunk) {  // (a NaN of the row makes NaN of zeros)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) h[i][j] = 0.f;
+          for (int j = 0; j < 8; ++j) y[i][j] = 0.f;
         }
         uint32_t byte;
-        const u2 codes = mx8_codes(h[i], &byte);
+        const u2 codes = mx8_codes(y[i], &byte);
         if (!in || c >= padded) continue;
         *reinterpret_cast<u2*>(a.codes + row * padded * kChunk + c * kChunk) = codes;
         if (c % 4 == 0) a.scales[row * (padded / 4) + c / 4] = uint8_t(byte);

@@ -101,6 +101,14 @@ __device__ __forceinline__ void d_terms(const f16v& d, int t, u4 (&out)[PD]) {
   }
 }
 
+// What the first term leaves of them, as BF16.
+__device__ __forceinline__ u4 second_term(const f16v& d, int t, const u4& term) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = d[t * 8 + i] - (i % 2 ? bf16_hi : bf16_lo)(term[i / 2]);
+  return pack16(v);
+}
+
 struct TokenArgs {
   const void* table;
   int64_t stride;
@@ -219,11 +227,13 @@ __device__ __forceinline__ void narrow_tokens(const TokenArgs& a, uint32_t block
       // The lane's columns: v + r0 + 8 q + 4 half + e.
       const int64_t first = v + r0 + half * 4;
       const bool whole = v + r0 + 32 <= v1;
+      bool labels = false;  // whether any of the wavefront's elements here is a label's
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         const int64_t place = label[i] - first;
         const bool mine = place >= 0 && place < 32 && place / 4 % 2 == 0 && label[i] < v1;
         const bool some = __builtin_amdgcn_ballot_w64(mine) != 0ull;
+        labels = labels || some;
         if constexpr (GRAD) {
           const float c = inv[i] * ratio[i];
 #pragma unroll
@@ -285,6 +295,16 @@ __device__ __forceinline__ void narrow_tokens(const TokenArgs& a, uint32_t block
 #pragma unroll
               for (int i = 0; i < TM; ++i)
                 dx[i][e] = mfma(f[first_of<P, PD>(k)], d[i][second_of<P, PD>(k)], dx[i][e]);
+          }
+          if (PD == 1 && labels) {  // a label's element is most of its row's gradient: its second term too
+#pragma unroll
+            for (int i = 0; i < TM; ++i) d[i][0] = second_term(z2[i], t, d[i][0]);
+#pragma unroll
+            for (int e = 0; e < EP / 32; ++e) {
+              const u4 f = L::turned(st, r0 + t * 16, e * 32, lane);
+#pragma unroll
+              for (int i = 0; i < TM; ++i) dx[i][e] = mfma(f, d[i][0], dx[i][e]);
+            }
           }
         }
       }
@@ -424,10 +444,10 @@ __device__ __forceinline__ void narrow_vocab(const VocabArgs& a, uint32_t block,
 #pragma unroll
         for (int p = 0; p < P; ++p) f[p] = L::rows(st + p * TILE, r0 + row, s, half);
 #pragma unroll
-        for (int k = 0; k < kPairs<P, 1>; ++k)
+        for (int k = 0; k < kPairs<P, 1>; ++k)  // (in narrow_tokens' order: the same scores bit by bit)
 #pragma unroll
           for (int i = 0; i < TV; ++i)
-            d[i] = mfma(f[first_of<P, 1>(k)], w[i][second_of<P, 1>(k)][s], d[i]);
+            d[i] = mfma(f[second_of<P, 1>(k)], w[i][first_of<P, 1>(k)][s], d[i]);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -442,6 +462,7 @@ __device__ __forceinline__ void narrow_vocab(const VocabArgs& a, uint32_t block,
       // The labels among the wavefront's rows of the table, one after the other.
       const int64_t off = rows.labels[cur][r0 + row] - v0;
       uint64_t some = __builtin_amdgcn_ballot_w64(half == 0 && off >= 0 && off < 32 * TV);
+      const bool labels = some != 0ull;
       while (some != 0ull) {
         const int k = __builtin_ctzll(some);
         some &= some - 1;
@@ -470,6 +491,16 @@ __device__ __forceinline__ void narrow_vocab(const VocabArgs& a, uint32_t block,
 #pragma unroll
             for (int i = 0; i < TV; ++i)
               dw[i][e] = mfma(f[first_of<P, PD>(k)], q[i][second_of<P, PD>(k)], dw[i][e]);
+        }
+        if (PD == 1 && labels) {  // (as in narrow_tokens)
+#pragma unroll
+          for (int i = 0; i < TV; ++i) q[i][0] = second_term(d[i], t, q[i][0]);
+#pragma unroll
+          for (int e = 0; e < EP / 32; ++e) {
+            const u4 f = L::turned(st, r0 + t * 16, e * 32, lane);
+#pragma unroll
+            for (int i = 0; i < TV; ++i) dw[i][e] = mfma(f, q[i][0], dw[i][e]);
+          }
         }
       }
     }
