@@ -60,6 +60,8 @@ struct Gemm {
   // `steps`.
   int32_t blocks;
   int64_t steps;
+  // With pairs == 2: the largest *live for which the second plane is read.
+  int32_t few;
 };
 
 // Pair number i: the planes of a and b.
@@ -190,12 +192,14 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
   uint8_t* scratch = lds + STAGES * STAGE + wave * Epi::template kScratch<TN, TM>;
 
   int64_t m_end = g.m, k_end = g.k;
+  int pairs = g.pairs;
   if (g.live != nullptr) {
     const int live = __builtin_amdgcn_readfirstlane(*g.live);
     if constexpr (LIVE_K)
       k_end = live;
     else
       m_end = live;
+    if (pairs == 2 && live > g.few) pairs = 1;
   }
   const uint32_t mtiles = LIVE_K ? mtiles_most : uint32_t((m_end + BM - 1) / BM);
   const uint32_t plain = mtiles * ntiles;
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
     uint32_t mt, nt;
     tile_at(ltile - z * plain, mtiles, ntiles, strip, &mt, &nt);
     int pa, pb;
-    planes_of(g.pairs, lpair, &pa, &pb);
+    planes_of(pairs, lpair, &pa, &pb);
     const int64_t k0 = int64_t(z) * sp.per * kStepK;
     sa.open(g.a, pa, int64_t(nt) * BN, g.n, k0, k_end, lane, wave);
     sb.open(g.b, pb, int64_t(mt) * BM, m_end, k0, k_end, lane, wave);
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
   // of loads on their way is always the same.
   auto next_load = [&]() {
     if (lstep == lsteps) {
-      if (++lpair == g.pairs) {
+      if (++lpair == pairs) {
         if (ltile + stride < end)
           lpair = 0, ltile += stride;
         else
@@ -323,7 +327,7 @@ __global__ __launch_bounds__(WN* WM* kWave, 1) void gemm_tiles(Gemm g, Epi epi, 
 #pragma unroll
       for (int j = 0; j < TM; ++j) acc[i][j] = f16v{};
     const uint32_t z = tile / plain;
-    const int steps = steps_of(z) * g.pairs;
+    const int steps = steps_of(z) * pairs;
     for (int step = 0; step < steps; ++step) {
       next_load();
       // This step is in LDS (the next STAGES - 2 may be on their way), and every wavefront holds the

@@ -13,7 +13,7 @@
 // All sums are in orders that the sizes determine; there are no atomics on them.
 //
 // BF16 operands are taken as they are.  D is rounded to BF16 (2^-8 of each element at most, as the
-// gradients' own rounding; two terms of it where rows are few and the products do not bound the call).
+// gradients' own rounding; two terms of it where few rows count and the products do not bound the call).
 // With the weights' ratio in D, equal weights leave the label's element, next to -1, almost exact.  FP32
 // operands, and D with them, are the sum of three BF16 terms, of whose nine products six are taken: what
 // is left out is below 2^-22 of each product.
@@ -23,6 +23,7 @@
 namespace embbag {
 namespace {
 
+constexpr int32_t kFew = 256;                          // rows whose D has two terms
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of D, of W's terms: a piece's
 constexpr int kRowsAtOnce = 4096;                     // rows whose places 1024 threads find in a round
 constexpr int64_t kMaxPitch = int64_t(1) << 19;       // elements of a row of D
@@ -335,6 +336,9 @@ struct GradEpi {
   const Token* tokens;
   float unit;
   int64_t first, columns;
+  // With two terms: the largest number of rows that count for which the second is stored.
+  const int32_t* live;
+  int32_t few;
   template <int TN, int TM>
   static constexpr int kScratch = 32 * kTurnPitch<__bf16, TN> * 2;
 
@@ -343,6 +347,7 @@ struct GradEpi {
                                              uint8_t* scratch) const {
     const int row = lane_id() % 32, half = lane_id() / 32;
     __bf16* turn = reinterpret_cast<__bf16*>(scratch);
+    const bool one = TERMS == 2 && scalar(*live) > few;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const int64_t at = m + j * 32 + row;
@@ -384,6 +389,7 @@ struct GradEpi {
             if (to < m_end && n + h * 32 + c < pitch)
               *reinterpret_cast<u4*>(d + k * plane + to * pitch + n + h * 32 + c) = v;
           });
+          if (one) break;
           if (k + 1 < TERMS) {
 #pragma unroll
             for (int i = 0; i < kTiles<__bf16, TN>; ++i)
@@ -539,6 +545,7 @@ struct Plan {
   bool f32;            // three terms of everything
   int terms;           // of D
   int pairs;           // of planes, in the gradients' products
+  int32_t few;         // of two terms the second is dropped where more rows count
   bool pack;           // whether W is packed
   int32_t padded;      // elements of a packed row
   int64_t piece;       // columns of the vocabulary at a time (a multiple of 256)
@@ -568,8 +575,13 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   Plan p = {};
   p.f32 = f32;
   const int planes = f32 ? 3 : 1;
-  // Few rows: the products' time is W's way from memory, and a second term of D costs little.
-  p.terms = f32 ? 3 : rows <= 256 ? 2 : 1;
+  // A second term of D where few rows count: the products' time is W's way from memory then, and the few
+  // roundings of labels' elements do not average out.  (Whether they do is known on the device; room for the
+  // term is taken where D is small.)  Over fewer than 1024 entries the element, 1 - p, is off by as much as p
+  // in the same direction in every row, and the term stays.
+  const bool small = vocab < 1024;
+  p.terms = f32 ? 3 : rows <= kFew || small || rows * vocab <= kPieceBytes / 2 ? 2 : 1;
+  p.few = small ? INT32_MAX : kFew;
   p.pairs = f32 ? 6 : p.terms;
   p.pack = f32 || dim % 8 != 0;
   p.padded = (dim + kStepK - 1) / kStepK * kStepK;
@@ -626,7 +638,7 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
     p.dx_splits = split_steps(tiles_of(p.dx, rows, dim), psteps, blocks_of(p.dx));
     const int64_t area = int64_t(blocks_of(p.dx)) * p.dx.bm * p.dx.bn, whole = int64_t(rows) * dim;
     p.dxp = take(size_t(area > whole ? area : whole) * 4);
-    p.dw = cheaper(p.piece, dim, up(rows, kStepK) * p.pairs, 8);
+    p.dw = cheaper(p.piece, dim, up(rows, kStepK) * (rows <= p.few ? p.pairs : 1), 8);
     p.dw_splits = split_steps(tiles_of(p.dw, p.piece, dim), up(rows, kStepK), blocks_of(p.dw));
     if (p.dw_splits.count > 1) p.dwp = take(size_t(p.dw_splits.count) * size_t(p.piece) * size_t(dim) * 4);
   }
@@ -705,7 +717,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     }
   };
   if (p.narrow) {
-    NarrowArgs q = {p.nar, p.terms, w, sizeof(TW) == 2, a.table_stride, xp, xplane, head, rows.tokens, rows.target,
+    NarrowArgs q = {p.nar, p.f32 ? 3 : N <= kFew ? 2 : 1, w, sizeof(TW) == 2, a.table_stride, xp, xplane, head, rows.tokens, rows.target,
                     unit, parts, dxp, dw, sizeof(TW) == 2, a.grad_table_stride, &head->factor_w};
     hipError_t e = launch_narrow_scores(q, st);
     if (e != hipSuccess) return e;
@@ -738,7 +750,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   const Shape ss = p.scores;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
-    const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0};
+    const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0, 0};
     run_gemm<false, false, false>(
         g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n}, ss, st);
     join_sums(int32_t(up(n, ss.part())), v0 == 0, v0 + n == V);
@@ -750,10 +762,10 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
     const Side wsd = side_w(v0, n);
-    const Gemm g = {wsd, xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0};
+    const Gemm g = {wsd, xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0, 0};
     auto grad = [&](auto terms) {
       run_gemm<false, false, false>(
-          g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, unit, v0, n}, ss, st);
+          g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, unit, v0, n, &head->live, p.few}, ss, st);
     };
     if constexpr (TERMS == 3)
       grad(std::integral_constant<int, 3>());
@@ -762,11 +774,11 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     else
       grad(std::integral_constant<int, 1>());
     if (dx != nullptr) {
-      const Gemm gx = {wsd, ds, E, N, n, &head->live, p.pairs, p.dx_splits, blocks_of(p.dx), up(p.piece, kStepK)};
+      const Gemm gx = {wsd, ds, E, N, n, &head->live, p.pairs, p.dx_splits, blocks_of(p.dx), up(p.piece, kStepK), p.few};
       run_gemm<true, false, false>(gx, StoreEpi<float>{dxp, E, E, nullptr, -1, v0 > 0}, p.dx, st);
     }
     if (dw != nullptr) {
-      const Gemm gw = {xs, ds, E, n, N, &head->live, p.pairs, p.dw_splits, 0, 0};
+      const Gemm gw = {xs, ds, E, n, N, &head->live, p.pairs, p.dw_splits, 0, 0, p.few};
       const Shape sw = p.dw;
       TW* to = dw + v0 * a.grad_table_stride;
       if (p.dw_splits.count == 1) {
