@@ -19,6 +19,7 @@
 // is left out is below 2^-22 of each product.
 #include "gemm.hpp"
 #include "xent.hpp"
+#include "xent_few.hpp"
 
 namespace embbag {
 namespace {
@@ -547,12 +548,14 @@ struct Plan {
   int pairs;           // of planes, in the gradients' products
   int32_t few;         // of two terms the second is dropped where more rows count
   bool pack;           // whether W is packed
+  bool few_wide;       // the products of xent_few.hpp
   int32_t padded;      // elements of a packed row
   int64_t piece;       // columns of the vocabulary at a time (a multiple of 256)
   Shape scores, dx, dw;
   Splits dx_splits, dw_splits;
+  int32_t few_parts;   // of dx, with few_wide
   // Workspace.
-  size_t place, row, tokens, target, x, parts, w, d, dxp, dwp, total;
+  size_t place, row, tokens, target, x, parts, xf, z, df, w, d, dxp, dwp, total;
 };
 
 // Tiles of 256 x 256 (one block per compute unit) or 128 x 128 (two, of which one's products run while the
@@ -583,7 +586,10 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   p.terms = f32 ? 3 : rows <= kFew || small || rows * vocab <= kPieceBytes / 2 ? 2 : 1;
   p.few = small ? INT32_MAX : kFew;
   p.pairs = f32 ? 6 : p.terms;
-  p.pack = f32 || dim % 8 != 0;
+  p.narrow = dim <= kNarrow;
+  p.few_wide = f32 && !p.narrow && few_wide(rows, dim) && vocab <= kMaxPitch &&
+               (!backward || rows * up(vocab, 256) * 256 * 6 <= kPieceBytes * 2);
+  p.pack = (f32 || dim % 8 != 0) && !p.few_wide;
   p.padded = (dim + kStepK - 1) / kStepK * kStepK;
   size_t at = 256;
   auto take = [&](size_t bytes) {
@@ -595,7 +601,6 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   p.row = take(size_t(rows) * 4);
   p.tokens = take(size_t(rows) * sizeof(Token));
   p.target = take(size_t(rows) * 4);
-  p.narrow = dim <= kNarrow;
   if (p.narrow) {
     p.padded = dim <= 64 ? 64 : 128;
     p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
@@ -623,7 +628,14 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
   const int64_t steps = up(dim, kStepK);
   p.scores = rows <= 64 ? few_rows(rows) : cheaper(rows, p.piece, steps * (f32 ? 6 : 1), 16);
-  p.parts = take(size_t(up(p.piece, p.scores.part())) * size_t(rows) * sizeof(float2));
+  p.parts = take(size_t(up(p.piece, p.few_wide ? 32 : p.scores.part())) * size_t(rows) * sizeof(float2));
+  if (p.few_wide) {
+    p.xf = take(size_t(up(rows, 32) * 32) * size_t(p.padded) * 6);
+    if (backward) {
+      p.z = take(size_t(rows) * size_t(p.piece) * 4);
+      p.df = take(size_t(up(rows, 32) * 32) * size_t(p.piece) * 6);
+    }
+  }
   p.w = p.pack ? take(size_t(p.piece) * size_t(p.padded) * 2 * planes) : 0;
   if (backward) {
     p.d = take(size_t(rows) * size_t(p.piece) * 2 * p.terms);
@@ -637,7 +649,8 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
       p.dx = {128, 128};
     p.dx_splits = split_steps(tiles_of(p.dx, rows, dim), psteps, blocks_of(p.dx));
     const int64_t area = int64_t(blocks_of(p.dx)) * p.dx.bm * p.dx.bn, whole = int64_t(rows) * dim;
-    p.dxp = take(size_t(area > whole ? area : whole) * 4);
+    p.few_parts = p.few_wide ? few_parts(rows, vocab, dim) : 0;
+    p.dxp = take(size_t(p.few_wide ? whole * p.few_parts : area > whole ? area : whole) * 4);
     p.dw = cheaper(p.piece, dim, up(rows, kStepK) * (rows <= p.few ? p.pairs : 1), 8);
     p.dw_splits = split_steps(tiles_of(p.dw, p.piece, dim), up(rows, kStepK), blocks_of(p.dw));
     if (p.dw_splits.count > 1) p.dwp = take(size_t(p.dw_splits.count) * size_t(p.piece) * size_t(dim) * 4);
@@ -746,6 +759,43 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     }
     return Side{wp, xpitch, wplane * 2};
   };
+  const int64_t dplane = int64_t(N) * p.piece;
+  const Side ds = {d, p.piece * 2, dplane * 2};
+  auto product_dw = [&](int64_t v0, int64_t n) {
+    const Gemm g = {xs, ds, E, n, N, &head->live, p.pairs, p.dw_splits, 0, 0, p.few};
+    TW* to = dw + v0 * a.grad_table_stride;
+    if (p.dw_splits.count == 1) {
+      run_gemm<true, true, true>(g, StoreEpi<TW>{to, a.grad_table_stride, E, &head->factor_w, 0, false}, p.dw, st);
+    } else {
+      float* dwp = reinterpret_cast<float*>(ws + p.dwp);
+      run_gemm<true, true, true>(g, StoreEpi<float>{dwp, E, E, nullptr, p.piece * E, false}, p.dw, st);
+      join_dw(dwp, p.dw_splits.count, p.piece * E, n, to);
+    }
+  };
+  if constexpr (TERMS == 3) {
+    if (p.few_wide) {
+      const bool back = dx != nullptr || dw != nullptr;
+      float* z = back ? reinterpret_cast<float*>(ws + p.z) : nullptr;
+      const int32_t tiles = int32_t(up(N, 32));
+      const Fragments xf = {reinterpret_cast<__bf16*>(ws + p.xf), tiles};
+      const Fragments df = {dx != nullptr ? reinterpret_cast<__bf16*>(ws + p.df) : nullptr, tiles};
+      hipLaunchKernelGGL(few_x, dim3(unsigned(up(p.padded / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, xp, xplane,
+                         p.padded, &head->live, xf);
+      launch_few_scores(w, a.table_stride, V, E, N, xf, &head->live, z, p.piece,
+                        StatsEpi{parts, N, rows.tokens, rows.target, unit, 0, V}, st);
+      join_sums(int32_t(up(V, 32)), true, true);
+      if (!back) return hipGetLastError();
+      hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, z, p.piece,
+                         V, rows.tokens, unit, &head->live, dw != nullptr ? d : nullptr, dplane, df);
+      if (dx != nullptr) {
+        launch_few_dx(w, a.table_stride, V, E, N, df, &head->live, p.few_parts, dxp,
+                      int64_t(N) * E, st);
+        join_dx({p.few_parts, int64_t(N) * E, 0, 0, 0, 0});
+      }
+      if (dw != nullptr) product_dw(0, V);
+      return hipGetLastError();
+    }
+  }
   const int32_t pairs = TERMS == 3 ? 6 : 1;
   const Shape ss = p.scores;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
@@ -757,8 +807,6 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   }
   if (dx == nullptr && dw == nullptr) return hipGetLastError();
 
-  const int64_t dplane = int64_t(N) * p.piece;
-  const Side ds = {d, p.piece * 2, dplane * 2};
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
     const Side wsd = side_w(v0, n);
@@ -777,18 +825,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       const Gemm gx = {wsd, ds, E, N, n, &head->live, p.pairs, p.dx_splits, blocks_of(p.dx), up(p.piece, kStepK), p.few};
       run_gemm<true, false, false>(gx, StoreEpi<float>{dxp, E, E, nullptr, -1, v0 > 0}, p.dx, st);
     }
-    if (dw != nullptr) {
-      const Gemm gw = {xs, ds, E, n, N, &head->live, p.pairs, p.dw_splits, 0, 0, p.few};
-      const Shape sw = p.dw;
-      TW* to = dw + v0 * a.grad_table_stride;
-      if (p.dw_splits.count == 1) {
-        run_gemm<true, true, true>(gw, StoreEpi<TW>{to, a.grad_table_stride, E, &head->factor_w, 0, false}, sw, st);
-      } else {
-        float* dwp = reinterpret_cast<float*>(ws + p.dwp);
-        run_gemm<true, true, true>(gw, StoreEpi<float>{dwp, E, E, nullptr, p.piece * E, false}, sw, st);
-        join_dw(dwp, p.dw_splits.count, p.piece * E, n, to);
-      }
-    }
+    if (dw != nullptr) product_dw(v0, n);
   }
   if (dx != nullptr)
     join_dx({p.dx_splits.count, 0, blocks_of(p.dx), p.dx.bm, int32_t(up(E, p.dx.bn)), up(p.piece, kStepK)});
