@@ -17,6 +17,11 @@
 // With the weights' ratio in D, equal weights leave the label's element, next to -1, almost exact.  FP32
 // operands, and D with them, are the sum of three BF16 terms, of whose nine products six are taken: what
 // is left out is below 2^-22 of each product.
+//
+// Four products, 8 N V E operations, where 6 N V E would do if the scores were kept: at 4096 x 131072 x 2048
+// they would be 2.1 GB written and read in FP32.  Bound by the products, with few rows by W's bytes.  Measured, us:
+// 4096 x 131072 x 2048 BF16 7020, 1999 x 50001 x 300 279, 1 x 200003 x 1024 without gradients 85 (410 MB at 4.8
+// TB/s).
 #include "gemm.hpp"
 #include "xent.hpp"
 #include "xent_few.hpp"
@@ -204,6 +209,8 @@ struct StatsEpi {
   float unit;
   int64_t first;         // the piece's first column
   int64_t columns;       // of the piece
+  float* scores;         // [live][scores_pitch]; null: not kept
+  int64_t scores_pitch;
   template <int TN, int TM>
   static constexpr int kScratch = 0;
 
@@ -215,6 +222,17 @@ struct StatsEpi {
     for (int j = 0; j < TM; ++j) {
       const int64_t at = m + j * 32 + row;
       const bool in = at < m_end;
+      if (scores != nullptr && in) {
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int64_t c = n + i * 32 + q * 8 + half * 4;
+            if (c < scores_pitch)
+              store4(scores + at * scores_pitch + c,
+                     f4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+          }
+      }
       if (n + 32 * TN > columns) {
         const int64_t left = columns - n - half * 4;
 #pragma unroll
@@ -512,8 +530,9 @@ __global__ __launch_bounds__(kBlock) void xent_join_parts(const float* __restric
 // Slices where the parts are many: their loads are a chain otherwise (33 rows of 128 from 250 parts: 18 us
 // with one).
 template <class T>
-void launch_join_parts(const float* parts, const PartCount& pc, const int32_t* live, int64_t rows, int32_t dim, const int32_t* map, const float* factor, T* out, int64_t pitch,
-                       int64_t row0, hipStream_t st) {
+void launch_join_parts(const float* parts, const PartCount& pc, const int32_t* live, int64_t rows, int32_t dim,
+                       const int32_t* map, const float* factor, T* out, int64_t pitch, int64_t row0,
+                       hipStream_t st) {
   const int64_t n = (rows - row0) * (dim / 4);
   const FastDiv d = fast_div(uint32_t(dim / 4));
   auto run = [&](auto slices) {
@@ -549,6 +568,7 @@ struct Plan {
   int32_t few;         // of two terms the second is dropped where more rows count
   bool pack;           // whether W is packed
   bool few_wide;       // the products of xent_few.hpp
+  bool keep;           // whether the scores stay in the workspace
   int32_t padded;      // elements of a packed row
   int64_t piece;       // columns of the vocabulary at a time (a multiple of 256)
   Shape scores, dx, dw;
@@ -637,6 +657,10 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
     }
   }
   p.w = p.pack ? take(size_t(p.piece) * size_t(p.padded) * 2 * planes) : 0;
+  // Six pairs of planes' products again cost more than the scores' way through memory, where they fit.  KEEPFIG
+  p.keep = f32 && backward && !p.few_wide && dim >= 192 && pieces == 1 && rows > 0 && rows <= 65535 &&
+           rows * p.piece * 4 <= kPieceBytes * 2;
+  if (p.keep) p.z = take(size_t(rows) * size_t(p.piece) * 4);
   if (backward) {
     p.d = take(size_t(rows) * size_t(p.piece) * 2 * p.terms);
     // dx: the larger tiles where they, split, leave few compute units idle.
@@ -730,7 +754,8 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     }
   };
   if (p.narrow) {
-    NarrowArgs q = {p.nar, p.f32 ? 3 : N <= kFew ? 2 : 1, w, sizeof(TW) == 2, a.table_stride, xp, xplane, head, rows.tokens, rows.target,
+    NarrowArgs q = {p.nar, p.f32 ? 3 : N <= kFew ? 2 : 1, w, sizeof(TW) == 2, a.table_stride, xp, xplane, head,
+                    rows.tokens, rows.target,
                     unit, parts, dxp, dw, sizeof(TW) == 2, a.grad_table_stride, &head->factor_w};
     hipError_t e = launch_narrow_scores(q, st);
     if (e != hipSuccess) return e;
@@ -782,7 +807,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       hipLaunchKernelGGL(few_x, dim3(unsigned(up(p.padded / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, xp, xplane,
                          p.padded, &head->live, xf);
       launch_few_scores(w, a.table_stride, V, E, N, xf, &head->live, z, p.piece,
-                        StatsEpi{parts, N, rows.tokens, rows.target, unit, 0, V}, st);
+                        StatsEpi{parts, N, rows.tokens, rows.target, unit, 0, V, nullptr, 0}, st);
       join_sums(int32_t(up(V, 32)), true, true);
       if (!back) return hipGetLastError();
       hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, z, p.piece,
@@ -798,11 +823,12 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   }
   const int32_t pairs = TERMS == 3 ? 6 : 1;
   const Shape ss = p.scores;
+  float* kept = p.keep && (dx != nullptr || dw != nullptr) ? reinterpret_cast<float*>(ws + p.z) : nullptr;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
     const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0, 0};
     run_gemm<false, false, false>(
-        g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n}, ss, st);
+        g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n, kept, p.piece}, ss, st);
     join_sums(int32_t(up(n, ss.part())), v0 == 0, v0 + n == V);
   }
   if (dx == nullptr && dw == nullptr) return hipGetLastError();
@@ -815,7 +841,10 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       run_gemm<false, false, false>(
           g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, unit, v0, n, &head->live, p.few}, ss, st);
     };
-    if constexpr (TERMS == 3)
+    if (kept != nullptr)
+      hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, kept,
+                         p.piece, V, rows.tokens, unit, &head->live, d, dplane, Fragments{nullptr, 0});
+    else if constexpr (TERMS == 3)
       grad(std::integral_constant<int, 3>());
     else if (p.terms == 2)
       grad(std::integral_constant<int, 2>());

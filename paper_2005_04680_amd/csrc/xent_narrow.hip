@@ -14,6 +14,9 @@
 //
 // Streaming tiles are double-buffered: the next one's elements are on their way in registers while this
 // one's products run, and are split into their BF16 terms on the way to LDS.
+//
+// Bound by matrix and vector instructions, each about half of the cycles (exponentials, D's terms and their
+// packing beside the products).  Measured, us: FP32 2048 x 100003 x 64 672, 33 x 32001 x 128 57.
 #include <type_traits>
 
 #include "xent.hpp"
