@@ -16,7 +16,8 @@
 // gradients' own rounding; two terms of it where few rows count and the products do not bound the call).
 // With the weights' ratio in D, equal weights leave the label's element, next to -1, almost exact.  FP32
 // operands, and D with them, are the sum of three BF16 terms, of whose nine products six are taken: what
-// is left out is below 2^-22 of each product.
+// is left out is below 2^-22 of each product.  Their scores, six times a BF16 one's work, are kept in FP32 instead of
+// computed again where they fit in 512 MB, and D is made of them.
 //
 // Four products, 8 N V E operations, where 6 N V E would do if the scores were kept: at 4096 x 131072 x 2048
 // they would be 2.1 GB written and read in FP32.  Bound by the products, with few rows by W's bytes.  Measured, us:
@@ -201,6 +202,7 @@ __global__ __launch_bounds__(kBlock) void xent_pack_w(const T* __restrict__ w, i
 
 // A tile's parts: of each row and the wavefront's 32 TN columns the exponent of the largest score, rounded,
 // and the sum of the exponentials beside exactly that.
+template <bool KEEP>
 struct StatsEpi {
   float2* parts;         // [the piece's columns / (32 TN)][pitch]
   int64_t pitch;
@@ -209,7 +211,7 @@ struct StatsEpi {
   float unit;
   int64_t first;         // the piece's first column
   int64_t columns;       // of the piece
-  float* scores;         // [live][scores_pitch]; null: not kept
+  float* scores;         // [live][scores_pitch], with KEEP
   int64_t scores_pitch;
   template <int TN, int TM>
   static constexpr int kScratch = 0;
@@ -218,21 +220,27 @@ struct StatsEpi {
   __device__ __forceinline__ void operator()(f16v (&acc)[TN][TM], int64_t n, int64_t m, int64_t m_end, int,
                                              uint8_t*) const {
     const int row = lane_id() % 32, half = lane_id() / 32;
+    if constexpr (KEEP) {
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int64_t at = m + j * 32 + row;
-      const bool in = at < m_end;
-      if (scores != nullptr && in) {
+      for (int j = 0; j < TM; ++j) {
+        const int64_t at = m + j * 32 + row;
+        float* to = scores + at * scores_pitch + n + half * 4;
+        const int64_t left = at < m_end ? scores_pitch - n - half * 4 : 0;
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const int64_t c = n + i * 32 + q * 8 + half * 4;
-            if (c < scores_pitch)
-              store4(scores + at * scores_pitch + c,
-                     f4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+            const int c = i * 32 + q * 8;
+            if (c < left)
+              store4(to + c, f4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
           }
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int64_t at = m + j * 32 + row;
+      const bool in = at < m_end;
       if (n + 32 * TN > columns) {
         const int64_t left = columns - n - half * 4;
 #pragma unroll
@@ -657,7 +665,8 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
     }
   }
   p.w = p.pack ? take(size_t(p.piece) * size_t(p.padded) * 2 * planes) : 0;
-  // Six pairs of planes' products again cost more than the scores' way through memory, where they fit.  KEEPFIG
+  // Six pairs of planes' products again cost more than the scores' way through memory, where they fit: us, again /
+  // kept, 1411 x 3929 x 2664 965 / 707, 3615 x 6188 x 724 1030 / 819, 2000 x 20000 x 512 1101 / 1012, x 196 619 / 597.
   p.keep = f32 && backward && !p.few_wide && dim >= 192 && pieces == 1 && rows > 0 && rows <= 65535 &&
            rows * p.piece * 4 <= kPieceBytes * 2;
   if (p.keep) p.z = take(size_t(rows) * size_t(p.piece) * 4);
@@ -807,7 +816,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       hipLaunchKernelGGL(few_x, dim3(unsigned(up(p.padded / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, xp, xplane,
                          p.padded, &head->live, xf);
       launch_few_scores(w, a.table_stride, V, E, N, xf, &head->live, z, p.piece,
-                        StatsEpi{parts, N, rows.tokens, rows.target, unit, 0, V, nullptr, 0}, st);
+                        StatsEpi<false>{parts, N, rows.tokens, rows.target, unit, 0, V, nullptr, 0}, st);
       join_sums(int32_t(up(V, 32)), true, true);
       if (!back) return hipGetLastError();
       hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, z, p.piece,
@@ -827,8 +836,18 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
     const Gemm g = {side_w(v0, n), xs, n, N, E, &head->live, pairs, {1, int32_t(up(E, kStepK))}, 0, 0, 0};
-    run_gemm<false, false, false>(
-        g, StatsEpi{parts, N, rows.tokens, rows.target, unit, v0, n, kept, p.piece}, ss, st);
+    auto stats = [&](auto keep) {
+      run_gemm<false, false, false>(
+          g, StatsEpi<keep.value>{parts, N, rows.tokens, rows.target, unit, v0, n, kept, p.piece}, ss, st);
+    };
+    if constexpr (TERMS == 3) {
+      if (kept != nullptr)
+        stats(std::true_type());
+      else
+        stats(std::false_type());
+    } else {
+      stats(std::false_type());
+    }
     join_sums(int32_t(up(n, ss.part())), v0 == 0, v0 + n == V);
   }
   if (dx == nullptr && dw == nullptr) return hipGetLastError();

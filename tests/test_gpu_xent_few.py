@@ -1,5 +1,5 @@
-"""Cross entropy of few rows over a wide table in FP32, whose products read the table as it stands: at the
-edges of its tiles (32 and 128 rows, 32 rows of the table, 32 and 128 elements of a row), within the bounds that
+"""Cross entropy of few rows over a wide table in FP32, whose products read the table as it stands, and of more
+rows, whose scores are kept (300 rows of 260 and the like): at the edges of the tiles (32 and 128 rows, 32 rows of the table, 32 and 128 elements of a row), within the bounds that
 count the roundings."""
 import pytest
 import torch
@@ -20,7 +20,7 @@ def _gpu():
 @pytest.mark.parametrize("N,V,E", [(1, 1, 132), (1, 2000, 132), (2, 31, 136), (31, 33, 160), (32, 255, 164), (33, 1000, 132),
                                    (64, 257, 256), (65, 100, 260), (128, 513, 388), (129, 1003, 516), (257, 64, 516),
                                    (300, 1500, 700), (512, 700, 1028), (513, 700, 1028), (194, 300, 260),
-                                   (195, 300, 260)])
+                                   (195, 300, 260), (300, 257, 192), (1000, 1003, 204), (700, 40, 1500)])
 def test_sizes(N, V, E, tx, tw):
     check(N, V, E, N + V + E, tx, tw, ignored=0.2 if N > 2 else 0.0)
 
@@ -32,12 +32,12 @@ def test_weights_and_scale(N, V, E, scale):
 
 
 @pytest.mark.parametrize("N,V,E,t", [(7, 100003, 132, "f32"), (128, 524288, 132, "bf16"), (3, 524289, 132, "f32"),
-                                     (200, 20011, 1500, "f32")])
+                                     (200, 20011, 1500, "f32"), (1500, 30001, 260, "f32"), (600, 250001, 196, "f32")])
 def test_large(N, V, E, t):
     check(N, V, E, N, "f32", t, sure=4.0)
 
 
-@pytest.mark.parametrize("N", [5, 70, 150])
+@pytest.mark.parametrize("N", [5, 70, 150, 300])
 def test_rows_left_out_may_hold_anything(N):
     x, w, labels = inputs(N, 700, 260, 3, "f32", "f32", ignored=0.3)
     weights = torch.full((N,), 0.25, device=DEV)
@@ -52,7 +52,7 @@ def test_rows_left_out_may_hold_anything(N):
         close(g, e, what)
 
 
-@pytest.mark.parametrize("N", [1, 40, 190])
+@pytest.mark.parametrize("N", [1, 40, 190, 300])
 def test_no_row_counts(N):
     x, w, labels = inputs(N, 700, 260, 3, "f32", "f32")
     labels.fill_(-1)
@@ -60,7 +60,7 @@ def test_no_row_counts(N):
         assert (g == 0).all()
 
 
-@pytest.mark.parametrize("N,tx,tw", [(5, "f32", "f32"), (70, "f32", "bf16"), (130, "bf16", "f32")])
+@pytest.mark.parametrize("N,tx,tw", [(5, "f32", "f32"), (70, "f32", "bf16"), (130, "bf16", "f32"), (300, "f32", "f32")])
 def test_strides(N, tx, tw):
     x, w, labels = inputs(N, 1000, 260, 8, tx, tw)
     want = run(x, w, labels)
@@ -76,7 +76,7 @@ def test_strides(N, tx, tw):
         assert torch.equal(run(xs, ws, labels, grads=(xs, None))[1], want[1])
 
 
-@pytest.mark.parametrize("N", [1, 70, 190])
+@pytest.mark.parametrize("N", [1, 70, 190, 300])
 def test_each_output_alone_and_again(N):
     x, w, labels = inputs(N, 1000, 260, 9, "f32", "f32")
     loss, dx, dw = run(x, w, labels)
@@ -87,7 +87,7 @@ def test_each_output_alone_and_again(N):
     assert torch.equal(run(x, w, labels, dx=False)[2], dw)
 
 
-@pytest.mark.parametrize("N", [3, 70])
+@pytest.mark.parametrize("N", [3, 70, 300])
 def test_a_row_with_nan_or_infinity_keeps_it(N):
     """The other rows' losses and gradients are the same bits; the table's gradient takes the row's NaN."""
     x, w, labels = inputs(N, 500, 260, 5, "f32", "f32", ignored=0.0)
