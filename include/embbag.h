@@ -567,8 +567,8 @@ typedef struct {
 
 int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStream_t stream);
 
-/* Softmax cross entropy of the scores over a table, without keeping the scores, with
- * the gradients of both of their sides.  With z[r][v] = scale * sum over e of
+/* Softmax cross entropy of the scores over a table, without keeping the scores where they
+ * are large, with the gradients of both of their sides.  With z[r][v] = scale * sum over e of
  * x[r][e] * table[v][e] and q = softmax(z[r]) over the vocabulary, for every row r:
  *   loss[r] = w * (log(sum over v of exp z[r][v]) - z[r][labels[r]]),
  *   grad_x[r] = scale * w * sum over v of (q[v] - [v == labels[r]]) * table[v],
@@ -584,11 +584,11 @@ int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStr
  * grad_x may be x itself with the same stride.  A label >= vocab is a data error; its row
  * is left out then.  Scores and sums are FP32.  BF16 sides: q - [v == label], times w
  * over the largest weight, is rounded to BF16 (two terms of it where at most 256 rows
- * count, or over small tables) for the gradients' products.  If either side is FP32 both enter with 24 bits.  An infinity in a
- * row of either side makes its scores infinite or NaN.
+ * count, or over small tables) for the gradients' products.  If either side is FP32 both
+ * enter with 24 bits.  An infinity in a row of either side makes its scores infinite or NaN.
  * `workspace`: 256-byte aligned; `type` is EMBBAG_F32 if either side is FP32, `backward`
  * whether a gradient is wanted.  It holds a piece of the vocabulary's q at a time (at most
- * about 512 MB of it, or 256 columns). */
+ * about 512 MB of it, or 256 columns; twice that and the scores of few or FP32 rows). */
 typedef struct {
   int32_t rows;
   int32_t dim;

@@ -1,5 +1,5 @@
 // Softmax cross entropy of the scores over a table, with the gradients of the scores' inputs and
-// of the table; the scores are never kept.
+// of the table; the scores are kept only where they are small.
 //
 // z = scale x W^T, loss = w (log sum exp z - z[label]), D = softmax(z) - onehot(label):
 //   dx = scale w D W,   dW = scale (w D)^T x.
@@ -16,8 +16,8 @@
 // gradients' own rounding; two terms of it where few rows count and the products do not bound the call).
 // With the weights' ratio in D, equal weights leave the label's element, next to -1, almost exact.  FP32
 // operands, and D with them, are the sum of three BF16 terms, of whose nine products six are taken: what
-// is left out is below 2^-22 of each product.  Their scores, six times a BF16 one's work, are kept in FP32 instead of
-// computed again where they fit in 512 MB, and D is made of them.
+// is left out is below 2^-22 of each product.  Where scores cost more to compute again than to keep (FP32 sides,
+// few rows) and fit in 512 MB, they stay in FP32 and D is made of them.
 //
 // Four products, 8 N V E operations, where 6 N V E would do if the scores were kept: at 4096 x 131072 x 2048
 // they would be 2.1 GB written and read in FP32.  Bound by the products, with few rows by W's bytes.  Measured, us:
@@ -667,8 +667,10 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   p.w = p.pack ? take(size_t(p.piece) * size_t(p.padded) * 2 * planes) : 0;
   // Six pairs of planes' products again cost more than the scores' way through memory, where they fit: us, again /
   // kept, 1411 x 3929 x 2664 965 / 707, 3615 x 6188 x 724 1030 / 819, 2000 x 20000 x 512 1101 / 1012, x 196 619 / 597.
-  p.keep = f32 && backward && !p.few_wide && dim >= 192 && pieces == 1 && rows > 0 && rows <= 65535 &&
-           rows * p.piece * 4 <= kPieceBytes * 2;
+  // Of BF16 rows that are few beside dim, W's bytes once more do: 16 x 100000 x 512 130 / 114, 100 x 50000 x 1024
+  // 164 / 147, 123 x 84048 x 492 209 / 197, 33 x 32001 x 136 45.8 / 45.6.
+  p.keep = backward && !p.few_wide && pieces == 1 && rows > 0 && rows <= 65535 &&
+           rows * p.piece * 4 <= kPieceBytes * 2 && (f32 ? dim >= 192 : rows <= kFew && rows <= dim / 4);
   if (p.keep) p.z = take(size_t(rows) * size_t(p.piece) * 4);
   if (backward) {
     p.d = take(size_t(rows) * size_t(p.piece) * 2 * p.terms);
@@ -820,7 +822,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       join_sums(int32_t(up(V, 32)), true, true);
       if (!back) return hipGetLastError();
       hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, z, p.piece,
-                         V, rows.tokens, unit, &head->live, dw != nullptr ? d : nullptr, dplane, df);
+                         V, rows.tokens, unit, &head->live, dw != nullptr ? d : nullptr, dplane, 3, df);
       if (dx != nullptr) {
         launch_few_dx(w, a.table_stride, V, E, N, df, &head->live, p.few_parts, dxp,
                       int64_t(N) * E, st);
@@ -840,14 +842,10 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       run_gemm<false, false, false>(
           g, StatsEpi<keep.value>{parts, N, rows.tokens, rows.target, unit, v0, n, kept, p.piece}, ss, st);
     };
-    if constexpr (TERMS == 3) {
-      if (kept != nullptr)
-        stats(std::true_type());
-      else
-        stats(std::false_type());
-    } else {
+    if (kept != nullptr)
+      stats(std::true_type());
+    else
       stats(std::false_type());
-    }
     join_sums(int32_t(up(n, ss.part())), v0 == 0, v0 + n == V);
   }
   if (dx == nullptr && dw == nullptr) return hipGetLastError();
@@ -862,7 +860,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     };
     if (kept != nullptr)
       hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, kept,
-                         p.piece, V, rows.tokens, unit, &head->live, d, dplane, Fragments{nullptr, 0});
+                         p.piece, V, rows.tokens, unit, &head->live, d, dplane, p.terms, Fragments{nullptr, 0});
     else if constexpr (TERMS == 3)
       grad(std::integral_constant<int, 3>());
     else if (p.terms == 2)

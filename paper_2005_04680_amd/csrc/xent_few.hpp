@@ -162,11 +162,11 @@ __global__ __launch_bounds__(kBlock) void few_scores(const TW* __restrict__ w, i
 }
 
 // D of the rows that count, in three terms, from their scores: 8 columns per thread, zeros past the table.  In
-// planes for dW's product (`d` not null), in fragments for dx's.
+// fragments for dx's product above (`f` not empty); `planes` planes of it for the tiles' (`d` not null).
 __global__ __launch_bounds__(kBlock) void few_d(const float* __restrict__ scores, int64_t pitch, int64_t vocab,
                                                 const Token* __restrict__ tokens, float unit,
                                                 const int32_t* __restrict__ rows, __bf16* __restrict__ d,
-                                                int64_t plane, Fragments f) {
+                                                int64_t plane, int planes, Fragments f) {
   const int at = blockIdx.y;
   const int64_t n = (int64_t(blockIdx.x) * kBlock + threadIdx.x) * 8;
   if (at >= *rows || n >= pitch) return;
@@ -184,7 +184,8 @@ __global__ __launch_bounds__(kBlock) void few_d(const float* __restrict__ scores
   if (f.data != nullptr) f.store(n, at, terms);
   if (d == nullptr) return;
 #pragma unroll
-  for (int k = 0; k < 3; ++k) *reinterpret_cast<u4*>(d + k * plane + at * pitch + n) = terms[k];
+  for (int k = 0; k < 3; ++k)
+    if (k < planes) *reinterpret_cast<u4*>(d + k * plane + at * pitch + n) = terms[k];
 }
 
 // N elements of a row.
