@@ -669,7 +669,7 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   // kept, 1411 x 3929 x 2664 965 / 707, 3615 x 6188 x 724 1030 / 819, 2000 x 20000 x 512 1101 / 1012, x 196 619 / 597.
   // Of BF16 rows that are few beside dim, W's bytes once more do: 16 x 100000 x 512 130 / 114, 100 x 50000 x 1024
   // 164 / 147, 123 x 84048 x 492 209 / 197, 33 x 32001 x 136 45.8 / 45.6.
-  p.keep = backward && !p.few_wide && pieces == 1 && rows > 0 && rows <= 65535 &&
+  p.keep = backward && !p.few_wide && pieces == 1 && rows > 0 &&
            rows * p.piece * 4 <= kPieceBytes * 2 && (f32 ? dim >= 192 : rows <= kFew && rows <= dim / 4);
   if (p.keep) p.z = take(size_t(rows) * size_t(p.piece) * 4);
   if (backward) {
@@ -808,6 +808,10 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       join_dw(dwp, p.dw_splits.count, p.piece * E, n, to);
     }
   };
+  auto d_of_scores = [&](const float* z, __bf16* to, const Fragments& f) {
+    hipLaunchKernelGGL(few_d, dim3(unsigned(up(int64_t(N) * (p.piece / 8), kBlock))), dim3(kBlock), 0, st, z,
+                       fast_div(uint32_t(p.piece / 8)), V, rows.tokens, unit, &head->live, to, dplane, p.terms, f);
+  };
   if constexpr (TERMS == 3) {
     if (p.few_wide) {
       const bool back = dx != nullptr || dw != nullptr;
@@ -815,14 +819,13 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
       const int32_t tiles = int32_t(up(N, 32));
       const Fragments xf = {reinterpret_cast<__bf16*>(ws + p.xf), tiles};
       const Fragments df = {dx != nullptr ? reinterpret_cast<__bf16*>(ws + p.df) : nullptr, tiles};
-      hipLaunchKernelGGL(few_x, dim3(unsigned(up(p.padded / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, xp, xplane,
-                         p.padded, &head->live, xf);
+      hipLaunchKernelGGL(few_x, dim3(unsigned(up(int64_t(N) * (p.padded / 8), kBlock))), dim3(kBlock), 0, st, xp,
+                         xplane, fast_div(uint32_t(p.padded / 8)), &head->live, xf);
       launch_few_scores(w, a.table_stride, V, E, N, xf, &head->live, z, p.piece,
                         StatsEpi<false>{parts, N, rows.tokens, rows.target, unit, 0, V, nullptr, 0}, st);
       join_sums(int32_t(up(V, 32)), true, true);
       if (!back) return hipGetLastError();
-      hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, z, p.piece,
-                         V, rows.tokens, unit, &head->live, dw != nullptr ? d : nullptr, dplane, 3, df);
+      d_of_scores(z, dw != nullptr ? d : nullptr, df);
       if (dx != nullptr) {
         launch_few_dx(w, a.table_stride, V, E, N, df, &head->live, p.few_parts, dxp,
                       int64_t(N) * E, st);
@@ -859,8 +862,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
           g, GradEpi<terms.value>{d, p.piece, dplane, rows.tokens, unit, v0, n, &head->live, p.few}, ss, st);
     };
     if (kept != nullptr)
-      hipLaunchKernelGGL(few_d, dim3(unsigned(up(p.piece / 8, kBlock)), unsigned(N)), dim3(kBlock), 0, st, kept,
-                         p.piece, V, rows.tokens, unit, &head->live, d, dplane, p.terms, Fragments{nullptr, 0});
+      d_of_scores(kept, d, Fragments{nullptr, 0});
     else if constexpr (TERMS == 3)
       grad(std::integral_constant<int, 3>());
     else if (p.terms == 2)

@@ -50,14 +50,15 @@ struct Fragments {
 };
 
 // x's terms from their planes.
-__global__ __launch_bounds__(kBlock) void few_x(const __bf16* __restrict__ x, int64_t plane, int32_t padded,
+__global__ __launch_bounds__(kBlock) void few_x(const __bf16* __restrict__ x, int64_t plane, FastDiv chunks,
                                                 const int32_t* __restrict__ rows, Fragments to) {
-  const int at = blockIdx.y, k = (int(blockIdx.x) * kBlock + int(threadIdx.x)) * 8;
-  if (at >= *rows || k >= padded) return;
+  const uint32_t i = blockIdx.x * kBlock + threadIdx.x, at = quotient(i, chunks);
+  if (int(at) >= *rows) return;
+  const int padded = int(chunks.div) * 8, k = int(i - at * chunks.div) * 8;
   u4 t[3];
 #pragma unroll
   for (int p = 0; p < 3; ++p) t[p] = *reinterpret_cast<const u4*>(x + p * plane + int64_t(at) * padded + k);
-  to.store(k, at, t);
+  to.store(k, int(at), t);
 }
 
 // 4 elements on their way (zeros past the row), untouched until values().
@@ -86,13 +87,14 @@ struct Four<__bf16> {
 template <int TM, class TW, class Stats>
 __global__ __launch_bounds__(kBlock) void few_scores(const TW* __restrict__ w, int64_t stride, int64_t vocab,
                                                      int32_t dim, Fragments x, const int32_t* __restrict__ rows,
-                                                     float* __restrict__ scores, int64_t pitch, Stats stats) {
+                                                     float* __restrict__ scores, int64_t pitch, uint32_t blocks,
+                                                     Stats stats) {
   __shared__ f4 shared[kWavesPerBlock][TM][4][kWave];
   __shared__ f4 turn[kWavesPerBlock][32][8];
   const int lane = lane_id(), wave = wave_id(), row = lane % 32, half = lane / 32;
-  const int row0 = int(blockIdx.y) * kFewBlock, live = scalar(*rows) - row0;
+  const int row0 = int(blockIdx.x / blocks) * kFewBlock, live = scalar(*rows) - row0;
   if (live <= 0) return;
-  const int64_t n0 = int64_t(blockIdx.x) * 32;
+  const int64_t n0 = int64_t(blockIdx.x % blocks) * 32;
   // Load i: rows 8 i to 8 i + 7, 8 lanes each.
   const TW* p[4];
 #pragma unroll
@@ -163,13 +165,13 @@ __global__ __launch_bounds__(kBlock) void few_scores(const TW* __restrict__ w, i
 
 // D of the rows that count, in three terms, from their scores: 8 columns per thread, zeros past the table.  In
 // fragments for dx's product above (`f` not empty); `planes` planes of it for the tiles' (`d` not null).
-__global__ __launch_bounds__(kBlock) void few_d(const float* __restrict__ scores, int64_t pitch, int64_t vocab,
+__global__ __launch_bounds__(kBlock) void few_d(const float* __restrict__ scores, FastDiv chunks, int64_t vocab,
                                                 const Token* __restrict__ tokens, float unit,
                                                 const int32_t* __restrict__ rows, __bf16* __restrict__ d,
                                                 int64_t plane, int planes, Fragments f) {
-  const int at = blockIdx.y;
-  const int64_t n = (int64_t(blockIdx.x) * kBlock + threadIdx.x) * 8;
-  if (at >= *rows || n >= pitch) return;
+  const uint32_t chunk = blockIdx.x * kBlock + threadIdx.x, q = quotient(chunk, chunks);
+  if (int(q) >= *rows) return;
+  const int64_t at = q, pitch = int64_t(chunks.div) * 8, n = int64_t(chunk - q * chunks.div) * 8;
   const Token t = tokens[at];
   const float c = t.inv * t.ratio;
   const f4 lo = load4(scores + at * pitch + n), hi = load4(scores + at * pitch + n + 4);
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(kBlock) void few_d(const float* __restrict__ scores
   }
   u4 terms[3];
   nearest_terms(v, terms);
-  if (f.data != nullptr) f.store(n, at, terms);
+  if (f.data != nullptr) f.store(n, int(at), terms);
   if (d == nullptr) return;
 #pragma unroll
   for (int k = 0; k < 3; ++k)
@@ -206,22 +208,24 @@ __device__ __forceinline__ void load_some(const __bf16* p, float (&v)[2]) {
   v[0] = bf16_lo(x), v[1] = bf16_hi(x);
 }
 
-// Part blockIdx.y of dx = D W: 32 TN columns of the table, `per` chunks of 16 of its rows, which the wavefronts
+// A part of `count` of dx = D W: 32 TN columns of the table, `per` chunks of 16 of its rows, which the wavefronts
 // take in turn.  A lane's TN elements are of TN tiles (tile t's row i is column TN i + t), so that a row is read
 // in wide pieces; the wavefronts' sums are joined in order.
 template <int TM, int TN, class TW>
 __global__ __launch_bounds__(kBlock) void few_dx(const TW* __restrict__ w, int64_t stride, int64_t vocab,
                                                  int32_t dim, Fragments d, const int32_t* __restrict__ rows,
-                                                 int32_t per, float* __restrict__ parts, int64_t part) {
+                                                 int32_t per, float* __restrict__ parts, int64_t part,
+                                                 uint32_t columns, uint32_t count) {
   constexpr int GROUP = 4 / TN;  // tiles of rows that are joined at a time
   static_assert(TN <= 4 && TM % GROUP == 0, "join");
   __shared__ f4 shared[kWavesPerBlock][GROUP][TN][4][kWave];
   const int lane = lane_id(), wave = wave_id(), row = lane % 32, half = lane / 32;
-  const int row0 = int(blockIdx.z) * kFewBlock, live = scalar(*rows) - row0;
+  const uint32_t z = blockIdx.x / columns % count;
+  const int row0 = int(blockIdx.x / columns / count) * kFewBlock, live = scalar(*rows) - row0;
   if (live <= 0) return;
-  const int e0 = int(blockIdx.x) * 32 * TN, e = e0 + row * TN;
+  const int e0 = int(blockIdx.x % columns) * 32 * TN, e = e0 + row * TN;
   const bool in = e < dim;
-  const int64_t first = int64_t(blockIdx.y) * per * 16;
+  const int64_t first = int64_t(z) * per * 16;
   const int64_t end = first + int64_t(per) * 16 < vocab ? first + int64_t(per) * 16 : vocab;
   const TW* p = w + (in ? e : 0);
   f16v acc[TN][TM];
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(kBlock) void few_dx(const TW* __restrict__ w, int64
         for (int t = 0; t < TN; ++t) six_products(a[t], b[j], acc[t][j]);
       }
   }
-  float* out = parts + blockIdx.y * part;
+  float* out = parts + z * part;
 #pragma unroll
   for (int g = 0; g < TM; g += GROUP) {
     if (g * 32 >= live) break;
@@ -313,10 +317,11 @@ inline int32_t few_parts(int32_t rows, int64_t vocab, int32_t dim) {
 template <class TW, class Stats>
 void launch_few_scores(const TW* w, int64_t stride, int64_t vocab, int32_t dim, int32_t rows, const Fragments& x,
                        const int32_t* live, float* scores, int64_t pitch, const Stats& stats, hipStream_t st) {
-  const dim3 grid(unsigned((vocab + 31) / 32), unsigned((rows + kFewBlock - 1) / kFewBlock));
+  const uint32_t blocks = uint32_t((vocab + 31) / 32);
+  const dim3 grid(blocks * uint32_t((rows + kFewBlock - 1) / kFewBlock));
   auto run = [&](auto tm) {
     hipLaunchKernelGGL((few_scores<tm.value, TW, Stats>), grid, dim3(kBlock), 0, st, w, stride, vocab, dim, x, live,
-                       scores, pitch, stats);
+                       scores, pitch, blocks, stats);
   };
   if (rows > 64)
     run(std::integral_constant<int, 4>());
@@ -333,10 +338,10 @@ void launch_few_dx(const TW* w, int64_t stride, int64_t vocab, int32_t dim, int3
   const int32_t per = int32_t((chunks + count - 1) / count);
   auto run = [&](auto tm, auto tn) {
     constexpr int COLUMNS = 32 * tn.value;
-    const dim3 grid(unsigned((dim + COLUMNS - 1) / COLUMNS), unsigned(count),
-                    unsigned((rows + kFewBlock - 1) / kFewBlock));
+    const uint32_t columns = uint32_t((dim + COLUMNS - 1) / COLUMNS);
+    const dim3 grid(columns * uint32_t(count) * uint32_t((rows + kFewBlock - 1) / kFewBlock));
     hipLaunchKernelGGL((few_dx<tm.value, tn.value, TW>), grid, dim3(kBlock), 0, st, w, stride, vocab, dim, d, live, per,
-                       parts, part);
+                       parts, part, columns, uint32_t(count));
   };
   if (rows > 64)
     run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
