@@ -182,7 +182,14 @@ __global__ __launch_bounds__(kBlock) void few_d(const float* __restrict__ scores
     v[i] = n + i >= vocab ? 0.f : n + i == t.label ? (e * t.inv - 1.f) * t.ratio : e * c;
   }
   u4 terms[3];
-  nearest_terms(v, terms);
+  if (planes == 3) {
+    nearest_terms(v, terms);
+  } else {  // (Two terms: a NaN has to be in the first.)
+    terms[0] = pack16(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] -= (i % 2 ? bf16_hi : bf16_lo)(terms[0][i / 2]);
+    terms[1] = terms[2] = pack16(v);
+  }
   if (f.data != nullptr) f.store(n, int(at), terms);
   if (d == nullptr) return;
 #pragma unroll

@@ -87,10 +87,10 @@ def test_each_output_alone_and_again(N):
     assert torch.equal(run(x, w, labels, dx=False)[2], dw)
 
 
-@pytest.mark.parametrize("N", [3, 70, 300])
-def test_a_row_with_nan_or_infinity_keeps_it(N):
-    """The other rows' losses and gradients are the same bits; the table's gradient takes the row's NaN."""
-    x, w, labels = inputs(N, 500, 260, 5, "f32", "f32", ignored=0.0)
+@pytest.mark.parametrize("N,t", [(3, "f32"), (70, "f32"), (300, "f32"), (3, "bf16"), (60, "bf16"), (70, "bf16")])
+def test_a_row_with_nan_or_infinity_keeps_it(N, t):
+    """The other rows' losses and gradients are the same bits; the row's own, and the table's, are NaN."""
+    x, w, labels = inputs(N, 500, 260, 5, t, t, ignored=0.0)
     loss, dx, _ = run(x, w, labels)
     for bad in (float("nan"), float("inf")):
         y = x.clone()
@@ -98,4 +98,4 @@ def test_a_row_with_nan_or_infinity_keeps_it(N):
         got = run(y, w, labels)
         keep = torch.arange(N, device=DEV) != 1
         assert torch.equal(got[0][keep], loss[keep]) and torch.equal(got[1][keep], dx[keep])
-        assert not torch.isfinite(got[0][1]) and torch.isnan(got[2]).any()
+        assert not torch.isfinite(got[0][1]) and torch.isnan(got[1][1]).all() and torch.isnan(got[2]).all(1).any()
