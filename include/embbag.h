@@ -584,7 +584,7 @@ int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStr
  * grad_x may be x itself with the same stride.  A label >= vocab is a data error; its row
  * is left out then.  Scores and sums are FP32.  BF16 sides: q - [v == label], times w
  * over the largest weight, is rounded to BF16 (two terms of it where at most 256 rows
- * count, or over small tables) for the gradients' products.  If either side is FP32 both
+ * count, whatever `rows` is, or vocab is below 1024) for the gradients' products.  If either side is FP32 both
  * enter with 24 bits.  An infinity in a row of either side makes its scores infinite or NaN.
  * `workspace`: 256-byte aligned; `type` is EMBBAG_F32 if either side is FP32, `backward`
  * whether a gradient is wanted.  It holds a piece of the vocabulary's q at a time (at most

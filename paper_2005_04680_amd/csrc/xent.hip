@@ -13,7 +13,8 @@
 // All sums are in orders that the sizes determine; there are no atomics on them.
 //
 // BF16 operands are taken as they are.  D is rounded to BF16 (2^-8 of each element at most, as the
-// gradients' own rounding; two terms of it where few rows count and the products do not bound the call).
+// gradients' own rounding; two terms of it where few rows count, so that the products do not bound the call, or the
+// table is small).
 // With the weights' ratio in D, equal weights leave the label's element, next to -1, almost exact.  FP32
 // operands, and D with them, are the sum of three BF16 terms, of whose nine products six are taken: what
 // is left out is below 2^-22 of each product.  Where scores cost more to compute again than to keep (FP32 sides,
@@ -30,7 +31,6 @@
 namespace embbag {
 namespace {
 
-constexpr int32_t kFew = 256;                          // rows whose D has two terms
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of D, of W's terms: a piece's
 constexpr int kRowsAtOnce = 4096;                     // rows whose places 1024 threads find in a round
 constexpr int64_t kMaxPitch = int64_t(1) << 19;       // elements of a row of D
@@ -355,7 +355,7 @@ __device__ __forceinline__ void turn_rows(T* turn, const f16v (&acc)[TN][TM], in
 }
 
 // A tile of D (times the weights' ratio): TERMS planes [live][pitch], zeros in the columns past the
-// vocabulary.
+// vocabulary.  Of two the second is stored only where at most `few` rows count.
 template <int TERMS>
 struct GradEpi {
   __bf16* d;
@@ -363,7 +363,6 @@ struct GradEpi {
   const Token* tokens;
   float unit;
   int64_t first, columns;
-  // With two terms: the largest number of rows that count for which the second is stored.
   const int32_t* live;
   int32_t few;
   template <int TN, int TM>
@@ -606,14 +605,11 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   Plan p = {};
   p.f32 = f32;
   const int planes = f32 ? 3 : 1;
-  // A second term of D where few rows count: the products' time is W's way from memory then, and the few
-  // roundings of labels' elements do not average out.  (Whether they do is known on the device; room for the
-  // term is taken where D is small.)  Over fewer than 1024 entries the element, 1 - p, is off by as much as p
-  // in the same direction in every row, and the term stays.
-  const bool small = vocab < 1024;
-  p.terms = f32 ? 3 : rows <= kFew || small || rows * vocab <= kPieceBytes / 2 ? 2 : 1;
-  p.few = small ? INT32_MAX : kFew;
-  p.pairs = f32 ? 6 : p.terms;
+  p.terms = f32 ? 3 : 2;
+  p.few = few_of(vocab);
+  p.pairs = f32 ? 6 : 2;
+  // Rows of D's planes in all: a second term is that of at most `few` rows, which come first.
+  const int64_t d_rows = f32 ? int64_t(rows) * 3 : int64_t(rows) + (rows < p.few ? rows : p.few);
   p.narrow = dim <= kNarrow;
   p.few_wide = f32 && !p.narrow && few_wide(rows, dim) && vocab <= kMaxPitch &&
                (!backward || rows * up(vocab, 256) * 256 * 6 <= kPieceBytes * 2);
@@ -649,7 +645,7 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
     if (piece > v) piece = v;
   };
   at_most(kMaxPitch);
-  if (backward) at_most(kPieceBytes * 2 / (int64_t(rows > 0 ? rows : 1) * 2 * p.terms));
+  if (backward) at_most(kPieceBytes * 2 / (int64_t(rows > 0 ? rows : 1) * 2 * (f32 ? 3 : rows <= p.few ? 2 : 1)));
   if (p.pack) at_most(kPieceBytes * 2 / (int64_t(p.padded) * 2 * planes));
   const int64_t pieces = up(vocab, piece);
   p.piece = up(up(vocab, pieces), 256) * 256;  // pieces of one size
@@ -673,7 +669,7 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
            rows * p.piece * 4 <= kPieceBytes * 2 && (f32 ? dim >= 192 : rows <= kFew && rows <= dim / 4);
   if (p.keep) p.z = take(size_t(rows) * size_t(p.piece) * 4);
   if (backward) {
-    p.d = take(size_t(rows) * size_t(p.piece) * 2 * p.terms);
+    p.d = take(size_t(d_rows) * size_t(p.piece) * 2);
     // dx: the larger tiles where they, split, leave few compute units idle.
     const int64_t psteps = up(p.piece, kStepK);
     p.dx = {256, 256};
@@ -765,7 +761,7 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     }
   };
   if (p.narrow) {
-    NarrowArgs q = {p.nar, p.f32 ? 3 : N <= kFew ? 2 : 1, w, sizeof(TW) == 2, a.table_stride, xp, xplane, head,
+    NarrowArgs q = {p.nar, p.f32 ? 3 : N <= p.few ? 2 : 1, p.few, w, sizeof(TW) == 2, a.table_stride, xp, xplane, head,
                     rows.tokens, rows.target,
                     unit, parts, dxp, dw, sizeof(TW) == 2, a.grad_table_stride, &head->factor_w};
     hipError_t e = launch_narrow_scores(q, st);
@@ -863,12 +859,8 @@ hipError_t launch_types(const embbag_xent_t& a, const Plan& p, char* ws, int32_t
     };
     if (kept != nullptr)
       d_of_scores(kept, d, Fragments{nullptr, 0});
-    else if constexpr (TERMS == 3)
-      grad(std::integral_constant<int, 3>());
-    else if (p.terms == 2)
-      grad(std::integral_constant<int, 2>());
     else
-      grad(std::integral_constant<int, 1>());
+      grad(std::integral_constant<int, TERMS == 3 ? 3 : 2>());
     if (dx != nullptr) {
       const Gemm gx = {wsd, ds, E, N, n, &head->live, p.pairs, p.dx_splits, blocks_of(p.dx), up(p.piece, kStepK), p.few};
       run_gemm<true, false, false>(gx, StoreEpi<float>{dxp, E, E, nullptr, -1, v0 > 0}, p.dx, st);

@@ -9,6 +9,13 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// D of BF16 sides has a second term where at most so many rows count, or the table has fewer rows than
+// kSmallTable: the few roundings of the labels' elements do not average out, and over a small table such an element,
+// 1 - p, is off by as much as p in the same direction in every row.  How many rows count is known on the device.
+constexpr int32_t kFew = 256;
+constexpr int64_t kSmallTable = 1024;
+inline int32_t few_of(int64_t vocab) { return vocab < kSmallTable ? INT32_MAX : kFew; }
+
 // Numbers as sums of three BF16 terms, each the nearest to what is left.  What BF16 cannot hold, beyond its
 // largest number (infinities and NaN too), comes in the last term, which meets the other side's first alone.
 __device__ __forceinline__ void nearest_terms(const float (&x)[8], u4 (&t)[3]) {
@@ -80,7 +87,8 @@ struct Narrow {
 Narrow narrow_plan(int32_t rows, int64_t vocab, int32_t dim, bool f32);
 struct NarrowArgs {
   Narrow n;
-  int terms;  // of D; of the sides 3 if that is 3, else 1
+  int terms;  // of D (1: 2 where at most `few` rows count); of the sides 3 if that is 3, else 1
+  int32_t few;
   const void* table;
   bool table_bf16;
   int64_t table_stride;

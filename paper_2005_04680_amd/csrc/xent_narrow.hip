@@ -541,18 +541,24 @@ __global__ __launch_bounds__(kBlock, 2) void narrow_scores(TokenArgs a) {
 
 // Both gradients, of which either may have no blocks: neither needs the other, and one launch leaves no
 // compute unit idle between them.  Blocks from `turn` on are of the second kind; dx is the first kind if
-// `dx_first`.
+// `dx_first`.  With PD == 1 D has two terms where at most `few` rows count.
 template <int EP, int P, int PD, int WM, class TW, class TO>
 __global__ __launch_bounds__(kBlock, 2) void narrow_gradients(TokenArgs t, VocabArgs v, uint32_t first,
-                                                              uint64_t turn, bool dx_first) {
+                                                              uint64_t turn, bool dx_first, int32_t few) {
   extern __shared__ __align__(16) uint8_t lds[];
   const uint64_t block = uint64_t(first) + blockIdx.x;
   const bool second = block >= turn;
   const uint32_t at = uint32_t(second ? block - turn : block);
-  if (second != dx_first)
-    narrow_tokens<EP, P, PD, WM, true, TW>(t, at, lds);
-  else
-    narrow_vocab<EP, P, PD, TW, TO>(v, at, lds);
+  auto run = [&](auto terms) {
+    if (second != dx_first)
+      narrow_tokens<EP, P, terms.value, WM, true, TW>(t, at, lds);
+    else
+      narrow_vocab<EP, P, terms.value, TW, TO>(v, at, lds);
+  };
+  if constexpr (PD == 1) {
+    if (__builtin_amdgcn_readfirstlane(t.head->live) <= few) return run(std::integral_constant<int, 2>());
+  }
+  run(std::integral_constant<int, PD>());
 }
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -597,7 +603,7 @@ void launch_both(const NarrowArgs& n, hipStream_t st) {
   const bool dx_first = int64_t(n.n.per) * n.n.bm > int64_t(n.n.dw_per) * BV;
   for_launches(nx + nw, kBlock, [&](uint32_t first, dim3 grid) {
     hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, st, token_args(n), vocab_args(n), first,
-                       uint64_t(dx_first ? nx : nw), dx_first);
+                       uint64_t(dx_first ? nx : nw), dx_first, n.few);
   });
 }
 
