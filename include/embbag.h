@@ -587,8 +587,10 @@ int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStr
  * count, whatever `rows` is, or vocab is below 1024) for the gradients' products.  If either side is FP32 both
  * enter with 24 bits.  An infinity in a row of either side makes its scores infinite or NaN.
  * `workspace`: 256-byte aligned; `type` is EMBBAG_F32 if either side is FP32, `backward`
- * whether a gradient is wanted.  It holds a piece of the vocabulary's q at a time (at most
- * about 512 MB of it, or 256 columns; twice that and the scores of few or FP32 rows). */
+ * whether a gradient is wanted.  It holds x's rows as BF16 (of FP32 three numbers for each, of few rows twice),
+ * FP32 sums of grad_x, and of a piece of the vocabulary at a time at most 512 MB each (or 256 columns) of the
+ * rows' sums, of an FP32 table's three numbers, of q - [v == label], its second term and the scores of few or FP32
+ * rows. */
 typedef struct {
   int32_t rows;
   int32_t dim;

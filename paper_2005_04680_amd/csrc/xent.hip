@@ -647,6 +647,9 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   at_most(kMaxPitch);
   if (backward) at_most(kPieceBytes * 2 / (int64_t(rows > 0 ? rows : 1) * 2 * (f32 ? 3 : rows <= p.few ? 2 : 1)));
   if (p.pack) at_most(kPieceBytes * 2 / (int64_t(p.padded) * 2 * planes));
+  // The parts of the rows' sums, of 32 columns each at least (few rows) or 64: the only limit of many rows without
+  // gradients (2^20 x 2^20: 32 GB otherwise).
+  at_most(kPieceBytes * 2 / (int64_t(rows > 0 ? rows : 1) * int64_t(sizeof(float2))) * (rows <= 64 ? 32 : 64));
   const int64_t pieces = up(vocab, piece);
   p.piece = up(up(vocab, pieces), 256) * 256;  // pieces of one size
   p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);

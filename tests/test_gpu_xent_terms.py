@@ -62,3 +62,13 @@ def test_one_row_more(N, V, E):
 @pytest.mark.parametrize("N,V,E", [(600, 500, 64), (513, 1023, 128), (600, 40, 36), (600, 1023, 132)])
 def test_small_tables(N, V, E):
     check_two_terms(*counting(N, V, E, N, N + V))
+
+
+def test_pieces_without_gradients():
+    """So many rows that the loss alone takes the vocabulary in pieces: 2^20 rows, 4096 columns at a time."""
+    N, V = 1 << 20, 10001
+    x, w, labels = counting(N, V, 132, 300, 5)
+    r = torch.nonzero(labels >= 0)[:, 0]
+    loss = run(x, w, labels, dx=False, dw=False)[0]
+    close(loss[r], expected(x[r], w, labels[r])[0], "loss")
+    assert int((loss != 0).sum()) <= 300
