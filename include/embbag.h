@@ -455,8 +455,8 @@ int embbag_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t r
 
 /* RMS norm of rows with the residual's addition.  For every row, in FP64:
  *   h = x + residual,   sum_out = h,   out = h / sqrt(mean(h^2) + eps) * weight,
- * and the 8-bit rows (codes, scales) hold `out` as FP32, before its rounding to BF16.  Each
- * output is rounded once, through FP32; `out` comes from the sum before it is rounded.
+ * and the 8-bit rows (codes, scales) hold `out`.  sum_out and `out` are these values rounded to FP32,
+ * and the 8-bit rows and BF16 outputs are rounded from that; `out` comes from the sum before it is rounded.
  * x [rows][dim] of x_type, residual and sum_out of residual_type, out of out_type:
  * row strides in elements and alignments as embbag_mx4_quantize's src.  weight [dim]
  * of weight_type, aligned as a row, null for ones.  eps: positive.  residual, sum_out,

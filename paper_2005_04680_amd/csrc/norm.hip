@@ -4,10 +4,11 @@
 // A row lives in the registers of T threads, 8 consecutive elements (a chunk) at a
 // time: every input is read once and every output written once.  The sum of
 // squares is FP64, so that it neither overflows nor loses small rows (an FP32 square does beyond
-// 1.8e19 and below 1e-23).  The forward's outputs are FP64 to their one rounding: an 8-bit code lies next to
-// a border of its rounding often enough that FP32's last bits move codes (16M elements: some tens, 2^-4
-// of the element each).  The gradient works in FP32, its factor 1/sqrt as a power of two and a rest: its
-// exponent scales the elements first, which is exact.
+// 1.8e19 and below 1e-23).  The forward's outputs are FP64 to their rounding to FP32, from which BF16 and 8-bit
+// rows are rounded: an element lies next to a border of E4M3's rounding often enough that the last bits of FP32
+// arithmetic move codes (of 16M elements some tens, 2^-4 of the element each; the one rounding to FP32 about 9, which
+// then are those of `out` and not of the exact norm).  The gradient works in FP32, its factor 1/sqrt as a power
+// of two and a rest: its exponent scales the elements first, which is exact.
 //
 // Bound by bytes; the next row's loads are on their way during a row (16384 x 4096 BF16 gradient 171 us without,
 // 115 with).  Measured, us: 16384 x 4096 BF16 with a residual 102 (537 MB at 5.26 TB/s; a copy 5.24), 4096 x 4096
