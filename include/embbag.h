@@ -489,8 +489,9 @@ int embbag_rmsnorm(const embbag_rmsnorm_t* args, hipStream_t stream);
 /* Its gradients.  With n = h / sqrt(mean(h^2) + eps) and g = dy * weight,
  *   dh = (g - n * mean(n * g)) / sqrt(mean(h^2) + eps) + dsum,
  *   dweight = sum over the rows of dy * n,
- * where h is the sum that the norm was taken of (sum_out, or x without a residual), dy
- * the gradient of `out` and dsum that of sum_out (null: 0).  dh is the gradient of x
+ * where h is the row that the norm is taken of (sum_out, or x without a residual), dy
+ * the gradient of `out` and dsum that of sum_out (null: 0).  A BF16 sum_out is that row rounded, and the
+ * gradient is the norm's at the rounded row.  dh is the gradient of x
  * and of the residual alike.  dy [rows][dim] of dy_type; h, dsum and dh of h_type;
  * strides and alignments as above; weight as above; dweight [dim] of weight_type (of
  * dy_type where weight is null), null if it is not wanted.  dh may be dsum, h or dy

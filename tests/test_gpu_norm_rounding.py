@@ -64,3 +64,28 @@ def test_codes_are_those_of_the_exact_norm_but_next_to_a_midpoint(rows, dim):
     same = codes[:, :nb * 32] == got[:, :nb * 32]
     assert (same | near | np.repeat(edge, 32, 1)).all()
     assert (got[:, nb * 32:] == 0).all()
+
+
+@pytest.mark.parametrize("rows,dim", [(3, 36), (17, 516), (4, 4100), (300, 64)])
+def test_forward_and_back_over_a_bf16_stream(rows, dim):
+    """The gradient is that of the norm of the row it is given: exactly so of a BF16 sum_out, which is the forward's row
+    with each element off by half a step of BF16, d = 2^-8 of itself.  Beside the forward's own row: 1/rms is off by d (of
+    its size), n by 2 d, so mean(n g) by 2 d of mean|n g|, n * mean by 4 d, and the whole, times 1/rms, by 5 d;
+    dweight by 2 d of the sum of |dy n|.  (Squares of d: another d in all.)"""
+    seed = rows + dim
+    x, r, w = rows_of(rows, dim, seed, "bf16"), rows_of(rows, dim, seed + 1, "bf16"), weight_of(dim, seed + 2, "f32")
+    dy = rows_of(rows, dim, seed + 3, "bf16")
+    out, s = (torch.empty(rows, dim, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    pk.check(pk.embbag_rmsnorm(dev(x), dev(w), 1e-6, out=out, residual=dev(r), sum_out=s))
+    assert torch.equal(s, (dev(x).float() + dev(r).float()).bfloat16())
+    dh, dw = torch.empty_like(s), torch.empty(dim, device=DEV)
+    ws = torch.empty(pk.embbag_rmsnorm_grad_workspace_bytes(rows, dim), dtype=torch.uint8, device=DEV)
+    pk.check(pk.embbag_rmsnorm_grad(dev(dy), s, dev(w), 1e-6, dh, ws, dweight=dw))
+    want, wdw, size, dwsize = ref.rmsnorm_grad(host(dy), host(s), host(w), 1e-6)
+    close(dh, want, GRAD_U * U * size + rounding(want, "bf16"), "dh of the rounded row")
+    close(dw, wdw, (rows + 8) * U * dwsize + rounding(wdw, "f32"), "dw of the rounded row")
+    d = 2.0 ** -8
+    want, wdw, size, dwsize = ref.rmsnorm_grad(host(dy), host(x) + host(r), host(w), 1e-6)
+    tol = (GRAD_U * U + 6 * d) * size
+    close(dh, want, tol + rounding(np.abs(want) + tol, "bf16"), "dh")
+    close(dw, wdw, ((rows + 8) * U + 3 * d) * dwsize, "dw")
