@@ -415,9 +415,10 @@ int embbag_mx4_matmul(const void* x, int32_t x_type, int64_t x_stride, int32_t m
 
 /* The same scores from 8-bit rows (EMBBAG_MX8_CODE_BYTES; defined below), which embbag_rmsnorm
  * writes: out[i][j] = sum over e of x[i][e] * W[j][e], exact products.  Into FP32 the sums are FP32
- * (values of either side below 2^-126 may count as 0); into BF16 the matrix instructions add eight products
- * at a time, of which bits more than 13 below the largest product's highest are dropped, and those
- * sums in FP32.  Its gradient with respect to the rows' values is embbag_mx4_matmul_grad. */
+ * (values of either side below 2^-126 may count as 0, of 2^128 and more are infinite); into BF16 the
+ * matrix instructions add eight products at a time, of which bits more than 13 below the largest product's highest
+ * are dropped (at most 2^-10 of the sum of the products' magnitudes, which shows where large ones cancel), and
+ * those sums in FP32.  Its gradient with respect to the rows' values is embbag_mx4_matmul_grad. */
 size_t embbag_mx4_matmul_x8_workspace_bytes(int32_t m, int64_t n, int32_t k);
 int embbag_mx4_matmul_x8(const uint8_t* x_codes, const uint8_t* x_scales, int32_t m,
                          const uint8_t* codes, const uint8_t* scales, int64_t n, int32_t k, void* out,
@@ -444,7 +445,8 @@ int embbag_mx4_matmul_grad(const void* dy, int32_t dy_type, int64_t dy_stride, i
  *   scales [rows][EMBBAG_MX4_SCALE_BYTES(E)] uint8, 4-byte aligned, as a table's.
  * A block whose largest magnitude is a has the scale 2^e with the smallest e >= -127
  * for which a <= 448 * 2^e, and each element x the code nearest to x * 2^-e, ties to
- * the even code: no element is off by more than half a step.  All-zero blocks and
+ * the even code: no element is off by more than half a step (magnitudes from 248 * 2^120 on round to
+ * 2^128, which reads back as an infinity).  All-zero blocks and
  * blocks with an infinity or a NaN as embbag_mx4_quantize's. */
 #define EMBBAG_MX8_CODE_BYTES(E) ((((int64_t)(E) + 127) / 128) * 128)
 
