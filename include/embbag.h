@@ -582,7 +582,8 @@ int embbag_logits_process(const embbag_logits_t* args, int32_t* d_status, hipStr
  * x [rows][dim] of x_type, table [vocab][dim] of table_type (for split tables the high
  * halves, as BF16), grad_x and grad_table (each nullable) of their sides' types: row
  * strides in elements and alignments as embbag_mx4_quantize's src, table_stride at most
- * 2^19.  labels: device int32 [rows], loss: FP32 [rows].  scale and row_weights: finite.  rows <= 2^20,
+ * 2^19.  labels: device int32 [rows], loss: FP32 [rows].  |scale| <= 2^127, row_weights and scale times
+ * the largest of them: finite.  rows <= 2^20,
  * vocab <= 2^31 - 1, rows * vocab <= 2^40.  Outputs must not overlap inputs, but
  * grad_x may be x itself with the same stride.  A label >= vocab is a data error; its row
  * is left out then.  Scores and sums are FP32.  BF16 sides: q - [v == label], times w

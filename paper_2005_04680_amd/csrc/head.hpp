@@ -265,6 +265,7 @@ hipError_t launch_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, in
 
 constexpr int32_t kMaxXentRows = 1 << 20;
 constexpr int64_t kMaxXentStride = int64_t(1) << 19;  // of the table: a tile's rows within 2^30 bytes
+constexpr float kMaxXentScale = 0x1p127f;  // times log2(e) it is finite
 size_t xent_workspace(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward);
 hipError_t launch_xent(const embbag_xent_t& a, char* ws, int32_t* status, hipStream_t st);
 

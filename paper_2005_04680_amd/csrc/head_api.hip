@@ -343,7 +343,7 @@ int embbag_xent(const embbag_xent_t* args, void* workspace, size_t workspace_byt
   if (args == nullptr) return EMBBAG_ERR_INVALID_ARG;
   const embbag_xent_t& a = *args;
   if (!xent_sizes_ok(a.rows, a.vocab, a.dim) || !type_ok(a.x_type) || !type_ok(a.table_type) ||
-      !(a.scale >= -3.4028234663852886e38f && a.scale <= 3.4028234663852886e38f))
+      !(a.scale >= -kMaxXentScale && a.scale <= kMaxXentScale))
     return EMBBAG_ERR_INVALID_ARG;
   if (!rows_ok(a.table, a.table_type, a.table_stride, a.dim) || a.table_stride > kMaxXentStride ||
       (a.grad_table != nullptr && !rows_ok(a.grad_table, a.table_type, a.grad_table_stride, a.dim)))
