@@ -2,8 +2,8 @@
 rows are the scores' matrix, all three learned; served from a 4-bit catalogue and 8-bit rows.
 
 A training step is
-  embbag_forward -> embbag_rmsnorm -> embbag_xent (the scores of the whole catalogue, never
-  stored) -> embbag_rmsnorm_grad -> embbag_backward_sgd, and plain SGD on the catalogue and
+  embbag_forward -> embbag_rmsnorm -> embbag_xent (the scores of the whole catalogue, kept
+  nowhere but in its workspace) -> embbag_rmsnorm_grad -> embbag_backward_sgd, and plain SGD on the catalogue and
   the norm's weights,
 and serving is
   embbag_forward -> embbag_rmsnorm (into 8 bits) -> embbag_mx4_matmul_x8 ->

@@ -226,13 +226,11 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t mtiles, uint32_t n
 // steps of all of them: those of the next tile are on their way while a tile is stored.
 //
 // 256 x 256 tiles keep the accumulators of a wavefront in 256 registers and read each fragment
-// from LDS for four products.
+// from LDS for four products.  Left out one at a time at 4096 x 65536 x 4096 with both sides in 4 bits (633 us with
+// strips of 8): loads to LDS 457, stores of the output 533, LDS reads and loads and stores 315.
 //
 // 8-bit rows (X8): a load brings 8 rows of 128 bytes, place j of row r holds chunk j ^ (r % 8); a
 // fragment is two chunks, 16 elements of the product's first block and 16 of its second.
-//
-// Left out one at a time at 4096 x 65536 x 4096 (633 us with
-// strips of 8): loads to LDS 457, stores of the output 533, LDS reads and loads and stores 315.
 template <bool X8, int TN, int TM, int WN, int WM, int STAGES, class T>
 __global__ __launch_bounds__(WN* WM* kWave, 1) void scores_tile(
     const uint8_t* __restrict__ xc, const uint32_t* __restrict__ xs, int64_t xpitch, int32_t m,
@@ -751,32 +749,30 @@ void launch_direct(const TX* x, int64_t stride, const uint8_t* xc, const uint32_
 template <bool X8, class T>
 void launch_tiles(const uint8_t* xc, const uint32_t* xs, const uint32_t* ws, int32_t m,
                   int32_t groups, const Mx4View& w, T* out, int64_t ldo, hipStream_t st) {
-  {
-    auto tiles = [&](int64_t bn, int64_t bm) {
-      return (w.rows + bn - 1) / bn * ((m + bm - 1) / bm);
-    };
-    auto rounds = [](int64_t t, int64_t resident) { return (t + resident - 1) / resident; };
-    // The largest tiles where the chip takes four rounds of them or more and those cost less than the
-    // rounds of the next size (a round of 256 of 256 x 256 about 10/7 of one of 512 of
-    // 128 x 128); smaller ones while they leave compute units idle.  Measured, us, 256 x 256 /
-    // 128 x 128 / 128 x 64 / 64 x 64: 4096 x 65536 x 4096 652 / 847 / 1653 / 1760; 1000 x 131072 x
-    // 4096 339 / 449 / 886 / 858; 4096 x 65536 x 256 153 / 180 / 282 / 319; 2000 x 20000 x 1024 57 /
-    // 49 / 70 / 73; 1024 x 8192 x 1024 19 / 16 / 18 / 20; 200 x 200003 x 256 42 / 31 / 38 / 41;
-    // 64 x 200003 x 1024 55 / 34 / 31 / 36; 512 x 4096 x 4096 31 / 17 / 23 / 20; 300 x 1000 x 4096
-    // 55 / 26 / 23 / 19.
-    const int64_t big = tiles(256, 256), mid = tiles(128, 128);
-    const int64_t big_rounds = rounds(big, kNumCu);
-    if constexpr (!kExact<X8, T>) {
-      if (m > 512 && big_rounds >= 4 && big_rounds * 10 < rounds(mid, 2 * kNumCu) * 7)
-        return launch_tile<X8, 4, 4, 2, 2, X8 ? 2 : 3, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
-    }
-    if (m > 64 && mid >= kNumCu / 2)
-      launch_tile<X8, 2, 2, 2, 2, X8 ? 2 : 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
-    else if (tiles(128, 64) >= kNumCu)
-      launch_tile<X8, 1, 2, 4, 1, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
-    else
-      launch_tile<X8, 1, 1, 2, 2, X8 ? 3 : 4, X8 ? 2 : 3>(xc, xs, m, groups, w, ws, out, ldo, st);
+  auto tiles = [&](int64_t bn, int64_t bm) {
+    return (w.rows + bn - 1) / bn * ((m + bm - 1) / bm);
+  };
+  auto rounds = [](int64_t t, int64_t resident) { return (t + resident - 1) / resident; };
+  // The largest tiles where the chip takes four rounds of them or more and those cost less than the
+  // rounds of the next size (a round of 256 of 256 x 256 about 10/7 of one of 512 of
+  // 128 x 128); smaller ones while they leave compute units idle.  Measured, us, 256 x 256 /
+  // 128 x 128 / 128 x 64 / 64 x 64: 4096 x 65536 x 4096 652 / 847 / 1653 / 1760; 1000 x 131072 x
+  // 4096 339 / 449 / 886 / 858; 4096 x 65536 x 256 153 / 180 / 282 / 319; 2000 x 20000 x 1024 57 /
+  // 49 / 70 / 73; 1024 x 8192 x 1024 19 / 16 / 18 / 20; 200 x 200003 x 256 42 / 31 / 38 / 41;
+  // 64 x 200003 x 1024 55 / 34 / 31 / 36; 512 x 4096 x 4096 31 / 17 / 23 / 20; 300 x 1000 x 4096
+  // 55 / 26 / 23 / 19.
+  const int64_t big = tiles(256, 256), mid = tiles(128, 128);
+  const int64_t big_rounds = rounds(big, kNumCu);
+  if constexpr (!kExact<X8, T>) {
+    if (m > 512 && big_rounds >= 4 && big_rounds * 10 < rounds(mid, 2 * kNumCu) * 7)
+      return launch_tile<X8, 4, 4, 2, 2, X8 ? 2 : 3, 1>(xc, xs, m, groups, w, ws, out, ldo, st);
   }
+  if (m > 64 && mid >= kNumCu / 2)
+    launch_tile<X8, 2, 2, 2, 2, X8 ? 2 : 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
+  else if (tiles(128, 64) >= kNumCu)
+    launch_tile<X8, 1, 2, 4, 1, 3, 2>(xc, xs, m, groups, w, ws, out, ldo, st);
+  else
+    launch_tile<X8, 1, 1, 2, 2, X8 ? 3 : 4, X8 ? 2 : 3>(xc, xs, m, groups, w, ws, out, ldo, st);
 }
 
 template <class T>

@@ -31,7 +31,7 @@
 namespace embbag {
 namespace {
 
-constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of D, of W's terms: a piece's
+constexpr int64_t kPieceBytes = int64_t(512) << 20;   // of D, W's terms, the sums' parts or kept scores: at most, each
 constexpr int kRowsAtOnce = 4096;                     // rows whose places 1024 threads find in a round
 constexpr int64_t kMaxPitch = int64_t(1) << 19;       // elements of a row of D
 
@@ -612,7 +612,7 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   const int64_t d_rows = f32 ? int64_t(rows) * 3 : int64_t(rows) + (rows < p.few ? rows : p.few);
   p.narrow = dim <= kNarrow;
   p.few_wide = f32 && !p.narrow && few_wide(rows, dim) && vocab <= kMaxPitch &&
-               (!backward || rows * up(vocab, 256) * 256 * 6 <= kPieceBytes * 2);
+               (!backward || rows * up(vocab, 256) * 256 * 6 <= kPieceBytes);
   p.pack = (f32 || dim % 8 != 0) && !p.few_wide;
   p.padded = (dim + kStepK - 1) / kStepK * kStepK;
   size_t at = 256;
@@ -645,11 +645,11 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
     if (piece > v) piece = v;
   };
   at_most(kMaxPitch);
-  if (backward) at_most(kPieceBytes * 2 / (int64_t(rows > 0 ? rows : 1) * 2 * (f32 ? 3 : rows <= p.few ? 2 : 1)));
-  if (p.pack) at_most(kPieceBytes * 2 / (int64_t(p.padded) * 2 * planes));
+  if (backward) at_most(kPieceBytes / (int64_t(rows > 0 ? rows : 1) * 2 * (f32 ? 3 : rows <= p.few ? 2 : 1)));
+  if (p.pack) at_most(kPieceBytes / (int64_t(p.padded) * 2 * planes));
   // The parts of the rows' sums, of 32 columns each at least (few rows) or 64: the only limit of many rows without
   // gradients (2^20 x 2^20: 32 GB otherwise).
-  at_most(kPieceBytes * 2 / (int64_t(rows > 0 ? rows : 1) * int64_t(sizeof(float2))) * (rows <= 64 ? 32 : 64));
+  at_most(kPieceBytes / (int64_t(rows > 0 ? rows : 1) * int64_t(sizeof(float2))) * (rows <= 64 ? 32 : 64));
   const int64_t pieces = up(vocab, piece);
   p.piece = up(up(vocab, pieces), 256) * 256;  // pieces of one size
   p.x = take(size_t(rows) * size_t(p.padded) * 2 * planes);
@@ -669,7 +669,7 @@ Plan plan_of(int32_t rows, int64_t vocab, int32_t dim, bool f32, bool backward) 
   // Of BF16 rows that are few beside dim, W's bytes once more do: 16 x 100000 x 512 130 / 114, 100 x 50000 x 1024
   // 164 / 147, 123 x 84048 x 492 209 / 197, 33 x 32001 x 136 45.8 / 45.6.
   p.keep = backward && !p.few_wide && pieces == 1 && rows > 0 &&
-           rows * p.piece * 4 <= kPieceBytes * 2 && (f32 ? dim >= 192 : rows <= kFew && rows <= dim / 4);
+           rows * p.piece * 4 <= kPieceBytes && (f32 ? dim >= 192 : rows <= kFew && rows <= dim / 4);
   if (p.keep) p.z = take(size_t(rows) * size_t(p.piece) * 4);
   if (backward) {
     p.d = take(size_t(d_rows) * size_t(p.piece) * 2);

@@ -10,7 +10,8 @@ other entry points (device pointers and the current HIP stream to the C ABI of
 ``embbag_mx8_dequantize``.  Logits:
 ``embbag_logits_process`` (penalties, biases, masks) and ``embbag_distill`` (loss
 and gradient against a teacher's top logits).  ``embbag_xent``: loss on labels over an
-FP32 or BF16 table, with the gradients of both sides, no logits kept.
+FP32 or BF16 table, with the gradients of both sides, in pieces of the vocabulary (the logits stay in the workspace
+only where they are few).
 """
 from __future__ import annotations
 
