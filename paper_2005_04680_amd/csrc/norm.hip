@@ -11,10 +11,11 @@
 // of two and a rest: its exponent scales the elements first, which is exact.
 //
 // Bound by bytes; the next row's loads are on their way during a row (16384 x 4096 BF16 gradient 171 us without,
-// 115 with).  Measured, us: 16384 x 4096 BF16 with a residual 102 (537 MB at 5.26 TB/s; a copy 5.24), 4096 x 4096
+// 118 with).  Measured, us: 16384 x 4096 BF16 with a residual 102 (537 MB at 5.26 TB/s; a copy 5.24), 4096 x 4096
 // BF16 with an FP32 residual into 8 bits 32 (185 MB at 5.8 TB/s, partly from the caches) and 9.5 to read
-// back, the gradient of 16384 x 4096 with dsum 115 (4.7 TB/s).  FP64 costs rows of more than 8192 elements 9 %
-// (1024 threads, 16 elements each, spill; 4000 x 16384 100 us in FP32, 109) and the others nothing.
+// back, the gradient of 16384 x 4096 with dsum 118 (4.6 TB/s).  FP64 costs rows of more than 8192 elements 9 %
+// (1024 threads, 16 elements each, spill; 4000 x 16384 100 us in FP32, 109) and the others nothing.  The gradient of such
+// rows has no room for the next one and spills too: 4000 x 16384 with dsum 192 us, 2.7 TB/s.
 #include <type_traits>
 
 #include "head.hpp"

@@ -22,8 +22,8 @@
 //
 // Four products, 8 N V E operations, where 6 N V E would do if the scores were kept: at 4096 x 131072 x 2048
 // they would be 2.1 GB written and read in FP32.  Bound by the products, with few rows by W's bytes.  Measured, us:
-// 4096 x 131072 x 2048 BF16 7020, 1999 x 50001 x 300 279, 1 x 200003 x 1024 without gradients 85 (410 MB at 4.8
-// TB/s).
+// 4096 x 131072 x 2048 BF16 7060, 1999 x 50001 x 300 (1200 rows count) 279, 2048 x 100003 x 512 (205 count, two terms
+// of D) 292, 1 x 200003 x 1024 without gradients 85 (410 MB at 4.8 TB/s).
 #include "gemm.hpp"
 #include "xent.hpp"
 #include "xent_few.hpp"
